@@ -488,6 +488,111 @@ BS_API bs_status bs_stack_backward_strided(const bs_stack *stack, const void *in
                                            uint64_t workspace_bytes, void *stream);
 
 /*
+ * Group normalisation with a residual operand and an activation, channels last: the normalisation of a network that is trained from
+ * scratch (its statistics are those of the image itself, the same in training and at inference), in one call with the element-wise
+ * layers that stand behind it (Section 2 lists them as what a stack is made of; Section 7 names training as the next step).
+ *   over each of the N * groups groups (H * W pixels of C / groups neighbouring channels):  xh = (x - mean) / sqrt(var + eps)
+ *   y = act(xh * weight[c] + bias[c] + residual),  var without Bessel's correction
+ * Statistics and arithmetic are float32, the result is rounded once to the storage type.  There is no handle: nothing is kept
+ * between calls, every call plans by integer arithmetic on its description.  Calls on different streams need workspaces of their own.
+ */
+typedef enum bs_activation {
+    BS_ACT_IDENTITY = 0,
+    BS_ACT_RELU = 1, /* z > 0 ? z : +0                                       */
+    BS_ACT_SILU = 2, /* z / (1 + exp(-z))                                    */
+    BS_ACT_GELU = 3  /* z * Phi(z), Phi the normal distribution function     */
+} bs_activation;
+
+/*
+ * One group normalisation.  shape is N, C, H, W; in memory the C channels of a pixel are contiguous and the pixels of all images follow
+ * each other, *_stride elements from one to the next: 0 = C (dense), more where the tensor is a channel slice of a larger one.
+ * Storage types: dtype for every tensor, param_dtype (BS_F32 or dtype) for weight, bias and their gradients.
+ */
+typedef struct bs_group_norm_desc {
+    int64_t shape[4];
+    int32_t groups;     /* divides C                    */
+    int32_t dtype;      /* bs_dtype                     */
+    int32_t param_dtype;
+    int32_t activation; /* bs_activation                */
+    double eps;         /* finite, >= 0                 */
+    int64_t x_stride, residual_stride, y_stride, grad_y_stride, grad_x_stride, grad_residual_stride;
+} bs_group_norm_desc;
+
+/* Device bytes bs_group_norm (backward == 0) or bs_group_norm_backward (!= 0) needs as workspace; 0 for an invalid description. */
+BS_API uint64_t bs_group_norm_workspace_bytes(const bs_group_norm_desc *desc, int32_t backward);
+
+/*
+ * Enqueue the forward pass on `stream`.  Never synchronises, never allocates.
+ *   x, residual   device (residual NULL: none), aligned to their element size, as are all tensors here; the kernels use 128-bit
+ *                 accesses where C, strides and addresses are multiples of 16 bytes, smaller ones elsewhere
+ *   weight, bias  device, C elements each; NULL: ones, zeros
+ *   y             device, written; shares no byte with an input or the workspace
+ *   stats         device, N * groups pairs of floats (mean, 1 / sqrt(var + eps)), which the backward pass needs; NULL: not wanted
+ *   workspace     device, 16-byte aligned, >= bs_group_norm_workspace_bytes(desc, 0)
+ * Errors: BS_ERR_NULL, BS_ERR_SHAPE (dimension < 1, stride below C), BS_ERR_PARAM (groups, eps), BS_ERR_UNSUPPORTED (type, activation;
+ *         an image of 2^31 elements, 2^24 groups of all images), BS_ERR_ALIGN, BS_ERR_WORKSPACE, BS_ERR_ALIAS, BS_ERR_HIP.
+ */
+BS_API bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const void *residual, const void *weight, const void *bias,
+                               void *y, float *stats, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Enqueue the backward pass: from the forward pass's operands, its stats and the gradient with respect to y the gradients with respect to
+ * x, residual, weight and bias (each may be NULL: not wanted).  ReLU passes the gradient where its input is > 0.  Sums are float32, in an
+ * order that does not depend on timing: equal calls give equal bits.  No output shares a byte with an input, another output or the workspace.
+ * Errors: those of bs_group_norm.
+ */
+BS_API bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, const void *residual, const void *weight, const void *bias,
+                                        const float *stats, const void *grad_y, void *grad_x, void *grad_residual, void *grad_weight,
+                                        void *grad_bias, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Log probabilities: the end of a classifier (Section 5 evaluates classifiers), from rows of logits x to
+ *   logp      log of the given class's probability: x[target] - lse,  lse = log sum exp x
+ *   entropy   -sum p log p of the row's distribution
+ *   top_*     the `top` most probable classes, most probable first, equal logits in order of their index: log probability and index
+ * in one pass over the logits, and the gradient of logp and entropy.  Sums are float32.
+ * A class at -infinity (masked) has probability 0 and adds nothing to the entropy.  In a row where every class is masked, logp and top_logp
+ * are -infinity, the entropy is 0 and the gradient 0.  NaN or +infinity among the logits makes the row's results NaN; NaN ranks first.
+ * A target equal to ignore_index has logp 0 and no gradient; any other target outside 0 .. classes - 1 has logp and gradient NaN
+ * (nothing is read through it).
+ */
+#define BS_MAX_TOP 32
+
+typedef struct bs_log_probs_desc {
+    int64_t rows, classes;               /* rows may be 0: nothing is enqueued                */
+    int64_t row_stride, grad_row_stride; /* elements from a row to the next; 0 = classes      */
+    int64_t ignore_index;
+    int32_t dtype;                       /* bs_dtype of logits and their gradient             */
+    int32_t target_bytes;                /* 4 (int32) or 8 (int64)                            */
+    int32_t top;                         /* 0 .. min(classes, BS_MAX_TOP)                     */
+    int32_t reserved;
+} bs_log_probs_desc;
+
+/* Device bytes bs_log_probs needs as workspace (0: none). */
+BS_API uint64_t bs_log_probs_workspace_bytes(const bs_log_probs_desc *desc);
+
+/*
+ * Enqueue the forward pass on `stream`.  Never synchronises, never allocates.
+ *   logits                device, aligned to the element size (rows may begin at any element)
+ *   targets               device, one per row; NULL: no given classes (logp must be NULL)
+ *   logp, entropy, lse    device, a float per row each, any may be NULL; lse and entropy are what the backward pass needs
+ *   top_logp, top_index   device, rows x top; not used with top == 0
+ *   workspace             device, 16-byte aligned, >= bs_log_probs_workspace_bytes(desc)
+ * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, classes < 1, stride below classes), BS_ERR_PARAM (top, target_bytes), BS_ERR_UNSUPPORTED
+ *         (type; over 2^30 classes, 2^23 rows), BS_ERR_ALIGN, BS_ERR_WORKSPACE, BS_ERR_ALIAS, BS_ERR_HIP.
+ */
+BS_API bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const void *targets, float *logp, float *entropy, float *lse,
+                              float *top_logp, int32_t *top_index, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Enqueue the backward pass: grad_logits from the forward pass's logits, targets, lse and entropy and the gradients of logp and entropy
+ * (a float per row; either may be NULL: zero).  grad_logits may be the logits themselves (same address and stride); otherwise it shares no
+ * byte with an input.  Errors: those of bs_log_probs.
+ */
+BS_API bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logits, const void *targets, const float *lse,
+                                       const float *entropy, const float *grad_logp, const float *grad_entropy, void *grad_logits, void *stream);
+
+/*
  * Compile, without loading them and without touching any device, all run-time builds the
  * current plan (device or host-only) asks for, for GPU architecture `arch` ("gfx950"; NULL =
  * "gfx950").  A way to check on a machine without a GPU that a stack's kernels build.

@@ -28,6 +28,8 @@ BS_VARIANT_STRIPS = 11
 VARIANT_NAMES = {1: "stream", 2: "pool_direct", 3: "lds_tile", 4: "pool_rows", 5: "plane_pool", 6: "nhwc_stream",
                  7: "nhwc_pool", 8: "nhwc_tile", 9: "rows_chain", 10: "nhwc_rows", 11: "strips"}
 BS_LAYOUT_NCHW, BS_LAYOUT_NHWC = 0, 1
+BS_ACT_IDENTITY, BS_ACT_RELU, BS_ACT_SILU, BS_ACT_GELU = 0, 1, 2, 3
+BS_MAX_TOP = 32
 STATUS_NAMES = {
     0: "BS_OK", 1: "BS_ERR_NULL", 2: "BS_ERR_SHAPE", 3: "BS_ERR_PARAM", 4: "BS_ERR_UNSUPPORTED",
     5: "BS_ERR_NOT_PLANNED", 6: "BS_ERR_NO_FIT", 7: "BS_ERR_ALIGN", 8: "BS_ERR_WORKSPACE",
@@ -82,6 +84,19 @@ class bs_sequence_info(C.Structure):
                 ("run_time_build", C.c_int32), ("reserved", C.c_int32)]
 
 
+class bs_group_norm_desc(C.Structure):
+    _fields_ = [("shape", C.c_int64 * 4), ("groups", C.c_int32), ("dtype", C.c_int32), ("param_dtype", C.c_int32),
+                ("activation", C.c_int32), ("eps", C.c_double),
+                ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("grad_y_stride", C.c_int64), ("grad_x_stride", C.c_int64), ("grad_residual_stride", C.c_int64)]
+
+
+class bs_log_probs_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("classes", C.c_int64), ("row_stride", C.c_int64), ("grad_row_stride", C.c_int64),
+                ("ignore_index", C.c_int64), ("dtype", C.c_int32), ("target_bytes", C.c_int32), ("top", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -118,6 +133,12 @@ _SIGNATURES = {
     "bs_stack_backward_strided": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                             C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(C.c_void_p), C.c_void_p,
                                             C.c_uint64, C.c_void_p]),
+    "bs_group_norm_workspace_bytes": (C.c_uint64, [C.POINTER(bs_group_norm_desc), C.c_int32]),
+    "bs_group_norm": (C.c_int, [C.POINTER(bs_group_norm_desc)] + [C.c_void_p] * 7 + [C.c_uint64, C.c_void_p]),
+    "bs_group_norm_backward": (C.c_int, [C.POINTER(bs_group_norm_desc)] + [C.c_void_p] * 11 + [C.c_uint64, C.c_void_p]),
+    "bs_log_probs_workspace_bytes": (C.c_uint64, [C.POINTER(bs_log_probs_desc)]),
+    "bs_log_probs": (C.c_int, [C.POINTER(bs_log_probs_desc)] + [C.c_void_p] * 8 + [C.c_uint64, C.c_void_p]),
+    "bs_log_probs_backward": (C.c_int, [C.POINTER(bs_log_probs_desc)] + [C.c_void_p] * 8),
     "bs_probe_issue_rate": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
     "bs_probe_stream": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]),
     "bs_stack_jit_check": (C.c_int, [C.c_void_p, C.c_char_p, C.POINTER(C.c_int32)]),
@@ -375,6 +396,37 @@ def bs_probe_stream(reads_per_write: int, read_only: bool, in_ptr: int, in_bytes
 def bs_probe_issue_rate(kind: int, waves_per_simd: int, iterations: int, sink_ptr: int, sink_floats: int, stream) -> None:
     _check(load().bs_probe_issue_rate(int(kind), int(waves_per_simd), int(iterations), C.c_void_p(sink_ptr or None),
                                       int(sink_floats), C.c_void_p(stream or None)), "bs_probe_issue_rate")
+
+
+def bs_group_norm_workspace_bytes(desc: bs_group_norm_desc, backward: bool) -> int:
+    return int(load().bs_group_norm_workspace_bytes(C.byref(desc), int(bool(backward))))
+
+
+def bs_group_norm(desc: bs_group_norm_desc, x, residual, weight, bias, y, stats, workspace, workspace_bytes, stream) -> None:
+    """Pointers are integer device addresses (0 / None = NULL), here and below."""
+    _check(load().bs_group_norm(C.byref(desc), x or None, residual or None, weight or None, bias or None, y or None, stats or None,
+                                workspace or None, int(workspace_bytes), stream or None), "bs_group_norm")
+
+
+def bs_group_norm_backward(desc: bs_group_norm_desc, x, residual, weight, bias, stats, grad_y, grad_x, grad_residual, grad_weight, grad_bias,
+                           workspace, workspace_bytes, stream) -> None:
+    _check(load().bs_group_norm_backward(C.byref(desc), x or None, residual or None, weight or None, bias or None, stats or None,
+                                         grad_y or None, grad_x or None, grad_residual or None, grad_weight or None, grad_bias or None,
+                                         workspace or None, int(workspace_bytes), stream or None), "bs_group_norm_backward")
+
+
+def bs_log_probs_workspace_bytes(desc: bs_log_probs_desc) -> int:
+    return int(load().bs_log_probs_workspace_bytes(C.byref(desc)))
+
+
+def bs_log_probs(desc: bs_log_probs_desc, logits, targets, logp, entropy, lse, top_logp, top_index, workspace, workspace_bytes, stream) -> None:
+    _check(load().bs_log_probs(C.byref(desc), logits or None, targets or None, logp or None, entropy or None, lse or None, top_logp or None,
+                               top_index or None, workspace or None, int(workspace_bytes), stream or None), "bs_log_probs")
+
+
+def bs_log_probs_backward(desc: bs_log_probs_desc, logits, targets, lse, entropy, grad_logp, grad_entropy, grad_logits, stream) -> None:
+    _check(load().bs_log_probs_backward(C.byref(desc), logits or None, targets or None, lse or None, entropy or None, grad_logp or None,
+                                        grad_entropy or None, grad_logits or None, stream or None), "bs_log_probs_backward")
 
 
 def bs_stack_plan_backward(handle) -> None:

@@ -1,0 +1,198 @@
+// Group normalisation: argument checks, the split of the work, the launches.  Nothing here synchronises or allocates.
+#include "bs_norm.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "bs_internal.h"
+
+using namespace bs;
+
+namespace {
+
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+uint64_t aligned(uint64_t bytes) { return ceil_div(bytes, 256) * 256; }
+
+bs_status check_desc(const bs_group_norm_desc *d)
+{
+    if (!d) return BS_ERR_NULL;
+    for (int i = 0; i < 4; ++i)
+        if (d->shape[i] < 1) return BS_ERR_SHAPE;
+    if (d->dtype != BS_F32 && d->dtype != BS_BF16 && d->dtype != BS_F16) return BS_ERR_UNSUPPORTED;
+    if (d->param_dtype != BS_F32 && d->param_dtype != d->dtype) return BS_ERR_UNSUPPORTED;
+    if (d->activation < BS_ACT_IDENTITY || d->activation > BS_ACT_GELU) return BS_ERR_UNSUPPORTED;
+    if (!std::isfinite(d->eps) || d->eps < 0) return BS_ERR_PARAM;
+    const int64_t C = d->shape[1], limit = (1ll << 31) - 1;
+    if (d->groups < 1 || C % d->groups != 0) return BS_ERR_PARAM;
+    if (d->shape[2] > limit || d->shape[3] > limit || d->shape[0] > limit || C > limit) return BS_ERR_UNSUPPORTED;
+    if ((double)d->shape[1] * (double)d->shape[2] * (double)d->shape[3] > (double)limit) return BS_ERR_UNSUPPORTED;
+    // grids are counted in 32 bits: images, groups
+    if (d->shape[0] * (int64_t)d->groups > (1ll << 24) || d->shape[0] * C > limit) return BS_ERR_UNSUPPORTED;
+    for (const int64_t s : {d->x_stride, d->residual_stride, d->y_stride, d->grad_y_stride, d->grad_x_stride, d->grad_residual_stride})
+        if (s != 0 && (s < C || s > limit)) return BS_ERR_SHAPE;
+    return BS_OK;
+}
+
+struct Space {
+    uint64_t part = 0, sums = 0, bytes = 0;  // offsets, size
+};
+
+// Pixel chunks and channel blocks.  Work-groups of at least 16 KiB of one tensor, 2048 of them where the tensor has so much.
+void split(const bs_group_norm_desc &d, NormK &k)
+{
+    k.N = (uint32_t)d.shape[0];
+    k.C = (uint32_t)d.shape[1];
+    k.P = (uint32_t)(d.shape[2] * d.shape[3]);
+    k.G = (uint32_t)d.groups;
+    k.per = k.C / k.G;
+    k.blocks = (uint32_t)ceil_div(k.C, K_NORM_BLOCK_CHANNELS);
+    k.spans = (k.per + K_NORM_BLOCK_CHANNELS - 2) / K_NORM_BLOCK_CHANNELS + 1;
+    const uint64_t row = std::min<uint64_t>(k.C, K_NORM_BLOCK_CHANNELS) * dtype_size(d.dtype);
+    const uint64_t wanted = ceil_div(2048, (uint64_t)k.N * k.blocks), most = std::min<uint64_t>(256, ceil_div(k.P * row, 16384));
+    const uint64_t chunks = std::max<uint64_t>(1, std::min(wanted, most));
+    k.chunk = (uint32_t)ceil_div(k.P, chunks);
+    k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
+}
+
+Space space(const NormK &k, bool backward)
+{
+    Space s;
+    const uint64_t pairs = (uint64_t)k.N * k.G * 2 * sizeof(float);
+    s.sums = 0;  // forward: the statistics, where the caller does not want them
+    s.part = aligned(pairs);
+    s.bytes = s.part + aligned(backward ? (uint64_t)k.N * k.chunks * k.C * 2 * sizeof(float) : pairs * k.chunks * k.spans);
+    return s;
+}
+
+NormTensor tensor(const void *p, int64_t stride, const NormK &k) { return NormTensor{p, (uint64_t)(stride ? stride : k.C)}; }
+
+// Elements of a lane's vector: 128 bits, or less where the channels, a stride or an address are no multiple of that.
+int vector_of(const NormK &k, int32_t dtype, std::initializer_list<const NormTensor *> tensors)
+{
+    const uint64_t es = dtype_size(dtype);
+    uint64_t vec = 16 / es;
+    for (; vec > 1; vec /= 2) {
+        bool fits = k.C % vec == 0;
+        for (const NormTensor *t : tensors)
+            fits = fits && (!t->p || (t->stride % vec == 0 && reinterpret_cast<uintptr_t>(t->p) % (vec * es) == 0));
+        if (fits) break;
+    }
+    return (int)vec;
+}
+
+TensorBytes bytes_of(const NormK &k, const NormTensor &t, uint64_t es) { return TensorBytes{t.p, (uint64_t)k.N * k.P, k.C * es, t.stride * es}; }
+TensorBytes bytes_of(const void *p, uint64_t n) { return TensorBytes{p, 1, n, n}; }
+
+bool element_aligned(const void *p, uint64_t es) { return reinterpret_cast<uintptr_t>(p) % es == 0; }
+
+// No output shares a byte with an input, another output or the workspace.
+template <size_t NI, size_t NO>
+bs_status check_overlap(const TensorBytes (&in)[NI], const TensorBytes (&out)[NO])
+{
+    for (size_t i = 0; i < NO; ++i) {
+        if (!out[i].p) continue;
+        for (const TensorBytes &t : in)
+            if (t.p && tensors_overlap(out[i], t)) return BS_ERR_ALIAS;
+        for (size_t j = 0; j < i; ++j)
+            if (out[j].p && tensors_overlap(out[i], out[j])) return BS_ERR_ALIAS;
+    }
+    return BS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t bs_group_norm_workspace_bytes(const bs_group_norm_desc *desc, int32_t backward)
+{
+    if (check_desc(desc) != BS_OK) return 0;
+    NormK k{};
+    split(*desc, k);
+    return space(k, backward != 0).bytes;
+}
+
+bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const void *residual, const void *weight, const void *bias, void *y,
+                        float *stats, void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    const bs_status checked = check_desc(desc);
+    if (checked != BS_OK) return checked;
+    if (!x || !y) return BS_ERR_NULL;
+    NormK k{};
+    split(*desc, k);
+    k.x = tensor(x, desc->x_stride, k);
+    k.r = tensor(residual, desc->residual_stride, k);
+    k.y = tensor(y, desc->y_stride, k);
+    const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), pairs = (uint64_t)k.N * k.G * 8;
+    const Space s = space(k, false);
+    if (!workspace || workspace_bytes < s.bytes) return BS_ERR_WORKSPACE;
+    for (const void *p : {x, residual, (const void *)y})
+        if (!element_aligned(p, es)) return BS_ERR_ALIGN;
+    if (!element_aligned(weight, ps) || !element_aligned(bias, ps) || !element_aligned(stats, 8) || !element_aligned(workspace, 16)) return BS_ERR_ALIGN;
+    const bs_status alias = check_overlap({bytes_of(k, k.x, es), bytes_of(k, k.r, es), bytes_of(weight, k.C * ps), bytes_of(bias, k.C * ps)},
+                                          {bytes_of(k, k.y, es), bytes_of(stats, pairs), bytes_of(workspace, s.bytes)});
+    if (alias != BS_OK) return alias;
+    k.weight = weight;
+    k.bias = bias;
+    k.activation = (uint32_t)desc->activation;
+    k.f32_params = desc->param_dtype == BS_F32;
+    k.eps = (float)desc->eps;
+    char *const ws = static_cast<char *>(workspace);
+    k.stats = stats ? stats : reinterpret_cast<float *>(ws + s.sums);
+    k.part = reinterpret_cast<float *>(ws + s.part);
+    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.y});
+    for (const NormPass pass : {NORM_STATS, NORM_JOIN, NORM_APPLY}) {
+        const bs_status st = launch_norm(pass, k, desc->dtype, vec, stream);
+        if (st != BS_OK) return st;
+    }
+    return BS_OK;
+}
+
+bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, const void *residual, const void *weight, const void *bias,
+                                 const float *stats, const void *grad_y, void *grad_x, void *grad_residual, void *grad_weight, void *grad_bias,
+                                 void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    const bs_status checked = check_desc(desc);
+    if (checked != BS_OK) return checked;
+    if (!x || !stats || !grad_y) return BS_ERR_NULL;
+    NormK k{};
+    split(*desc, k);
+    k.x = tensor(x, desc->x_stride, k);
+    k.r = tensor(residual, desc->residual_stride, k);
+    k.dy = tensor(grad_y, desc->grad_y_stride, k);
+    k.dx = tensor(grad_x, desc->grad_x_stride, k);
+    k.dr = tensor(grad_residual, desc->grad_residual_stride, k);
+    const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), pairs = (uint64_t)k.N * k.G * 8;
+    const Space s = space(k, true);
+    if (!workspace || workspace_bytes < s.bytes) return BS_ERR_WORKSPACE;
+    for (const void *p : {x, residual, grad_y, (const void *)grad_x, (const void *)grad_residual})
+        if (!element_aligned(p, es)) return BS_ERR_ALIGN;
+    for (const void *p : {weight, bias, (const void *)grad_weight, (const void *)grad_bias})
+        if (!element_aligned(p, ps)) return BS_ERR_ALIGN;
+    if (!element_aligned(stats, 8) || !element_aligned(workspace, 16)) return BS_ERR_ALIGN;
+    const bs_status alias = check_overlap({bytes_of(k, k.x, es), bytes_of(k, k.r, es), bytes_of(weight, k.C * ps), bytes_of(bias, k.C * ps),
+                                           bytes_of(stats, pairs), bytes_of(k, k.dy, es)},
+                                          {bytes_of(k, k.dx, es), bytes_of(k, k.dr, es), bytes_of(grad_weight, k.C * ps), bytes_of(grad_bias, k.C * ps),
+                                           bytes_of(workspace, s.bytes)});
+    if (alias != BS_OK) return alias;
+    k.weight = weight;
+    k.bias = bias;
+    k.dweight = grad_weight;
+    k.dbias = grad_bias;
+    k.activation = (uint32_t)desc->activation;
+    k.f32_params = desc->param_dtype == BS_F32;
+    k.eps = (float)desc->eps;
+    char *const ws = static_cast<char *>(workspace);
+    k.stats = const_cast<float *>(stats);
+    k.sums = reinterpret_cast<float *>(ws + s.sums);
+    k.part = reinterpret_cast<float *>(ws + s.part);
+    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.dy, &k.dx, &k.dr});
+    const bool tensors = grad_x || grad_residual, params = grad_weight || grad_bias;
+    for (const NormPass pass : {NORM_GRAD_SUMS, NORM_GRAD_JOIN, NORM_GRAD_PARAMS, NORM_GRAD_APPLY}) {
+        if (pass == NORM_GRAD_PARAMS ? !params : pass == NORM_GRAD_SUMS ? !params && !grad_x : pass == NORM_GRAD_JOIN ? !grad_x : !tensors) continue;
+        const bs_status st = launch_norm(pass, k, desc->dtype, vec, stream);
+        if (st != BS_OK) return st;
+    }
+    return BS_OK;
+}
+
+}  // extern "C"
