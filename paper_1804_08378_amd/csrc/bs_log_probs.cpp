@@ -1,6 +1,8 @@
 // Log probabilities: argument checks and launches.  Nothing here synchronises or allocates.
 #include "bs_log_probs.h"
 
+#include <algorithm>
+
 #include "bs_internal.h"
 
 using namespace bs;
@@ -31,6 +33,34 @@ void fill(const bs_log_probs_desc &d, LogProbsK &k)
     k.wide_targets = d.target_bytes == 8;
 }
 
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// Work-groups of a row: one where the rows alone fill the device; else parts of at least `least` classes, `wanted` work-groups in all.
+void split(LogProbsK &k, uint64_t least, uint64_t wanted)
+{
+    const uint64_t parts = std::max<uint64_t>(1, std::min({ceil_div(wanted, k.rows), ceil_div(k.classes, least), (uint64_t)K_LOG_PROBS_MOST_PARTS}));
+    k.part = (uint32_t)(ceil_div(ceil_div(k.classes, parts), 8) * 8);
+    k.parts = (uint32_t)ceil_div(k.classes, k.part);
+}
+
+struct Space {
+    uint64_t keys = 0, sums = 0, bytes = 0;  // offsets, size
+};
+Space space(const LogProbsK &k)
+{
+    Space s;
+    if (k.parts == 1) return s;
+    s.sums = ceil_div(k.rows * k.parts * k.top * 8, 256) * 256;
+    s.bytes = s.sums + k.rows * k.parts * 16;
+    return s;
+}
+
+void fill_forward(const bs_log_probs_desc &d, LogProbsK &k)
+{
+    fill(d, k);
+    split(k, 2048, 512);
+}
+
 bool aligned(const void *p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 TensorBytes rows_of(const void *p, const LogProbsK &k, uint64_t stride, uint64_t es) { return TensorBytes{p, k.rows, k.classes * es, stride * es}; }
@@ -55,7 +85,10 @@ extern "C" {
 
 uint64_t bs_log_probs_workspace_bytes(const bs_log_probs_desc *desc)
 {
-    return 0;
+    if (check_desc(desc) != BS_OK || desc->rows == 0) return 0;
+    LogProbsK k{};
+    fill_forward(*desc, k);
+    return space(k).bytes;
 }
 
 bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const void *targets, float *logp, float *entropy, float *lse,
@@ -66,15 +99,18 @@ bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const 
     if (desc->rows == 0) return BS_OK;
     if (!logits || (logp && !targets) || (desc->top && (!top_logp || !top_index))) return BS_ERR_NULL;
     LogProbsK k{};
-    fill(*desc, k);
+    fill_forward(*desc, k);
+    const Space room = space(k);
     const uint64_t es = dtype_size(desc->dtype);
-    if (!aligned(logits, es) || !aligned(targets, (uint64_t)desc->target_bytes)) return BS_ERR_ALIGN;
+    if (room.bytes && (!workspace || workspace_bytes < room.bytes)) return BS_ERR_WORKSPACE;
+    if (!aligned(logits, es) || !aligned(targets, (uint64_t)desc->target_bytes) || !aligned(workspace, 16)) return BS_ERR_ALIGN;
     for (const void *p : {(const void *)logp, (const void *)entropy, (const void *)lse, (const void *)top_logp, (const void *)top_index})
         if (!aligned(p, 4)) return BS_ERR_ALIGN;
     if (!desc->top) top_logp = nullptr, top_index = nullptr;
     const uint64_t n = k.rows * 4;
     const bs_status alias = check_overlap({rows_of(logits, k, k.stride, es), bytes_of(targets, k.rows * (uint64_t)desc->target_bytes)},
-                                          {bytes_of(logp, n), bytes_of(entropy, n), bytes_of(lse, n), bytes_of(top_logp, n * k.top), bytes_of(top_index, n * k.top)});
+                                          {bytes_of(logp, n), bytes_of(entropy, n), bytes_of(lse, n), bytes_of(top_logp, n * k.top), bytes_of(top_index, n * k.top),
+                                           bytes_of(workspace, room.bytes)});
     if (alias != BS_OK) return alias;
     k.logits = logits;
     k.targets = targets;
@@ -83,7 +119,10 @@ bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const 
     k.lse = lse;
     k.top_logp = top_logp;
     k.top_index = top_index;
-    return launch_log_probs(k, desc->dtype, stream);
+    k.part_keys = reinterpret_cast<uint64_t *>(workspace);
+    k.part_sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + room.sums);
+    // a row that a wave reads in four vectors a lane needs no more of them
+    return launch_log_probs(k, desc->dtype, k.classes * es <= 64 * 16 * 4 ? 64 : 256, stream);
 }
 
 bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logits, const void *targets, const float *lse, const float *entropy,
@@ -113,7 +152,11 @@ bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logit
     k.grad_logp = grad_logp;
     k.grad_entropy = grad_entropy;
     k.grad_logits = grad_logits;
-    return launch_log_probs_backward(k, desc->dtype, stream);
+    split(k, 8192, 2048);
+    // 128-bit accesses on both sides need rows that stand alike in them
+    const bool vectors = (reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad_logits)) % 16 == 0 &&
+                         (k.rows == 1 || (k.stride - k.grad_stride) * es % 16 == 0);
+    return launch_log_probs_backward(k, desc->dtype, vectors, stream);
 }
 
 }  // extern "C"

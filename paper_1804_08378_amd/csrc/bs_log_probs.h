@@ -17,9 +17,15 @@ struct LogProbsK {
     uint64_t rows, stride, grad_stride;  // strides: elements from a row to the next
     int64_t ignore_index;
     uint32_t classes, top, wide_targets;
+    uint32_t parts, part;  // work-groups of a row, classes of one (a multiple of 8)
+    uint64_t *part_keys;   // workspace, rows x parts x top: the parts' best classes as numbers (rank_key)
+    float *part_sums;      // workspace, rows x parts x 4: reference, sum, weighted sum, unused
 };
 
-bs_status launch_log_probs(const LogProbsK &k, int32_t dtype, void *stream);
-bs_status launch_log_probs_backward(const LogProbsK &k, int32_t dtype, void *stream);
+constexpr uint32_t K_LOG_PROBS_MOST_PARTS = 256;
+
+// threads: of a work-group, 64 or 256.  join: behind the parts' launch, one work-group a row.
+bs_status launch_log_probs(const LogProbsK &k, int32_t dtype, int threads, void *stream);
+bs_status launch_log_probs_backward(const LogProbsK &k, int32_t dtype, bool vectors, void *stream);
 
 }  // namespace bs

@@ -3,7 +3,11 @@
 //   m = max x,  s = sum exp(x - m),  t = sum exp(x - m) (x - m);   lse = m + log s,  logp = x[target] - lse,  entropy = log s - t / s
 //   dx_j = g (delta_j,target - p_j) - h p_j (log p_j + entropy),   p = exp(x - lse), g and h the gradients of logp and of entropy
 //
-// Maximum and sums are kept running in float32 over one pass; a class at -infinity has probability 0 and adds nothing.
+// A lane keeps s and t running in float32 against a reference that need not be the maximum: one of the values seen, at most 1 below their
+// maximum, so that it moves a few times in a row however long.  A class at -infinity has probability 0 and adds nothing.
+//
+// The top classes cost one comparison a vector: a lane remembers its best value and the vector that has it.  The k-th best of these bests
+// bounds the k-th best class from below, and only the few lanes whose best passes the bound read their vectors again.
 #include <hip/hip_runtime.h>
 
 #include "bs_device.h"
@@ -13,43 +17,24 @@
 namespace bs {
 namespace {
 
-constexpr int T = 256;
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr float FAR = -200.0f;      // exp is 0 from here on: stands for larger distances where they are multiplied by it
+constexpr uint32_t LIST = 512;      // candidates for the top classes that a work-group keeps
 
 // exp for float32 results: the product with log2(e) in two parts, so that large arguments keep their last bits.
 BS_DEV float exp_exact(float v)
 {
-    const float hi = v * 1.44269504088896341f;
-    const float lo = __builtin_fmaf(v, 1.44269504088896341f, -hi) + v * 1.92596299112661746e-8f;
+    const float hi = v * LOG2E;
+    const float lo = __builtin_fmaf(v, LOG2E, -hi) + v * 1.92596299112661746e-8f;
     const float e = __builtin_amdgcn_exp2f(hi);
     return __builtin_fabsf(hi) < 160.0f ? __builtin_fmaf(e, lo * 0.693147180559945309f, e) : e;  // (beyond: 0, infinity or NaN)
 }
 
-// Running maximum, sum of exp(x - m) and sum of exp(x - m) (x - m).
-struct Running {
-    float m = -INFINITY, s = 0.0f, t = 0.0f;
-
-    BS_DEV void join(float mo, float so, float to)
-    {
-        const float mn = __builtin_fmaxf(m, mo);
-        const float base = mn == -INFINITY ? 0.0f : mn;
-        const float da = m - base, db = mo - base;  // (-infinity where that side is empty: its sums are 0, or NaN)
-        const float fa = exp_exact(da), fb = exp_exact(db);
-        t = fa * __builtin_fmaf(s, __builtin_fmaxf(da, -1e30f), t) + fb * __builtin_fmaf(so, __builtin_fmaxf(db, -1e30f), to);
-        s = __builtin_fmaf(s, fa, so * fb);
-        m = mn;
-    }
-    BS_DEV void add(float x)
-    {
-        const float one = x == -INFINITY ? 0.0f : 1.0f;
-        join(x, x != x ? x : one, 0.0f);
-    }
-};
-
 template <int DT>
-BS_DEV float element(const void *p, uint64_t i)
+BS_DEV float element(const char *p, uint64_t i)
 {
-    if constexpr (DT == DT_F32) return static_cast<const float *>(p)[i];
-    else return half_up<DT>(static_cast<const uint16_t *>(p)[i]);
+    if constexpr (DT == DT_F32) return reinterpret_cast<const float *>(p)[i];
+    else return half_up<DT>(reinterpret_cast<const uint16_t *>(p)[i]);
 }
 
 // A class as one number: larger values first, then lower indices; NaN above all, -0 equal to 0.  Never 0 for a class.
@@ -59,51 +44,181 @@ BS_DEV uint64_t rank_key(float x, uint32_t j)
     const uint32_t o = x != x ? 0xffffffffu : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
     return (uint64_t)o << 32 | (0xffffffffu - j);
 }
+BS_DEV uint32_t key_index(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
+BS_DEV float key_value(uint64_t key)
+{
+    const uint32_t o = (uint32_t)(key >> 32);
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
 
 BS_DEV int64_t target_of(const LogProbsK &k, uint64_t row)
 {
     return k.wide_targets ? static_cast<const int64_t *>(k.targets)[row] : static_cast<const int32_t *>(k.targets)[row];
 }
 
-template <int DT>
-__global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
-{
-    __shared__ float part[3][T / 64];
-    __shared__ uint64_t best[T / 64];
-    const uint64_t row = blockIdx.x;
-    const char *x = static_cast<const char *>(k.logits) + row * k.stride * (DT != DT_F32 ? 2 : 4);
-    Running r;
-    for (uint32_t j = threadIdx.x; j < k.classes; j += T) r.add(element<DT>(x, j));
+// ------------------------------------------------------------------------------------------------ sums
+struct Sums {
+    float base = 0.0f;         // reference: a value seen (0: none but -infinity and NaN so far)
+    float above = -INFINITY;   // the reference moves for values above this; -infinity: there is none yet
+    float s = 0.0f, t = 0.0f;  // sum of exp(x - base), of exp(x - base) (x - base)
+
+    BS_DEV void move(float to)
+    {
+        const bool first = above == -INFINITY;
+        const float d = first ? 0.0f : __builtin_fmaxf(base - to, FAR), f = first ? 0.0f : __builtin_amdgcn_exp2f(d * LOG2E);
+        t = f * __builtin_fmaf(s, d, t);
+        s *= f;
+        base = to;
+        above = to + 1.0f;
+    }
+    template <int N>
+    BS_DEV void add(const float (&v)[N], float most)
+    {
+        if (most > above) move(most);
+        float e[N], w[N];
 #pragma unroll
-    for (int o = 32; o; o >>= 1) r.join(__shfl_xor(r.m, o), __shfl_xor(r.s, o), __shfl_xor(r.t, o));
-    const uint32_t wave = threadIdx.x / 64;
-    if (threadIdx.x % 64 == 0) {
-        part[0][wave] = r.m;
-        part[1][wave] = r.s;
-        part[2][wave] = r.t;
+        for (int i = 0; i < N; ++i) {
+            const float d = v[i] - base;
+            e[i] = __builtin_amdgcn_exp2f(d * LOG2E);
+            w[i] = e[i] * max2(d, FAR);
+        }
+#pragma unroll
+        for (int n = N / 2; n; n /= 2)
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                e[i] += e[i + n];
+                w[i] += w[i + n];
+            }
+        s += e[0];
+        t += w[0];
+    }
+};
+
+template <int T>
+BS_DEV float over_lanes_max(float v)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = __builtin_fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// The work-group's sums from its lanes', in every lane.  lds: 3 * T / 64 floats.
+template <int T>
+BS_DEV Sums join_lanes(const Sums &mine, float *lds)
+{
+    const float own = mine.above == -INFINITY ? -INFINITY : mine.base;
+    const float wave_base = over_lanes_max<T>(own);
+    Sums r = mine;
+    r.move(wave_base == -INFINITY ? 0.0f : wave_base);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        r.s += __shfl_xor(r.s, o);
+        r.t += __shfl_xor(r.t, o);
+    }
+    if (wave_base == -INFINITY) r.above = -INFINITY;
+    if constexpr (T > 64) {
+        const uint32_t wave = threadIdx.x / 64;
+        if (threadIdx.x % 64 == 0) {
+            lds[3 * wave] = wave_base;
+            lds[3 * wave + 1] = r.s;
+            lds[3 * wave + 2] = r.t;
+        }
+        __syncthreads();
+        float base = lds[0];
+#pragma unroll
+        for (int w = 1; w < T / 64; ++w) base = __builtin_fmaxf(base, lds[3 * w]);
+        r = Sums();
+#pragma unroll
+        for (int w = 0; w < T / 64; ++w) {
+            Sums part;
+            part.base = lds[3 * w];
+            part.above = lds[3 * w] == -INFINITY ? -INFINITY : part.base;
+            part.s = lds[3 * w + 1];
+            part.t = lds[3 * w + 2];
+            part.move(base == -INFINITY ? 0.0f : base);
+            r.s += part.s;
+            r.t += part.t;
+        }
+        if (base != -INFINITY) {
+            r.base = base;
+            r.above = base;
+        }
+        __syncthreads();
+    }
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------------ top classes
+struct Selection {
+    uint64_t lane[256];
+    uint64_t list[LIST];
+    uint64_t bound;
+    uint32_t count, lanes;
+    uint16_t chosen[256];
+};
+
+// A lower bound of the k-th best class's number: the k-th best of 64 numbers that have a class each, the best of 64 sets of lanes (0: fewer than
+// k sets have any).  `key`: the lane's best, 0 for none.  Valid in every lane.
+template <int T>
+BS_DEV uint64_t bound_of(uint64_t key, uint32_t k, Selection &sel)
+{
+    sel.lane[threadIdx.x] = key;
+    if (threadIdx.x == 0) {
+        sel.bound = 0;
+        sel.count = sel.lanes = 0;
     }
     __syncthreads();
-    r = Running();
-    for (uint32_t w = 0; w < T / 64; ++w) r.join(part[0][w], part[1][w], part[2][w]);
-    const bool none = r.s == 0.0f;  // every class masked
-    const float lse = none ? -INFINITY : r.m + logf(r.s);
-    if (threadIdx.x == 0) {
-        if (k.entropy) k.entropy[row] = none ? 0.0f : logf(r.s) - r.t / r.s;
-        if (k.lse) k.lse[row] = lse;
-        if (k.targets && k.logp) {
-            const int64_t c = target_of(k, row);
-            float v;
-            if (c == k.ignore_index) v = 0.0f;
-            else if (c < 0 || c >= (int64_t)k.classes) v = __builtin_nanf("");
-            else v = none ? -INFINITY : (element<DT>(x, (uint64_t)c) - r.m) - logf(r.s);
-            k.logp[row] = v;
+    if (threadIdx.x < 64) {
+        uint64_t best = key;
+#pragma unroll
+        for (int w = 1; w < T / 64; ++w) {
+            const uint64_t other = sel.lane[threadIdx.x + 64 * w];
+            best = other > best ? other : best;
         }
+        if constexpr (T > 64) sel.list[threadIdx.x] = best;  // (the wave's own: no other wave touches the list before the barrier)
+        const uint64_t *from = T > 64 ? sel.list : sel.lane;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        uint32_t rank = 0;
+#pragma unroll 16
+        for (int i = 0; i < 64; ++i) rank += from[i] > best;
+        if (rank == k - 1) sel.bound = best;
     }
+    __syncthreads();
+    return sel.bound;
+}
+
+BS_DEV void offer(uint64_t key, uint64_t bound, Selection &sel)
+{
+    if (key >= bound && key != 0) {
+        const uint32_t at = atomicAdd(&sel.count, 1u);
+        if (at < LIST) sel.list[at] = key;
+    }
+}
+
+// The k best of the offered numbers, best first: put(place, key); places beyond the number offered get 0.  The caller has synchronised.
+template <int T, typename PUT>
+BS_DEV void put_ranked(uint32_t k, const Selection &sel, PUT put)
+{
+    const uint32_t n = sel.count;
+    for (uint32_t i = threadIdx.x; i < n; i += T) {
+        const uint64_t key = sel.list[i];
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += sel.list[j] > key;
+        if (rank < k) put(rank, key);
+    }
+    for (uint32_t i = n + threadIdx.x; i < k; i += T) put(i, 0);
+}
+
+// The same from any numbers, one after the other: every round finds the best below the last.  For rows with NaN or infinity, and where too
+// many candidates pass the bound.
+template <int T, typename GET, typename PUT>
+BS_DEV void put_by_rounds(uint32_t k, uint32_t n, Selection &sel, GET get, PUT put)
+{
     uint64_t last = ~0ull;
-    for (uint32_t i = 0; i < k.top; ++i) {
+    for (uint32_t r = 0; r < k; ++r) {
         uint64_t mine = 0;
-        for (uint32_t j = threadIdx.x; j < k.classes; j += T) {
-            const uint64_t key = rank_key(element<DT>(x, j), j);
+        for (uint32_t j = threadIdx.x; j < n; j += T) {
+            const uint64_t key = get(j);
             if (key < last && key > mine) mine = key;
         }
 #pragma unroll
@@ -112,37 +227,238 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
             mine = other > mine ? other : mine;
         }
         __syncthreads();
-        if (threadIdx.x % 64 == 0) best[wave] = mine;
+        if (threadIdx.x % 64 == 0) sel.lane[threadIdx.x / 64] = mine;
         __syncthreads();
-        last = best[0];
-        for (uint32_t w = 1; w < T / 64; ++w) last = best[w] > last ? best[w] : last;
-        if (threadIdx.x == 0) {
-            const uint32_t j = 0xffffffffu - (uint32_t)last;
-            k.top_index[row * k.top + i] = (int32_t)j;
-            k.top_logp[row * k.top + i] = none ? -INFINITY : (element<DT>(x, j) - r.m) - logf(r.s);
-        }
+        last = sel.lane[0];
+#pragma unroll
+        for (int w = 1; w < T / 64; ++w) last = sel.lane[w] > last ? sel.lane[w] : last;
+        if (threadIdx.x == 0) put(r, last);
     }
 }
 
+// ------------------------------------------------------------------------------------------------ a row's results
 template <int DT>
-__global__ __launch_bounds__(T) void log_probs_backward_kernel(LogProbsK k)
+BS_DEV void put_row(const LogProbsK &k, uint64_t row, const char *x, const Sums &r)
 {
+    const bool none = r.s == 0.0f;  // every class masked
+    const float log_s = logf(r.s);
+    if (k.entropy) k.entropy[row] = none ? 0.0f : log_s - r.t / r.s;
+    if (k.lse) k.lse[row] = none ? -INFINITY : r.base + log_s;
+    if (k.logp) {
+        const int64_t c = target_of(k, row);
+        float v;
+        if (c == k.ignore_index) v = 0.0f;
+        else if (c < 0 || c >= (int64_t)k.classes) v = __builtin_nanf("");
+        else v = none ? -INFINITY : (element<DT>(x, (uint64_t)c) - r.base) - log_s;
+        k.logp[row] = v;
+    }
+}
+
+struct PutTop {
+    const LogProbsK &k;
+    uint64_t row;
+    float base, log_s;
+    bool none;
+    BS_DEV PutTop(const LogProbsK &k_, uint64_t row_, const Sums &r) : k(k_), row(row_), base(r.base), log_s(logf(r.s)), none(r.s == 0.0f) {}
+    BS_DEV void operator()(uint32_t place, uint64_t key) const
+    {
+        k.top_index[row * k.top + place] = (int32_t)key_index(key);
+        k.top_logp[row * k.top + place] = none ? -INFINITY : (key_value(key) - base) - log_s;
+    }
+};
+
+// One part of one row (or, with PARTS false, the whole row) by a work-group of T threads.  A part begins at any element: the elements in
+// front of its first and behind its last whole 128-bit vector are a lane's each.
+template <int DT, int T, bool TOP, bool PARTS>
+__global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
+{
+    constexpr int VEC = DT == DT_F32 ? 4 : 8, U = 4;
+    constexpr uint64_t ES = DT == DT_F32 ? 4 : 2;
+    __shared__ float lds[3 * T / 64];
+    quiet_maxima();
+    const uint64_t row = PARTS ? blockIdx.x / k.parts : blockIdx.x;
+    const uint32_t part = PARTS ? blockIdx.x - (uint32_t)row * k.parts : 0, first = part * k.part;
+    const uint32_t n = PARTS ? min(k.classes - first, k.part) : k.classes;
+    const char *whole = static_cast<const char *>(k.logits) + row * k.stride * ES;
+    const char *x = whole + first * ES;
+    const uint32_t head = min(n, (uint32_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (uint32_t)ES);
+    const uint32_t vectors = (n - head) / VEC, edges = n - vectors * VEC, tid = threadIdx.x;
+    const uint32_t edge = tid < head ? tid : n - (edges - tid);  // the lane's odd element, for tid < edges
+
+    Sums sums;
+    float best = -INFINITY;
+    uint32_t at = tid < head ? tid : tid < vectors ? head + tid * VEC : edge;  // where the lane's first class stands
+    const bool any = tid < vectors || tid < edges;
+    auto take = [&](const auto &v, float most, uint32_t where) {
+        sums.add(v, most);
+        if constexpr (TOP) {
+            const bool better = most > best;
+            best = better ? most : best;
+            at = better ? where : at;
+        }
+    };
+    float odd[1] = {0.0f};
+    if (tid < edges) odd[0] = element<DT>(x, edge);
+    if (tid < head) take(odd, odd[0], tid);
+    const char *src = x + head * ES + tid * 16ull;
+    uint32_t i = tid;
+    auto whole_vector = [&](const Raw<DT, VEC> &raw, uint32_t where) {
+        float v[VEC];
+        unpack<DT, VEC>(raw, v);
+        float most;
+        if constexpr (VEC == 4) most = max2(max3(v[0], v[1], v[2]), v[3]);
+        else most = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max2(v[6], v[7]));
+        take(v, most, where);
+    };
+    for (; i + (U - 1) * T < vectors; i += U * T, src += U * T * 16) {
+        Raw<DT, VEC> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load_raw<DT, VEC>(src + u * T * 16, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) whole_vector(raw[u], head + (i + u * T) * VEC);
+    }
+    for (; i < vectors; i += T, src += T * 16) whole_vector(load_raw<DT, VEC>(src, 0), head + i * VEC);
+    if (tid >= head && tid < edges) take(odd, odd[0], edge);
+
+    const Sums r = join_lanes<T>(sums, lds);
+    if constexpr (PARTS) {
+        if (tid == 0) {
+            float *out = k.part_sums + 4 * (uint64_t)blockIdx.x;
+            out[0] = r.above == -INFINITY ? -INFINITY : r.base;
+            out[1] = r.s;
+            out[2] = r.t;
+        }
+    } else if (tid == 0) {
+        put_row<DT>(k, row, whole, r);
+    }
+    if constexpr (TOP) {
+        __shared__ Selection sel;
+        const PutTop top(k, row, r);
+        auto put = [&](uint32_t place, uint64_t key) {
+            if constexpr (PARTS) k.part_keys[(uint64_t)blockIdx.x * k.top + place] = key;
+            else top(place, key);
+        };
+        if (r.s == r.s) {  // (the same in every lane)
+            const uint64_t key = any ? rank_key(best, first + at) : 0;
+            uint64_t bound = bound_of<T>(key, k.top, sel);
+            if (bound) bound -= VEC - 1;  // the class is any of its vector
+            if (key >= bound && tid < vectors) sel.chosen[atomicAdd(&sel.lanes, 1u)] = (uint16_t)tid;
+            if (tid < edges) offer(rank_key(odd[0], first + edge), bound, sel);
+            __syncthreads();
+            const uint32_t lanes = sel.lanes;
+            for (uint32_t c = tid / 64; c < lanes; c += T / 64) {
+                for (uint32_t j = sel.chosen[c] + (tid % 64) * T; j < vectors; j += 64 * T) {
+                    float v[VEC];
+                    unpack<DT, VEC>(load_raw<DT, VEC>(x + head * ES + j * 16ull, 0), v);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) offer(rank_key(v[e], first + head + j * VEC + e), bound, sel);
+                }
+            }
+            __syncthreads();
+            if (sel.count <= LIST) {
+                put_ranked<T>(k.top, sel, put);
+                return;
+            }
+        }
+        put_by_rounds<T>(k.top, n, sel, [&](uint32_t j) { return rank_key(element<DT>(x, j), first + j); }, put);
+    }
+}
+
+// Joins the parts of a row.
+template <int DT, bool TOP>
+__global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
+{
+    constexpr int T = 256;
+    __shared__ float lds[3 * T / 64];
     const uint64_t row = blockIdx.x;
+    Sums mine;
+    if (threadIdx.x < k.parts) {  // at most 256
+        const float *in = k.part_sums + 4 * (row * k.parts + threadIdx.x);
+        if (in[0] != -INFINITY) {
+            mine.base = in[0];
+            mine.above = in[0];
+        }
+        mine.s = in[1];
+        mine.t = in[2];
+    }
+    const Sums r = join_lanes<T>(mine, lds);
     const char *x = static_cast<const char *>(k.logits) + row * k.stride * (DT != DT_F32 ? 2 : 4);
-    char *dx = static_cast<char *>(k.grad_logits) + row * k.grad_stride * (DT != DT_F32 ? 2 : 4);
+    if (threadIdx.x == 0) put_row<DT>(k, row, x, r);
+    if constexpr (TOP) {
+        __shared__ Selection sel;
+        const PutTop put(k, row, r);
+        const uint64_t *keys = k.part_keys + row * k.parts * k.top;
+        const uint32_t n = k.parts * k.top;
+        uint64_t best = 0;
+        for (uint32_t j = threadIdx.x; j < n; j += T) best = keys[j] > best ? keys[j] : best;
+        const uint64_t bound = bound_of<T>(best, k.top, sel);
+        if (best >= bound)
+            for (uint32_t j = threadIdx.x; j < n; j += T) offer(keys[j], bound, sel);
+        __syncthreads();
+        if (sel.count <= LIST) put_ranked<T>(k.top, sel, put);
+        else put_by_rounds<T>(k.top, n, sel, [&](uint32_t j) { return keys[j]; }, put);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+template <int DT, bool VECTORS>
+__global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
+{
+    constexpr int T = 256, VEC = DT == DT_F32 ? 4 : 8, U = 2;
+    constexpr uint64_t ES = DT == DT_F32 ? 4 : 2;
+    quiet_maxima();
+    // the last rows first: the forward pass has read them last, and the caches hold them still
+    const uint32_t bid = gridDim.x - 1 - blockIdx.x;
+    const uint64_t row = bid / k.parts;
+    const uint32_t first = (bid - (uint32_t)row * k.parts) * k.part, n = min(k.classes - first, k.part);
+    const char *x = static_cast<const char *>(k.logits) + (row * k.stride + first) * ES;
+    char *dx = static_cast<char *>(k.grad_logits) + (row * k.grad_stride + first) * ES;
     const float lse = k.lse[row], H = k.entropy ? k.entropy[row] : 0.0f, h = k.grad_entropy ? k.grad_entropy[row] : 0.0f;
     const int64_t c = k.targets ? target_of(k, row) : k.ignore_index;
     float g = k.grad_logp && c != k.ignore_index ? k.grad_logp[row] : 0.0f;
     if (c != k.ignore_index && (c < 0 || c >= (int64_t)k.classes)) g = __builtin_nanf("");
     const bool none = lse == -INFINITY;
-    for (uint32_t j = threadIdx.x; j < k.classes; j += T) {
-        const float d = element<DT>(x, j) - lse, p = exp_exact(d);
-        float v = -g * p - (p != 0.0f ? h * p * (d + H) : 0.0f);
-        if ((int64_t)j == c) v += g;
-        if (none) v = 0.0f;
-        if constexpr (DT == DT_F32) reinterpret_cast<float *>(dx)[j] = v;
-        else reinterpret_cast<uint16_t *>(dx)[j] = half_bits<DT>(v);
+    const uint32_t target = c >= first && c < (int64_t)(first + n) ? (uint32_t)(c - first) : 0xffffffffu;
+    const float gh = __builtin_fmaf(h, H, g);
+    auto grad = [&](float v) {
+        const float d = v - lse, p = DT == DT_F32 ? exp_exact(d) : __builtin_amdgcn_exp2f(d * LOG2E);
+        return none ? 0.0f : -p * __builtin_fmaf(h, max2(d, FAR), gh);
+    };
+    auto one = [&](uint32_t j) {
+        float v[1] = {grad(element<DT>(x, j))};
+        if (j == target && !none) v[0] += g;
+        store_elems<DT, 1>(dx, j, v);
+    };
+    if constexpr (!VECTORS) {
+        for (uint32_t j = threadIdx.x; j < n; j += T) one(j);
+        return;
     }
+    const uint32_t head = min(n, (uint32_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (uint32_t)ES);
+    const uint32_t vectors = (n - head) / VEC, edges = n - vectors * VEC, tid = threadIdx.x;
+    if (tid < edges) one(tid < head ? tid : n - (edges - tid));
+    x += head * ES;
+    dx += head * ES;
+    auto whole_vector = [&](const Raw<DT, VEC> &raw, uint32_t i) {
+        float v[VEC];
+        unpack<DT, VEC>(raw, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = grad(v[e]);
+        const uint32_t in = target - head - i * VEC;
+        if (in < VEC && !none) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] += e == (int)in ? g : 0.0f;
+        }
+        store_elems<DT, VEC>(dx + i * 16ull, 0, v);
+    };
+    uint32_t i = tid;
+    for (; i + (U - 1) * T < vectors; i += U * T) {
+        Raw<DT, VEC> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load_raw<DT, VEC>(x + (i + u * T) * 16ull, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) whole_vector(raw[u], i + u * T);
+    }
+    for (; i < vectors; i += T) whole_vector(load_raw<DT, VEC>(x + i * 16ull, 0), i);
 }
 
 bs_status checked()
@@ -153,25 +469,45 @@ bs_status checked()
     return BS_ERR_HIP;
 }
 
+template <int DT, bool TOP>
+void launch(const LogProbsK &k, int threads, hipStream_t st)
+{
+    const dim3 grid((uint32_t)(k.rows * k.parts));
+    if (k.parts > 1) {
+        log_probs_kernel<DT, 256, TOP, true><<<grid, dim3(256), 0, st>>>(k);
+        log_probs_join_kernel<DT, TOP><<<dim3((uint32_t)k.rows), dim3(256), 0, st>>>(k);
+    } else if (threads == 64) {
+        log_probs_kernel<DT, 64, TOP, false><<<grid, dim3(64), 0, st>>>(k);
+    } else {
+        log_probs_kernel<DT, 256, TOP, false><<<grid, dim3(256), 0, st>>>(k);
+    }
+}
+
+template <int DT>
+void launch_backward(const LogProbsK &k, bool vectors, hipStream_t st)
+{
+    const dim3 grid((uint32_t)(k.rows * k.parts)), block(256);
+    if (vectors) log_probs_backward_kernel<DT, true><<<grid, block, 0, st>>>(k);
+    else log_probs_backward_kernel<DT, false><<<grid, block, 0, st>>>(k);
+}
+
 }  // namespace
 
-bs_status launch_log_probs(const LogProbsK &k, int32_t dtype, void *stream)
+bs_status launch_log_probs(const LogProbsK &k, int32_t dtype, int threads, void *stream)
 {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((uint32_t)k.rows), block(T);
-    if (dtype == BS_F32) log_probs_kernel<DT_F32><<<grid, block, 0, st>>>(k);
-    else if (dtype == BS_BF16) log_probs_kernel<DT_BF16><<<grid, block, 0, st>>>(k);
-    else log_probs_kernel<DT_F16><<<grid, block, 0, st>>>(k);
+    if (dtype == BS_F32) k.top ? launch<DT_F32, true>(k, threads, st) : launch<DT_F32, false>(k, threads, st);
+    else if (dtype == BS_BF16) k.top ? launch<DT_BF16, true>(k, threads, st) : launch<DT_BF16, false>(k, threads, st);
+    else k.top ? launch<DT_F16, true>(k, threads, st) : launch<DT_F16, false>(k, threads, st);
     return checked();
 }
 
-bs_status launch_log_probs_backward(const LogProbsK &k, int32_t dtype, void *stream)
+bs_status launch_log_probs_backward(const LogProbsK &k, int32_t dtype, bool vectors, void *stream)
 {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((uint32_t)k.rows), block(T);
-    if (dtype == BS_F32) log_probs_backward_kernel<DT_F32><<<grid, block, 0, st>>>(k);
-    else if (dtype == BS_BF16) log_probs_backward_kernel<DT_BF16><<<grid, block, 0, st>>>(k);
-    else log_probs_backward_kernel<DT_F16><<<grid, block, 0, st>>>(k);
+    if (dtype == BS_F32) launch_backward<DT_F32>(k, vectors, st);
+    else if (dtype == BS_BF16) launch_backward<DT_BF16>(k, vectors, st);
+    else launch_backward<DT_F16>(k, vectors, st);
     return checked();
 }
 
