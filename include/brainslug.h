@@ -516,6 +516,9 @@ typedef struct bs_group_norm_desc {
     int32_t activation; /* bs_activation                */
     double eps;         /* finite, >= 0                 */
     int64_t x_stride, residual_stride, y_stride, grad_y_stride, grad_x_stride, grad_residual_stride;
+    int32_t wait_polls; /* how often a work-group looks for the sums of an image's other parts before it computes them itself:
+                           0 = default (some milliseconds), -1 = never looks; changes no result                              */
+    int32_t reserved;
 } bs_group_norm_desc;
 
 /* Device bytes bs_group_norm (backward == 0) or bs_group_norm_backward (!= 0) needs as workspace; 0 for an invalid description. */

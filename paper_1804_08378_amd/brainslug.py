@@ -88,7 +88,8 @@ class bs_group_norm_desc(C.Structure):
     _fields_ = [("shape", C.c_int64 * 4), ("groups", C.c_int32), ("dtype", C.c_int32), ("param_dtype", C.c_int32),
                 ("activation", C.c_int32), ("eps", C.c_double),
                 ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y_stride", C.c_int64),
-                ("grad_y_stride", C.c_int64), ("grad_x_stride", C.c_int64), ("grad_residual_stride", C.c_int64)]
+                ("grad_y_stride", C.c_int64), ("grad_x_stride", C.c_int64), ("grad_residual_stride", C.c_int64),
+                ("wait_polls", C.c_int32), ("reserved", C.c_int32)]
 
 
 class bs_log_probs_desc(C.Structure):

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <numeric>
 
 #include "bs_internal.h"
 
@@ -33,18 +34,10 @@ bs_status check_desc(const bs_group_norm_desc *d)
     return BS_OK;
 }
 
-struct Space {
-    uint64_t part = 0, sums = 0, bytes = 0;  // offsets, size
-};
-
-// Pixel chunks and channel blocks.  Work-groups of at least 16 KiB of one tensor, 2048 of them where the tensor has so much.
+// Pixel chunks and channel blocks of the kernels that read x twice.  Work-groups of at least 16 KiB of one tensor, 2048 of them where the
+// tensor has so much.
 void split(const bs_group_norm_desc &d, NormK &k)
 {
-    k.N = (uint32_t)d.shape[0];
-    k.C = (uint32_t)d.shape[1];
-    k.P = (uint32_t)(d.shape[2] * d.shape[3]);
-    k.G = (uint32_t)d.groups;
-    k.per = k.C / k.G;
     k.blocks = (uint32_t)ceil_div(k.C, K_NORM_BLOCK_CHANNELS);
     k.spans = (k.per + K_NORM_BLOCK_CHANNELS - 2) / K_NORM_BLOCK_CHANNELS + 1;
     const uint64_t row = std::min<uint64_t>(k.C, K_NORM_BLOCK_CHANNELS) * dtype_size(d.dtype);
@@ -54,14 +47,81 @@ void split(const bs_group_norm_desc &d, NormK &k)
     k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
 }
 
-Space space(const NormK &k, bool backward)
+// The same for the kernels that keep their pixels in registers; false where they do not apply: a group too wide, or an image of more chunks
+// than a work-group joins (fewer where short vectors leave little in the registers, and the chunks' sums would be many).
+bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool residual, NormK &k, bool &few)
+{
+    const int full = (int)(16 / dtype_size(d.dtype));
+    if (vec != full && vec != full / 2 && vec != 1) return false;
+    // the smallest block of whole groups and whole vectors that has a cache line of every pixel and divides the channels
+    const uint64_t unit = std::lcm((uint64_t)k.per, (uint64_t)vec), units = k.C / unit;
+    uint64_t m = 1;
+    while (m < units && (units % m != 0 || unit * m * dtype_size(d.dtype) < 128)) ++m;
+    k.block = (uint32_t)(unit * m);
+    k.blocks = k.C / k.block;
+    const uint32_t groups = k.block / k.per, lanes = K_NORM_RESIDENT_THREADS / std::max<uint32_t>(1, k.block / (uint32_t)vec);
+    if (lanes < 8 || groups > (uint32_t)K_NORM_RESIDENT_THREADS) return false;
+    const bool mixed = k.per % (uint32_t)vec != 0;
+    for (const bool small : {false, true}) {
+        const int e = backward ? norm_resident_grad_pixels(vec, d.activation, residual && d.activation != BS_ACT_IDENTITY, small, mixed)
+                               : norm_resident_pixels(vec, residual, small, mixed);
+        const uint64_t chunks = ceil_div(k.P, (uint64_t)lanes * e);
+        if (chunks > (uint64_t)(vec == full ? 128 : vec == full / 2 ? 32 : 16) || chunks * groups > (uint64_t)K_NORM_WORDS) {
+            if (!small) return false;
+            break;  // few pixels a lane would be too many chunks: stay with many
+        }
+        k.chunk = (uint32_t)ceil_div(k.P, chunks);
+        k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
+        few = small;
+        if ((uint64_t)k.N * k.blocks * k.chunks >= 512) break;  // two work-groups for every compute unit
+    }
+    k.groups = groups;
+    k.lanes = lanes;
+    k.last = k.P - (k.chunks - 1) * k.chunk;
+    k.chunk_each = k.chunk / lanes;
+    k.last_each = k.last / lanes;
+    const uint32_t cvb = k.block / (uint32_t)vec, root = (uint32_t)std::ceil(std::sqrt((double)lanes));
+    k.slices = std::max<uint32_t>(1, std::min(root, K_NORM_RESIDENT_THREADS / cvb));
+    k.slices_wide = std::max<uint32_t>(1, std::min(root, K_NORM_RESIDENT_THREADS / k.block));
+    k.by_chunks = make_fastdiv(k.chunks);
+    k.by_blocks = make_fastdiv(k.blocks);
+    k.by_cvb = make_fastdiv(cvb);
+    k.by_cols_wide = make_fastdiv(k.block);
+    k.by_per = make_fastdiv(k.per);
+    k.by_vectors = make_fastdiv(std::max<uint32_t>(1, k.per / (uint32_t)vec));
+    return true;
+}
+
+struct Space {
+    uint64_t pairs = 0, words = 0, part = 0, bytes = 0;  // offsets, size
+};
+
+Space space(const NormK &k, bool backward, bool resident)
 {
     Space s;
-    const uint64_t pairs = (uint64_t)k.N * k.G * 2 * sizeof(float);
-    s.sums = 0;  // forward: the statistics, where the caller does not want them
-    s.part = aligned(pairs);
-    s.bytes = s.part + aligned(backward ? (uint64_t)k.N * k.chunks * k.C * 2 * sizeof(float) : pairs * k.chunks * k.spans);
+    const uint64_t pairs = (uint64_t)k.N * k.G * 8;  // forward: the statistics, where the caller does not want them; backward: the groups' sums
+    s.words = aligned(pairs);
+    s.part = s.words + (resident && k.chunks > 1 ? aligned(pairs * k.chunks) : 0);
+    s.bytes = s.part + (backward ? aligned((uint64_t)k.N * k.chunks * k.C * 8) : resident ? 0 : aligned(pairs * k.chunks * k.spans));
     return s;
+}
+
+void sizes(const bs_group_norm_desc &d, NormK &k)
+{
+    k.N = (uint32_t)d.shape[0];
+    k.C = (uint32_t)d.shape[1];
+    k.P = (uint32_t)(d.shape[2] * d.shape[3]);
+    k.G = (uint32_t)d.groups;
+    k.per = k.C / k.G;
+}
+
+// Chooses the kernels and lays out the workspace.
+bool plan(const bs_group_norm_desc &d, int vec, bool backward, bool residual, NormK &k, Space &s, bool &few)
+{
+    const bool resident = split_resident(d, vec, backward, residual, k, few);
+    if (!resident) split(d, k);
+    s = space(k, backward, resident);
+    return resident;
 }
 
 NormTensor tensor(const void *p, int64_t stride, const NormK &k) { return NormTensor{p, (uint64_t)(stride ? stride : k.C)}; }
@@ -79,6 +139,8 @@ int vector_of(const NormK &k, int32_t dtype, std::initializer_list<const NormTen
     }
     return (int)vec;
 }
+
+uint32_t polls_of(const bs_group_norm_desc &d) { return d.wait_polls < 0 ? 0 : d.wait_polls ? (uint32_t)d.wait_polls : K_NORM_POLLS; }
 
 TensorBytes bytes_of(const NormK &k, const NormTensor &t, uint64_t es) { return TensorBytes{t.p, (uint64_t)k.N * k.P, k.C * es, t.stride * es}; }
 TensorBytes bytes_of(const void *p, uint64_t n) { return TensorBytes{p, 1, n, n}; }
@@ -106,9 +168,20 @@ extern "C" {
 uint64_t bs_group_norm_workspace_bytes(const bs_group_norm_desc *desc, int32_t backward)
 {
     if (check_desc(desc) != BS_OK) return 0;
-    NormK k{};
-    split(*desc, k);
-    return space(k, backward != 0).bytes;
+    // addresses and strides decide on the vectors later: room for every choice
+    uint64_t bytes = 0;
+    for (int vec = (int)(16 / dtype_size(desc->dtype)); vec; vec /= 2) {
+        for (const bool residual : {false, true}) {
+            NormK k{};
+            sizes(*desc, k);
+            if (k.C % (uint32_t)vec != 0) continue;
+            Space s;
+            bool few;
+            plan(*desc, vec, backward != 0, residual, k, s, few);
+            bytes = std::max(bytes, s.bytes);
+        }
+    }
+    return bytes;
 }
 
 bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const void *residual, const void *weight, const void *bias, void *y,
@@ -118,12 +191,15 @@ bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const voi
     if (checked != BS_OK) return checked;
     if (!x || !y) return BS_ERR_NULL;
     NormK k{};
-    split(*desc, k);
+    sizes(*desc, k);
     k.x = tensor(x, desc->x_stride, k);
     k.r = tensor(residual, desc->residual_stride, k);
     k.y = tensor(y, desc->y_stride, k);
     const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), pairs = (uint64_t)k.N * k.G * 8;
-    const Space s = space(k, false);
+    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.y});
+    Space s;
+    bool few = false;
+    const bool resident = plan(*desc, vec, false, residual != nullptr, k, s, few);
     if (!workspace || workspace_bytes < s.bytes) return BS_ERR_WORKSPACE;
     for (const void *p : {x, residual, (const void *)y})
         if (!element_aligned(p, es)) return BS_ERR_ALIGN;
@@ -137,9 +213,15 @@ bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const voi
     k.f32_params = desc->param_dtype == BS_F32;
     k.eps = (float)desc->eps;
     char *const ws = static_cast<char *>(workspace);
-    k.stats = stats ? stats : reinterpret_cast<float *>(ws + s.sums);
+    k.words = reinterpret_cast<uint64_t *>(ws + s.words);
+    k.polls = polls_of(*desc);
+    if (resident) {
+        k.stats = stats;
+        const bs_status st = k.chunks > 1 ? launch_norm_absent(k, stream) : BS_OK;
+        return st != BS_OK ? st : launch_norm_resident(k, desc->dtype, vec, few, stream);
+    }
+    k.stats = stats ? stats : reinterpret_cast<float *>(ws + s.pairs);
     k.part = reinterpret_cast<float *>(ws + s.part);
-    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.y});
     for (const NormPass pass : {NORM_STATS, NORM_JOIN, NORM_APPLY}) {
         const bs_status st = launch_norm(pass, k, desc->dtype, vec, stream);
         if (st != BS_OK) return st;
@@ -155,14 +237,17 @@ bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, 
     if (checked != BS_OK) return checked;
     if (!x || !stats || !grad_y) return BS_ERR_NULL;
     NormK k{};
-    split(*desc, k);
+    sizes(*desc, k);
     k.x = tensor(x, desc->x_stride, k);
     k.r = tensor(residual, desc->residual_stride, k);
     k.dy = tensor(grad_y, desc->grad_y_stride, k);
     k.dx = tensor(grad_x, desc->grad_x_stride, k);
     k.dr = tensor(grad_residual, desc->grad_residual_stride, k);
     const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), pairs = (uint64_t)k.N * k.G * 8;
-    const Space s = space(k, true);
+    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.dy, &k.dx, &k.dr});
+    Space s;
+    bool few = false;
+    const bool resident = plan(*desc, vec, true, residual != nullptr, k, s, few);
     if (!workspace || workspace_bytes < s.bytes) return BS_ERR_WORKSPACE;
     for (const void *p : {x, residual, grad_y, (const void *)grad_x, (const void *)grad_residual})
         if (!element_aligned(p, es)) return BS_ERR_ALIGN;
@@ -183,10 +268,18 @@ bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, 
     k.eps = (float)desc->eps;
     char *const ws = static_cast<char *>(workspace);
     k.stats = const_cast<float *>(stats);
-    k.sums = reinterpret_cast<float *>(ws + s.sums);
+    k.sums = reinterpret_cast<float *>(ws + s.pairs);
     k.part = reinterpret_cast<float *>(ws + s.part);
-    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.dy, &k.dx, &k.dr});
+    k.words = reinterpret_cast<uint64_t *>(ws + s.words);
+    k.polls = polls_of(*desc);
     const bool tensors = grad_x || grad_residual, params = grad_weight || grad_bias;
+    if (resident) {
+        if (!params) k.part = nullptr;
+        bs_status st = k.chunks > 1 && tensors ? launch_norm_absent(k, stream) : BS_OK;
+        if (st == BS_OK && (tensors || params)) st = launch_norm_resident_grad(k, desc->dtype, vec, few, stream);
+        if (st == BS_OK && params) st = launch_norm(NORM_GRAD_PARAMS, k, desc->dtype, vec, stream);
+        return st;
+    }
     for (const NormPass pass : {NORM_GRAD_SUMS, NORM_GRAD_JOIN, NORM_GRAD_PARAMS, NORM_GRAD_APPLY}) {
         if (pass == NORM_GRAD_PARAMS ? !params : pass == NORM_GRAD_SUMS ? !params && !grad_x : pass == NORM_GRAD_JOIN ? !grad_x : !tensors) continue;
         const bs_status st = launch_norm(pass, k, desc->dtype, vec, stream);

@@ -9,56 +9,13 @@
 // from the batch's own mean, and merges them (Chan's update), so that a mean far from zero cancels nothing.
 #include <hip/hip_runtime.h>
 
-#include "bs_device.h"
 #include "bs_internal.h"
-#include "bs_norm.h"
+#include "bs_norm_device.h"
 
 namespace bs {
 namespace {
 
 constexpr int T = K_NORM_THREADS;
-
-// ------------------------------------------------------------------------------------------------ activations
-// exp for float32 results: the product with log2(e) in two parts, so that large arguments keep their last bits.
-BS_DEV float exp_exact(float v)
-{
-    const float hi = v * 1.44269504088896341f;
-    const float lo = __builtin_fmaf(v, 1.44269504088896341f, -hi) + v * 1.92596299112661746e-8f;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return __builtin_fabsf(hi) < 160.0f ? __builtin_fmaf(e, lo * 0.693147180559945309f, e) : e;  // (beyond: 0, infinity or NaN)
-}
-
-// 16-bit results hide the last bits of the exponential and of the reciprocal; float32 ones do not.
-template <int DT>
-BS_DEV float sigmoid(float z)
-{
-    if constexpr (DT == DT_F32) return 1.0f / (1.0f + exp_exact(-z));
-    else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504088896341f));
-}
-
-template <int DT, int ACT>
-BS_DEV float act(float z)
-{
-    if constexpr (ACT == BS_ACT_RELU) return z > 0.0f ? z : 0.0f;
-    if constexpr (ACT == BS_ACT_SILU) return z * sigmoid<DT>(z);
-    if constexpr (ACT == BS_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.707106781186547524f));
-    return z;
-}
-
-template <int DT, int ACT>
-BS_DEV float act_slope(float z)
-{
-    if constexpr (ACT == BS_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if constexpr (ACT == BS_ACT_SILU) {
-        const float s = sigmoid<DT>(z);
-        return s * (1.0f + z * (1.0f - s));
-    }
-    if constexpr (ACT == BS_ACT_GELU) {
-        const float phi = 0.398942280401432678f * exp_exact(-0.5f * z * z);
-        return 0.5f * (1.0f + erff(z * 0.707106781186547524f)) + z * phi;
-    }
-    return 1.0f;
-}
 
 // ------------------------------------------------------------------------------------------------ lanes and channels
 // Where a lane stands: its channel vector (c0 .. c0 + VEC - 1 of the tensor) and its first pixel; lanes beyond the block do nothing.
@@ -88,29 +45,6 @@ BS_DEV Lane lane_of(const NormK &k, uint32_t bid)
     l.p0 = l.chunk * k.chunk;
     l.p1 = min(l.p0 + k.chunk, k.P);
     return l;
-}
-
-template <int DT>
-BS_DEV const char *at_pixel(const NormTensor &t, uint32_t P, uint32_t n, uint32_t p, uint32_t c)
-{
-    return static_cast<const char *>(t.p) + (((uint64_t)n * P + p) * t.stride + c) * (DT != DT_F32 ? 2 : 4);
-}
-
-template <int DT, int VEC>
-BS_DEV void load_vec(const char *p, float (&v)[VEC])
-{
-    unpack<DT, VEC>(load_raw<DT, VEC>(p, 0), v);
-}
-
-template <int DT, int VEC>
-BS_DEV void load_params(const void *p, bool f32, uint32_t c, float none, float (&v)[VEC])
-{
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        if (!p) v[i] = none;
-        else if (DT == DT_F32 || f32) v[i] = static_cast<const float *>(p)[c + i];
-        else v[i] = half_up<DT>(static_cast<const uint16_t *>(p)[c + i]);
-    }
 }
 
 // Sums of M values per channel over the work-group's pixel lanes: lds[m][channel of the block], valid after the call's barrier.
@@ -343,25 +277,39 @@ __global__ __launch_bounds__(64) void norm_grad_join_kernel(NormK k)
     }
 }
 
-// Gradients of weight and bias: a thread per channel.
+// Gradients of weight and bias: four channels of all images' chunks by a work-group, a thread every 256th chunk of one channel.
+constexpr int PT = 1024;
 template <int DT>
-__global__ __launch_bounds__(T) void norm_grad_params_kernel(NormK k)
+__global__ __launch_bounds__(PT) void norm_grad_params_kernel(NormK k)
 {
-    const uint32_t c = blockIdx.x * T + threadIdx.x;
-    if (c >= k.C) return;
-    float db = 0.0f, dw = 0.0f;
-    for (uint32_t q = 0; q < k.N * k.chunks; ++q) {
-        const float *in = k.part + 2 * ((uint64_t)q * k.C + c);
-        db += in[0];
-        dw += in[1];
+    __shared__ float db[PT], dw[PT];
+    const uint32_t c = blockIdx.x * 4 + threadIdx.x % 4, row = threadIdx.x / 4, rows = k.N * k.chunks;
+    float s0 = 0.0f, s1 = 0.0f;
+    if (c < k.C) {
+#pragma unroll 8
+        for (uint32_t q = row; q < rows; q += PT / 4) {
+            const float2 in = *reinterpret_cast<const float2 *>(k.part + 2 * ((uint64_t)q * k.C + c));
+            s0 += in.x;
+            s1 += in.y;
+        }
     }
+    db[threadIdx.x] = s0;
+    dw[threadIdx.x] = s1;
+    for (uint32_t half = PT / 2; half >= 4; half /= 2) {
+        __syncthreads();
+        if (threadIdx.x < half) {
+            db[threadIdx.x] += db[threadIdx.x + half];
+            dw[threadIdx.x] += dw[threadIdx.x + half];
+        }
+    }
+    if (threadIdx.x >= 4 || c >= k.C) return;
     auto put = [&](void *p, float v) {
         if (!p) return;
         if (DT == DT_F32 || k.f32_params) static_cast<float *>(p)[c] = v;
         else static_cast<uint16_t *>(p)[c] = half_bits<DT>(v);
     };
-    put(k.dbias, db);
-    put(k.dweight, dw);
+    put(k.dbias, db[threadIdx.x]);
+    put(k.dweight, dw[threadIdx.x]);
 }
 
 template <int DT, int VEC, int ACT>
@@ -418,7 +366,7 @@ void launch(NormPass pass, const NormK &k, hipStream_t st)
         if constexpr (ACT == 0 && VEC == 1) norm_grad_join_kernel<DT><<<dim3(k.N * k.G), dim3(64), 0, st>>>(k);
         break;
     case NORM_GRAD_PARAMS:
-        if constexpr (ACT == 0 && VEC == 1) norm_grad_params_kernel<DT><<<dim3((k.C + T - 1) / T), block, 0, st>>>(k);
+        if constexpr (ACT == 0 && VEC == 1) norm_grad_params_kernel<DT><<<dim3((k.C + 3) / 4), dim3(PT), 0, st>>>(k);
         break;
     case NORM_GRAD_APPLY: norm_grad_apply_kernel<DT, VEC, ACT><<<grid, block, 0, st>>>(k); break;
     }

@@ -297,3 +297,58 @@ def test_an_image_of_more_than_two_to_the_31_bytes_and_a_tensor_of_more_elements
         for at in (0, p - 2500):
             got = y.permute(0, 2, 3, 1)[i].reshape(-1, c)[at:at + 2500].view(1, 50, 50, c).permute(0, 3, 1, 2)
             close(got, ref.y, 5 * ref.z_off + 1e-6, "bf16", "y")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(2, 64, 40, 40, 8), (1, 64, 60, 50, 32), (3, 48, 21, 20, 4), (2, 30, 30, 30, 6), (1, 256, 33, 31, 2)])
+def test_work_groups_that_do_not_wait(shape, dtype):
+    """Images of several chunks whose work-groups look for no other's sums (wait_polls = -1) compute them all themselves: the same bits."""
+    x, weight, bias, res, dy = tensors(shape, dtype, 4, True)
+    n, c, h, w, groups = shape
+    want, stats = F.group_norm_forward(x, groups, weight, bias, res, "silu")
+    grads = F.group_norm_backward(x, stats, dy, groups, weight, bias, res, "silu")
+    for residual in (res, None):
+        if residual is None:
+            want, stats = F.group_norm_forward(x, groups, weight, bias, None, "silu")
+            grads = F.group_norm_backward(x, stats, dy, groups, weight, bias, None, "silu")
+        d = F._norm_operands(x, groups, weight, bias, residual, "silu", 1e-5, dy)[0]
+        d.wait_polls = -1
+        y, st, gx, gr = torch.empty_like(want), torch.empty_like(stats), torch.empty_like(x), torch.empty_like(x)
+        gw, gb = torch.empty_like(weight), torch.empty_like(bias)
+        stream = torch.cuda.current_stream().cuda_stream
+        for backward in (False, True):
+            size = bs.bs_group_norm_workspace_bytes(d, backward)
+            ws = torch.full((size,), 255 if backward else 0, dtype=torch.uint8, device="cuda")  # (what it holds does not matter)
+            r = residual.data_ptr() if residual is not None else 0
+            if backward:
+                bs.bs_group_norm_backward(d, x.data_ptr(), r, weight.data_ptr(), bias.data_ptr(), st.data_ptr(), dy.data_ptr(), gx.data_ptr(),
+                                          gr.data_ptr(), gw.data_ptr(), gb.data_ptr(), ws.data_ptr(), size, stream)
+            else:
+                bs.bs_group_norm(d, x.data_ptr(), r, weight.data_ptr(), bias.data_ptr(), y.data_ptr(), st.data_ptr(), ws.data_ptr(), size, stream)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(st, stats) and torch.equal(gx, grads[0]) and torch.equal(gw, grads[1]) and torch.equal(gb, grads[2])
+        if residual is not None:
+            assert torch.equal(gr, grads[3])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(3, 256, 56, 56, 32), (2, 64, 112, 112, 32), (1, 96, 100, 75, 32), (1, 8, 90, 130, 8), (1, 64, 182, 181, 8), (2, 36, 50, 51, 4),
+                                   (1, 1024, 20, 19, 1), (7, 512, 14, 14, 32), (1, 32, 300, 280, 4)])
+def test_images_of_many_chunks(shape, dtype):
+    check(shape, dtype, "silu", True, seed=6)
+    check(shape, dtype, "gelu", False, seed=7)
+
+
+def test_launches_one_after_the_other_share_a_workspace():
+    """The second call finds the first one's words in the workspace and must not take them for its own."""
+    shape, groups = (2, 64, 60, 60), 8
+    xs = [torch.randn(shape, device="cuda").contiguous(memory_format=torch.channels_last) * (i + 1) for i in range(6)]
+    want = [F.group_norm(x, groups) for x in xs]
+    d = F._norm_operands(xs[0], groups, None, None, None, "identity", 1e-5)[0]
+    size = bs.bs_group_norm_workspace_bytes(d, False)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    ys = [torch.empty_like(x) for x in xs]
+    for x, y in zip(xs, ys):
+        bs.bs_group_norm(d, x.data_ptr(), 0, 0, 0, y.data_ptr(), 0, ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ys, want))
