@@ -57,7 +57,8 @@ def torch_ext_fits() -> bool:
 def up_to_date() -> bool:
     if not os.path.exists(LIB):
         return False
-    if torch_tag() and (not torch_ext_fits() or os.path.getmtime(TORCH_EXT) < os.path.getmtime(os.path.join(CSRC, "bs_torch.cpp"))):
+    if torch_tag() and (not torch_ext_fits() or any(os.path.getmtime(TORCH_EXT) < os.path.getmtime(d) for d in (
+            os.path.join(CSRC, "bs_torch.cpp"), os.path.join(ROOT, "include", "brainslug.h")))):
         return False
     t = os.path.getmtime(LIB)
     deps = sources() + [os.path.join(CSRC, h) for h in JIT_HEADERS + ["bs_internal.h", "bs_rows_tables.h", "bs_nhwc_device.h", "bs_bwd_device.h", "bs_strip_device.h", "bs_backward_keys.h", "bs_norm.h", "bs_norm_device.h", "bs_norm_resident.h", "bs_log_probs.h"]]
@@ -98,7 +99,7 @@ def build_torch_ext() -> None:
            "-DBS_TORCH_TAG=\"%s\"" % torch_tag(), "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
     for d in [*cpp_extension.include_paths(), "/opt/rocm/include", sysconfig.get_paths()["include"]]:
         cmd += ["-isystem", d]
-    cmd += [os.path.join(CSRC, "bs_torch.cpp"), "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"]
+    cmd += ["-I", os.path.join(ROOT, "include"), os.path.join(CSRC, "bs_torch.cpp"), "-o", tmp, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, TORCH_EXT)
 

@@ -27,6 +27,8 @@
 #include <utility>
 #include <vector>
 
+#include "brainslug.h"
+
 namespace {
 
 using Shape = std::array<int64_t, 4>;
@@ -493,6 +495,282 @@ PyObject *set_error(PyObject *, PyObject *cls)
     Py_RETURN_NONE;
 }
 
+// ---------------------------------------------------------------------------------------------------- operators without a plan
+// Group normalisation and log probabilities (functional.py): the same bargain, every function returns None for what is not the plain case.
+struct Operators {
+    decltype(&bs_group_norm_workspace_bytes) norm_bytes;
+    decltype(&bs_group_norm) norm;
+    decltype(&bs_group_norm_backward) norm_backward;
+    decltype(&bs_log_probs_workspace_bytes) head_bytes;
+    decltype(&bs_log_probs) head;
+    decltype(&bs_log_probs_backward) head_backward;
+};
+Operators g_operators{};
+
+// set_operators((addresses of the six functions, in this order))
+PyObject *set_operators(PyObject *, PyObject *args)
+{
+    unsigned long long a[6];
+    if (!PyArg_ParseTuple(args, "(KKKKKK)", a, a + 1, a + 2, a + 3, a + 4, a + 5)) return nullptr;
+    g_operators = {reinterpret_cast<decltype(Operators::norm_bytes)>(a[0]), reinterpret_cast<decltype(Operators::norm)>(a[1]),
+                   reinterpret_cast<decltype(Operators::norm_backward)>(a[2]), reinterpret_cast<decltype(Operators::head_bytes)>(a[3]),
+                   reinterpret_cast<decltype(Operators::head)>(a[4]), reinterpret_cast<decltype(Operators::head_backward)>(a[5])};
+    Py_RETURN_NONE;
+}
+
+int32_t dtype_code(at::ScalarType t) { return t == at::kFloat ? BS_F32 : t == at::kBFloat16 ? BS_BF16 : t == at::kHalf ? BS_F16 : -1; }
+
+// A tensor argument that may be None; false: neither (no error set).
+bool optional_tensor(PyObject *o, at::Tensor &t)
+{
+    if (o == Py_None) return true;
+    const at::Tensor *p = tensor_of(o);
+    if (!p) return false;
+    t = *p;
+    return t.defined();
+}
+bool on_gpu(const at::Tensor &t, const at::Device &dev) { return t.is_cuda() && t.has_storage() && t.device() == dev; }
+
+// Elements from a pixel to the next of a channels-last tensor or a channel slice of one; 0: it is neither.
+int64_t pixel_stride(const at::Tensor &t)
+{
+    const int64_t n = t.size(0), c = t.size(1), h = t.size(2), w = t.size(3);
+    const int64_t sn = t.stride(0), sc = t.stride(1), sh = t.stride(2), sw = t.stride(3);
+    const int64_t step = w > 1 ? sw : h > 1 ? sh : n > 1 ? sn : c;
+    return step >= c && (c == 1 || sc == 1) && (w == 1 || sw == step) && (h == 1 || sh == w * step) && (n == 1 || sn == h * w * step) ? step : 0;
+}
+
+bool read_int(PyObject *o, int64_t &v)
+{
+    v = PyLong_Check(o) ? PyLong_AsLongLong(o) : 0;
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return PyLong_Check(o);
+}
+bool read_float(PyObject *o, double &v)
+{
+    v = PyFloat_Check(o) ? PyFloat_AS_DOUBLE(o) : 0;
+    return PyFloat_Check(o);
+}
+
+struct NormCall {
+    bs_group_norm_desc d{};
+    at::Tensor x, weight, bias, residual;
+    at::TensorOptions like;
+
+    // x, groups, weight, bias, residual, activation, eps; false: not the plain case
+    bool read(PyObject *xo, PyObject *groups, PyObject *wo, PyObject *bo, PyObject *ro, PyObject *act, PyObject *eps)
+    {
+        const at::Tensor *xp = tensor_of(xo);
+        if (!g_operators.norm || !xp || modes_active() || !xp->defined() || !xp->is_cuda() || !xp->has_storage() || xp->dim() != 4) return false;
+        x = *xp;
+        int64_t g, a;
+        if (!read_int(groups, g) || !read_int(act, a) || !read_float(eps, d.eps) || g < 1 || g > x.size(1)) return false;
+        if (!optional_tensor(wo, weight) || !optional_tensor(bo, bias) || !optional_tensor(ro, residual)) return false;
+        d.groups = (int32_t)g;
+        d.activation = (int32_t)a;
+        d.dtype = dtype_code(x.scalar_type());
+        d.param_dtype = BS_F32;
+        for (int i = 0; i < 4; ++i) d.shape[i] = x.size(i);
+        if (d.dtype < 0 || x.size(0) < 1 || (d.x_stride = pixel_stride(x)) == 0) return false;
+        like = x.options();
+        at::ScalarType type = at::ScalarType::Undefined;
+        for (const at::Tensor *p : {&weight, &bias}) {
+            if (!p->defined()) continue;
+            if (!on_gpu(*p, x.device()) || p->dim() != 1 || p->size(0) != x.size(1) || !p->is_contiguous()) return false;
+            if (p->scalar_type() != at::kFloat && p->scalar_type() != x.scalar_type()) return false;
+            if (type != at::ScalarType::Undefined && type != p->scalar_type()) return false;
+            type = p->scalar_type();
+            d.param_dtype = dtype_code(type);
+        }
+        return beside(residual, d.residual_stride);
+    }
+    // A tensor of x's shape, type and device that is read in place (or none).
+    bool beside(const at::Tensor &t, int64_t &stride) const
+    {
+        return !t.defined() || (on_gpu(t, x.device()) && t.sizes() == x.sizes() && t.scalar_type() == x.scalar_type() && (stride = pixel_stride(t)) != 0);
+    }
+    at::Tensor empty() const { return at::empty(x.sizes(), like.memory_format(at::MemoryFormat::ChannelsLast)); }
+    static void *ptr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+};
+
+at::Tensor workspace_of(uint64_t n, const at::TensorOptions &like)
+{
+    return n ? at::empty({(int64_t)n}, like.dtype(at::kByte)) : at::Tensor();
+}
+
+PyObject *tuple_of(std::initializer_list<at::Tensor> tensors)
+{
+    PyObject *t = PyTuple_New((Py_ssize_t)tensors.size());
+    if (!t) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor &v : tensors) {
+        PyObject *o = v.defined() ? THPVariable_Wrap(v) : Py_NewRef(Py_None);
+        if (!o) {
+            Py_DECREF(t);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(t, i++, o);
+    }
+    return t;
+}
+
+// group_norm(x, groups, weight, bias, residual, activation, eps, keep statistics?) -> y, (y, stats) or None
+PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    NormCall c;
+    if (n != 8 || !c.read(args[0], args[1], args[2], args[3], args[4], args[5], args[6])) Py_RETURN_NONE;
+    const bool keep = args[7] == Py_True;
+    at::Tensor y, stats;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        y = c.empty();
+        if (keep) stats = at::empty({c.x.size(0), c.d.groups, 2}, c.like.dtype(at::kFloat));
+        const uint64_t bytes = g_operators.norm_bytes(&c.d, 0);
+        const at::Tensor ws = workspace_of(bytes, c.like);
+        const int rc = g_operators.norm(&c.d, c.x.data_ptr(), c.ptr(c.residual), c.ptr(c.weight), c.ptr(c.bias), y.data_ptr(), static_cast<float *>(c.ptr(stats)),
+                                        c.ptr(ws), bytes, c10::hip::getCurrentHIPStream(c.x.device().index()).stream());
+        if (rc != 0) throw CallFailed(rc, "bs_group_norm");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return keep ? tuple_of({y, stats}) : THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+// group_norm_backward(x, stats, grad, groups, weight, bias, residual, activation, eps, wanted: bits 1 x, 2 weight, 4 bias, 8 residual)
+// -> (grad_x, grad_weight, grad_bias, grad_residual) or None
+PyObject *group_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    NormCall c;
+    if (n != 10 || !c.read(args[0], args[3], args[4], args[5], args[6], args[7], args[8])) Py_RETURN_NONE;
+    const at::Tensor *stats = tensor_of(args[1]), *grad = tensor_of(args[2]);
+    int64_t wanted;
+    if (!stats || !grad || !stats->defined() || !grad->defined() || !read_int(args[9], wanted) || !c.beside(*grad, c.d.grad_y_stride)) Py_RETURN_NONE;
+    if (!on_gpu(*stats, c.x.device()) || stats->scalar_type() != at::kFloat || !stats->is_contiguous() || stats->dim() != 3 || stats->size(0) != c.x.size(0) ||
+        stats->size(1) != c.d.groups || stats->size(2) != 2)
+        Py_RETURN_NONE;
+    const at::Tensor st = *stats, dy = *grad;
+    at::Tensor gx, gw, gb, gr;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        if (wanted & 1) gx = c.empty();
+        if ((wanted & 2) && c.weight.defined()) gw = at::empty({c.x.size(1)}, c.weight.options());
+        if ((wanted & 4) && c.bias.defined()) gb = at::empty({c.x.size(1)}, c.bias.options());
+        if ((wanted & 8) && c.residual.defined()) gr = c.empty();
+        const uint64_t bytes = g_operators.norm_bytes(&c.d, 1);
+        const at::Tensor ws = workspace_of(bytes, c.like);
+        const int rc = g_operators.norm_backward(&c.d, c.x.data_ptr(), c.ptr(c.residual), c.ptr(c.weight), c.ptr(c.bias), static_cast<const float *>(st.data_ptr()),
+                                                 dy.data_ptr(), c.ptr(gx), c.ptr(gr), c.ptr(gw), c.ptr(gb), c.ptr(ws), bytes,
+                                                 c10::hip::getCurrentHIPStream(c.x.device().index()).stream());
+        if (rc != 0) throw CallFailed(rc, "bs_group_norm_backward");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({gx, gw, gb, gr});
+    END_HANDLE_TH_ERRORS
+}
+
+struct HeadCall {
+    bs_log_probs_desc d{};
+    at::Tensor logits, targets;
+
+    // Elements from a row to the next where the classes of a row are contiguous; -1: they are not.
+    static int64_t row_stride(const at::Tensor &t)
+    {
+        const int64_t rows = t.size(0), classes = t.size(1);
+        if ((classes > 1 && t.stride(1) != 1) || (rows > 1 && t.stride(0) < classes)) return -1;
+        return rows > 1 ? t.stride(0) : classes;
+    }
+    bool read(PyObject *lo, PyObject *to, PyObject *top, PyObject *ignore)
+    {
+        const at::Tensor *lp = tensor_of(lo);
+        if (!g_operators.head || !lp || modes_active() || !lp->defined() || !lp->is_cuda() || !lp->has_storage() || lp->dim() != 2) return false;
+        logits = *lp;
+        int64_t k;
+        if (!optional_tensor(to, targets) || !read_int(top, k) || k < 0 || k > BS_MAX_TOP || !read_int(ignore, d.ignore_index)) return false;
+        d.rows = logits.size(0);
+        d.classes = logits.size(1);
+        d.top = (int32_t)k;
+        d.dtype = dtype_code(logits.scalar_type());
+        d.target_bytes = 8;
+        if (d.dtype < 0 || d.rows < 1 || d.classes < 1 || (d.row_stride = row_stride(logits)) < 0) return false;
+        if (targets.defined()) {
+            if (!on_gpu(targets, logits.device()) || targets.dim() != 1 || targets.size(0) != d.rows || !targets.is_contiguous()) return false;
+            if (targets.scalar_type() != at::kLong && targets.scalar_type() != at::kInt) return false;
+            d.target_bytes = targets.scalar_type() == at::kInt ? 4 : 8;
+        }
+        return true;
+    }
+    bool per_row(const at::Tensor &t) const
+    {
+        return !t.defined() || (on_gpu(t, logits.device()) && t.scalar_type() == at::kFloat && t.dim() == 1 && t.size(0) == d.rows && t.is_contiguous());
+    }
+};
+
+// log_probs(logits, targets, top, ignore_index) -> (logp, entropy, top_logp, top_index, lse) or None
+PyObject *log_probs(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    HeadCall c;
+    if (n != 4 || !c.read(args[0], args[1], args[2], args[3])) Py_RETURN_NONE;
+    at::Tensor logp, entropy, lse, top_logp, top_index;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const at::TensorOptions f32 = c.logits.options().dtype(at::kFloat);
+        if (c.targets.defined()) logp = at::empty({c.d.rows}, f32);
+        entropy = at::empty({c.d.rows}, f32);
+        lse = at::empty({c.d.rows}, f32);
+        if (c.d.top) {
+            top_logp = at::empty({c.d.rows, c.d.top}, f32);
+            top_index = at::empty({c.d.rows, c.d.top}, f32.dtype(at::kInt));
+        }
+        const uint64_t bytes = g_operators.head_bytes(&c.d);
+        const at::Tensor ws = workspace_of(bytes, f32);
+        auto p = [](const at::Tensor &t) { return static_cast<float *>(NormCall::ptr(t)); };
+        const int rc = g_operators.head(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), p(logp), p(entropy), p(lse), p(top_logp),
+                                        static_cast<int32_t *>(NormCall::ptr(top_index)), NormCall::ptr(ws), bytes,
+                                        c10::hip::getCurrentHIPStream(c.logits.device().index()).stream());
+        if (rc != 0) throw CallFailed(rc, "bs_log_probs");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({logp, entropy, top_logp, top_index, lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// log_probs_backward(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index) -> grad_logits or None
+PyObject *log_probs_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    HeadCall c;
+    at::Tensor lse, entropy, g, h, out;
+    PyObject *const zero = PyLong_FromLong(0);
+    const bool fits = n == 7 && c.read(args[0], args[1], zero, args[6]) && optional_tensor(args[2], lse) && optional_tensor(args[3], entropy) &&
+                      optional_tensor(args[4], g) && optional_tensor(args[5], h);
+    Py_XDECREF(zero);
+    if (!fits || !lse.defined() || !c.per_row(lse) || !c.per_row(entropy) || !c.per_row(g) || !c.per_row(h)) Py_RETURN_NONE;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        out = at::empty({c.d.rows, c.d.classes}, c.logits.options());
+        auto p = [](const at::Tensor &t) { return static_cast<const float *>(NormCall::ptr(t)); };
+        const int rc = g_operators.head_backward(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), p(lse), p(entropy), p(g), p(h), out.data_ptr(),
+                                                 c10::hip::getCurrentHIPStream(c.logits.device().index()).stream());
+        if (rc != 0) throw CallFailed(rc, "bs_log_probs_backward");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+template <typename F>
+constexpr PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
+
 PyMethodDef plan_methods[] = {
     {"run", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(plan_run)), METH_FASTCALL, "(x, residuals) -> (out, indices) or None"},
     {"infer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(plan_infer)), METH_FASTCALL, "(x, residuals) -> out or None"},
@@ -510,7 +788,15 @@ PyType_Slot plan_slots[] = {{Py_tp_new, reinterpret_cast<void *>(plan_new)},
                             {0, nullptr}};
 PyType_Spec plan_spec = {"_bs_torch.Plan", sizeof(PlanObject), 0, Py_TPFLAGS_DEFAULT, plan_slots};
 
-PyMethodDef module_methods[] = {{"set_error", set_error, METH_O, "(class): raised as class(status, where)"}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef module_methods[] = {{"set_error", set_error, METH_O, "(class): raised as class(status, where)"},
+                                {"set_operators", set_operators, METH_VARARGS, "((addresses,)): the library's functions without a plan"},
+                                {"group_norm", fast(group_norm), METH_FASTCALL, "(x, groups, weight, bias, residual, activation, eps, keep) -> y, (y, stats) or None"},
+                                {"group_norm_backward", fast(group_norm_backward), METH_FASTCALL,
+                                 "(x, stats, grad, groups, weight, bias, residual, activation, eps, wanted) -> gradients or None"},
+                                {"log_probs", fast(log_probs), METH_FASTCALL, "(logits, targets, top, ignore_index) -> results or None"},
+                                {"log_probs_backward", fast(log_probs_backward), METH_FASTCALL,
+                                 "(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index) -> gradient or None"},
+                                {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_bs_torch", nullptr, -1, module_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -7,6 +7,7 @@ pairs are the single passes, for programs that keep their own tape.  Everything 
 """
 from __future__ import annotations
 
+import ctypes as C
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -19,6 +20,25 @@ __all__ = ["group_norm", "group_norm_forward", "group_norm_backward", "GroupNorm
 
 ACTIVATIONS = {"identity": bs.BS_ACT_IDENTITY, "relu": bs.BS_ACT_RELU, "silu": bs.BS_ACT_SILU, "gelu": bs.BS_ACT_GELU}
 _DTYPES = {torch.float32: bs.BS_F32, torch.bfloat16: bs.BS_BF16, torch.float16: bs.BS_F16}
+
+
+_native = None  # the native calls (csrc/bs_torch.cpp), False: not built for this torch; None: not looked for yet
+
+
+def _native_calls():
+    """Every one of them takes the plain case -- tensors that are read in place, on one device, without dispatch modes -- and returns None for
+    any other, which the Python code takes or refuses."""
+    global _native
+    if _native is None:
+        with bs._native_lock:
+            if _native is None:
+                module, lib = bs._torch_calls(), bs.load()
+                if module is not None:
+                    names = ("bs_group_norm_workspace_bytes", "bs_group_norm", "bs_group_norm_backward", "bs_log_probs_workspace_bytes", "bs_log_probs",
+                             "bs_log_probs_backward")
+                    module.set_operators(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in names))
+                _native = module or False
+    return _native
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -95,6 +115,11 @@ def _norm_operands(x, groups, weight, bias, residual, activation, eps, grad=None
 
 
 def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stats):
+    native, act = _native_calls(), ACTIVATIONS.get(activation)
+    if native and out is None and act is not None:
+        done = native.group_norm(x, groups, weight, bias, residual, act, eps, keep_stats)
+        if done is not None:
+            return done if keep_stats else (done, None)
     d, x, residual, _ = _norm_operands(x, groups, weight, bias, residual, activation, eps)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device, memory_format=torch.channels_last)
@@ -126,6 +151,11 @@ def group_norm_backward(x, stats, grad, groups: int, weight=None, bias=None, res
                         need=(True, True, True, True)):
     """`(grad_x, grad_weight, grad_bias, grad_residual)` from the gradient `grad` of `group_norm_forward`'s result; `need` says which of
     them are wanted (those of absent operands are None)."""
+    native, act = _native_calls(), ACTIVATIONS.get(activation)
+    if native and act is not None:
+        done = native.group_norm_backward(x, stats, grad, groups, weight, bias, residual, act, eps, need[0] | need[1] << 1 | need[2] << 2 | need[3] << 3)
+        if done is not None:
+            return done
     with torch.no_grad():
         d, x, residual, grad = _norm_operands(x, groups, weight, bias, residual, activation, eps, grad)
         if tuple(stats.shape) != (x.shape[0], groups, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != x.device:
@@ -235,6 +265,11 @@ def _readable_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
 def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -100) -> LogProbs:
     """Log probabilities of `targets`, entropy and `top` best classes of every row of `logits` (rows x classes; rows may lie further apart
     than they are long).  What masked classes, empty rows and ignored targets give stands at bs_log_probs in include/brainslug.h."""
+    native = _native_calls()
+    if native:
+        done = native.log_probs(logits, targets, top, ignore_index)
+        if done is not None:
+            return LogProbs(*done)
     with torch.no_grad():
         d, targets = _head_operands(logits, targets, top, ignore_index)
         logits, d.row_stride = _readable_rows(logits)
@@ -255,6 +290,11 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient with respect to the logits from those of `logp` and `entropy` (a float a row; None: zero).  `out=logits` writes it over
     the logits."""
+    native = _native_calls()
+    if native and out is None:
+        done = native.log_probs_backward(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index)
+        if done is not None:
+            return done
     with torch.no_grad():
         d, targets = _head_operands(logits, targets, 0, ignore_index)
         rows = logits.shape[0]

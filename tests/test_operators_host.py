@@ -136,3 +136,37 @@ def test_pixel_strides():
         else:
             steps = {offsets[c * (p + 1)] - offsets[c * p] for p in range(n * h * w - 1)}
             assert len(steps) > 1 or min(steps) < c or (c > 1 and sc != 1), (t.shape, t.stride())
+
+
+@pytest.mark.gpu
+def test_native_and_python_calls_agree(monkeypatch):
+    """The native calls take the plain case; without them the Python code makes the same call of the library."""
+    g = torch.Generator().manual_seed(0)
+    x, res, dy = (torch.randn(3, 24, 6, 5, generator=g).cuda().contiguous(memory_format=torch.channels_last) for _ in range(3))
+    w, b = torch.rand(24, generator=g).cuda(), torch.randn(24, generator=g).cuda()
+    logits, t, gl, ge = torch.randn(7, 300, generator=g).cuda(), torch.randint(0, 300, (7,), generator=g).cuda(), torch.randn(7, generator=g).cuda(), torch.randn(7, generator=g).cuda()
+
+    def everything():
+        y, stats = F.group_norm_forward(x, 4, w, b, res, "gelu")
+        r = F.log_probs_forward(logits, t, 6)
+        return [y, stats, F.group_norm(x, 4, w, None), *F.group_norm_backward(x, stats, dy, 4, w, b, res, "gelu", need=(True, False, True, True)),
+                *r, F.log_probs_backward(logits, t, r.lse, r.entropy, gl, None), F.log_probs_backward(logits, t, r.lse, r.entropy, gl, ge)]
+
+    assert F._native_calls(), "the native calls are built"
+    native = everything()
+    monkeypatch.setattr(F, "_native", False)
+    for a, c in zip(native, everything()):
+        assert (a is None and c is None) or torch.equal(a, c)
+    monkeypatch.undo()
+    with pytest.raises(ValueError, match="residual"):
+        F.group_norm(x, 4, w, b, res[:, :8])
+    with pytest.raises(bs.BrainSlugError) as e:
+        F.group_norm(x, 5, w, b)
+    assert e.value.status == PARAM
+    with pytest.raises(bs.BrainSlugError) as e:
+        F.log_probs(logits, t, 33)
+    assert e.value.status == PARAM
+    with pytest.raises(TypeError):
+        F.log_probs(logits.double(), t)
+    with pytest.raises(ValueError, match="targets"):
+        F.log_probs(logits, t[:3])
