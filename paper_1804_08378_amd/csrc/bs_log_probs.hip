@@ -94,73 +94,85 @@ struct Sums {
     }
 };
 
-template <int T>
-BS_DEV float over_lanes_max(float v)
+// One lane's value from another by a fixed pattern inside rows of 16 lanes.
+template <int CTRL>
+BS_DEV float in_row(float v)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = __builtin_fmaxf(v, __shfl_xor(v, o));
-    return v;
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+constexpr int SWAP1 = 0xb1, SWAP2 = 0x4e, MIRROR8 = 0x141, MIRROR16 = 0x140;  // quad_perm, row_half_mirror, row_mirror
+
+BS_DEV float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+
+// Over the 64 lanes of a wave, the same in each: inside rows by patterns, the four rows by scalar reads (a shuffle through LDS costs five times a step).
+BS_DEV float wave_sum(float v)
+{
+    v += in_row<SWAP1>(v);
+    v += in_row<SWAP2>(v);
+    v += in_row<MIRROR8>(v);
+    v += in_row<MIRROR16>(v);
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+BS_DEV float wave_max(float v)  // (NaN is left out)
+{
+    v = max2(v, in_row<SWAP1>(v));
+    v = max2(v, in_row<SWAP2>(v));
+    v = max2(v, in_row<MIRROR8>(v));
+    v = max2(v, in_row<MIRROR16>(v));
+    return max2(max2(lane_value(v, 0), lane_value(v, 16)), max2(lane_value(v, 32), lane_value(v, 48)));
 }
 
 // The work-group's sums from its lanes', in every lane.  lds: 3 * T / 64 floats.
 template <int T>
 BS_DEV Sums join_lanes(const Sums &mine, float *lds)
 {
-    const float own = mine.above == -INFINITY ? -INFINITY : mine.base;
-    const float wave_base = over_lanes_max<T>(own);
+    const float base = wave_max(mine.above == -INFINITY ? -INFINITY : mine.base);
     Sums r = mine;
-    r.move(wave_base == -INFINITY ? 0.0f : wave_base);
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        r.s += __shfl_xor(r.s, o);
-        r.t += __shfl_xor(r.t, o);
-    }
-    if (wave_base == -INFINITY) r.above = -INFINITY;
+    r.move(base == -INFINITY ? 0.0f : base);
+    r.s = wave_sum(r.s);
+    r.t = wave_sum(r.t);
+    if (base == -INFINITY) r.above = -INFINITY;
     if constexpr (T > 64) {
-        const uint32_t wave = threadIdx.x / 64;
-        if (threadIdx.x % 64 == 0) {
-            lds[3 * wave] = wave_base;
-            lds[3 * wave + 1] = r.s;
-            lds[3 * wave + 2] = r.t;
+        constexpr int W = T / 64;
+        const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+        if (lane == 0) {
+            lds[wave] = base;
+            lds[W + wave] = r.s;
+            lds[2 * W + wave] = r.t;
         }
         __syncthreads();
-        float base = lds[0];
-#pragma unroll
-        for (int w = 1; w < T / 64; ++w) base = __builtin_fmaxf(base, lds[3 * w]);
-        r = Sums();
-#pragma unroll
-        for (int w = 0; w < T / 64; ++w) {
-            Sums part;
-            part.base = lds[3 * w];
-            part.above = lds[3 * w] == -INFINITY ? -INFINITY : part.base;
-            part.s = lds[3 * w + 1];
-            part.t = lds[3 * w + 2];
-            part.move(base == -INFINITY ? 0.0f : base);
-            r.s += part.s;
-            r.t += part.t;
-        }
-        if (base != -INFINITY) {
-            r.base = base;
-            r.above = base;
-        }
+        // every wave joins the waves' results, one a lane
+        Sums part;
+        const float its = lane < W ? lds[lane] : -INFINITY;
+        part.base = its;
+        part.above = its;
+        part.s = lane < W ? lds[W + lane] : 0.0f;
+        part.t = lane < W ? lds[2 * W + lane] : 0.0f;
+        const float all = wave_max(its);
+        part.move(all == -INFINITY ? 0.0f : all);
+        r.s = wave_sum(part.s);
+        r.t = wave_sum(part.t);
+        r.base = all == -INFINITY ? 0.0f : all;
+        r.above = all;
         __syncthreads();
     }
     return r;
 }
 
 // ------------------------------------------------------------------------------------------------ top classes
+template <int T>
 struct Selection {
-    uint64_t lane[256];
+    uint64_t lane[T];
     uint64_t list[LIST];
     uint64_t bound;
     uint32_t count, lanes;
-    uint16_t chosen[256];
+    uint16_t chosen[T];
 };
 
 // A lower bound of the k-th best class's number: the k-th best of 64 numbers that have a class each, the best of 64 sets of lanes (0: fewer than
 // k sets have any).  `key`: the lane's best, 0 for none.  Valid in every lane.
 template <int T>
-BS_DEV uint64_t bound_of(uint64_t key, uint32_t k, Selection &sel)
+BS_DEV uint64_t bound_of(uint64_t key, uint32_t k, Selection<T> &sel)
 {
     sel.lane[threadIdx.x] = key;
     if (threadIdx.x == 0) {
@@ -187,7 +199,8 @@ BS_DEV uint64_t bound_of(uint64_t key, uint32_t k, Selection &sel)
     return sel.bound;
 }
 
-BS_DEV void offer(uint64_t key, uint64_t bound, Selection &sel)
+template <int T>
+BS_DEV void offer(uint64_t key, uint64_t bound, Selection<T> &sel)
 {
     if (key >= bound && key != 0) {
         const uint32_t at = atomicAdd(&sel.count, 1u);
@@ -197,7 +210,7 @@ BS_DEV void offer(uint64_t key, uint64_t bound, Selection &sel)
 
 // The k best of the offered numbers, best first: put(place, key); places beyond the number offered get 0.  The caller has synchronised.
 template <int T, typename PUT>
-BS_DEV void put_ranked(uint32_t k, const Selection &sel, PUT put)
+BS_DEV void put_ranked(uint32_t k, const Selection<T> &sel, PUT put)
 {
     const uint32_t n = sel.count;
     for (uint32_t i = threadIdx.x; i < n; i += T) {
@@ -212,7 +225,7 @@ BS_DEV void put_ranked(uint32_t k, const Selection &sel, PUT put)
 // The same from any numbers, one after the other: every round finds the best below the last.  For rows with NaN or infinity, and where too
 // many candidates pass the bound.
 template <int T, typename GET, typename PUT>
-BS_DEV void put_by_rounds(uint32_t k, uint32_t n, Selection &sel, GET get, PUT put)
+BS_DEV void put_by_rounds(uint32_t k, uint32_t n, Selection<T> &sel, GET get, PUT put)
 {
     uint64_t last = ~0ull;
     for (uint32_t r = 0; r < k; ++r) {
@@ -237,19 +250,30 @@ BS_DEV void put_by_rounds(uint32_t k, uint32_t n, Selection &sel, GET get, PUT p
 }
 
 // ------------------------------------------------------------------------------------------------ a row's results
-template <int DT>
-BS_DEV void put_row(const LogProbsK &k, uint64_t row, const char *x, const Sums &r)
+// The row's given class: requested before anything else of the row, used behind everything.
+struct Given {
+    int64_t c = 0;
+    float x = 0.0f;
+    template <int DT>
+    BS_DEV void request(const LogProbsK &k, uint64_t row, const char *logits)
+    {
+        if (!k.logp) return;
+        c = target_of(k, row);
+        if (c >= 0 && c < (int64_t)k.classes) x = element<DT>(logits, (uint64_t)c);
+    }
+};
+
+BS_DEV void put_row(const LogProbsK &k, uint64_t row, const Given &given, const Sums &r)
 {
     const bool none = r.s == 0.0f;  // every class masked
     const float log_s = logf(r.s);
     if (k.entropy) k.entropy[row] = none ? 0.0f : log_s - r.t / r.s;
     if (k.lse) k.lse[row] = none ? -INFINITY : r.base + log_s;
     if (k.logp) {
-        const int64_t c = target_of(k, row);
         float v;
-        if (c == k.ignore_index) v = 0.0f;
-        else if (c < 0 || c >= (int64_t)k.classes) v = __builtin_nanf("");
-        else v = none ? -INFINITY : (element<DT>(x, (uint64_t)c) - r.base) - log_s;
+        if (given.c == k.ignore_index) v = 0.0f;
+        else if (given.c < 0 || given.c >= (int64_t)k.classes) v = __builtin_nanf("");
+        else v = none ? -INFINITY : (given.x - r.base) - log_s;
         k.logp[row] = v;
     }
 }
@@ -284,6 +308,8 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
     const uint32_t head = min(n, (uint32_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (uint32_t)ES);
     const uint32_t vectors = (n - head) / VEC, edges = n - vectors * VEC, tid = threadIdx.x;
     const uint32_t edge = tid < head ? tid : n - (edges - tid);  // the lane's odd element, for tid < edges
+    Given given;
+    if constexpr (!PARTS) given.request<DT>(k, row, whole);
 
     Sums sums;
     float best = -INFINITY;
@@ -310,14 +336,37 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
         else most = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max2(v[6], v[7]));
         take(v, most, where);
     };
-    for (; i + (U - 1) * T < vectors; i += U * T, src += U * T * 16) {
-        Raw<DT, VEC> raw[U];
+    // batches of U vectors; the next one is under way while one is worked on
+    Raw<DT, VEC> raw[U];
+    uint32_t batches = vectors / (U * T);
+    if (batches) {
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = load_raw<DT, VEC>(src + u * T * 16, 0);
+    }
+    for (; batches > 1; --batches, i += U * T) {
+        Raw<DT, VEC> next[U];
+        src += U * T * 16;
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = load_raw<DT, VEC>(src + u * T * 16, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) whole_vector(raw[u], head + (i + u * T) * VEC);
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = next[u];
+    }
+    // the last full batch, and up to U - 1 vectors of a lane behind it
+    Raw<DT, VEC> rest[U];
+    const uint32_t behind = i + (batches ? U * T : 0);
+    src += batches ? U * T * 16 : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (behind + u * T < vectors) rest[u] = load_raw<DT, VEC>(src + u * T * 16, 0);
+    if (batches) {
 #pragma unroll
         for (int u = 0; u < U; ++u) whole_vector(raw[u], head + (i + u * T) * VEC);
     }
-    for (; i < vectors; i += T, src += T * 16) whole_vector(load_raw<DT, VEC>(src, 0), head + i * VEC);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (behind + u * T < vectors) whole_vector(rest[u], head + (behind + u * T) * VEC);
     if (tid >= head && tid < edges) take(odd, odd[0], edge);
 
     const Sums r = join_lanes<T>(sums, lds);
@@ -329,10 +378,10 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
             out[2] = r.t;
         }
     } else if (tid == 0) {
-        put_row<DT>(k, row, whole, r);
+        put_row(k, row, given, r);
     }
     if constexpr (TOP) {
-        __shared__ Selection sel;
+        __shared__ Selection<T> sel;
         const PutTop top(k, row, r);
         auto put = [&](uint32_t place, uint64_t key) {
             if constexpr (PARTS) k.part_keys[(uint64_t)blockIdx.x * k.top + place] = key;
@@ -345,14 +394,15 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
             if (key >= bound && tid < vectors) sel.chosen[atomicAdd(&sel.lanes, 1u)] = (uint16_t)tid;
             if (tid < edges) offer(rank_key(odd[0], first + edge), bound, sel);
             __syncthreads();
-            const uint32_t lanes = sel.lanes;
-            for (uint32_t c = tid / 64; c < lanes; c += T / 64) {
-                for (uint32_t j = sel.chosen[c] + (tid % 64) * T; j < vectors; j += 64 * T) {
-                    float v[VEC];
-                    unpack<DT, VEC>(load_raw<DT, VEC>(x + head * ES + j * 16ull, 0), v);
+            // the chosen lanes' vectors once more, one a thread
+            const uint32_t each = (vectors + T - 1) / T, again = sel.lanes * each;
+            for (uint32_t e = tid; e < again; e += T) {
+                const uint32_t c = e / each, j = sel.chosen[c] + (e - c * each) * T;
+                if (j >= vectors) continue;
+                float v[VEC];
+                unpack<DT, VEC>(load_raw<DT, VEC>(x + head * ES + j * 16ull, 0), v);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) offer(rank_key(v[e], first + head + j * VEC + e), bound, sel);
-                }
+                for (int i = 0; i < VEC; ++i) offer(rank_key(v[i], first + head + j * VEC + i), bound, sel);
             }
             __syncthreads();
             if (sel.count <= LIST) {
@@ -371,6 +421,17 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
     constexpr int T = 256;
     __shared__ float lds[3 * T / 64];
     const uint64_t row = blockIdx.x;
+    Given given;
+    given.request<DT>(k, row, static_cast<const char *>(k.logits) + row * k.stride * (DT != DT_F32 ? 2 : 4));
+    // the best classes of the parts, up to U of a lane at once
+    constexpr int U = 4;
+    const uint64_t *keys = k.part_keys + row * k.parts * k.top;
+    const uint32_t n = k.parts * k.top;
+    uint64_t first[U], best = 0;
+    if constexpr (TOP) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) first[u] = threadIdx.x + u * T < n ? keys[threadIdx.x + u * T] : 0;
+    }
     Sums mine;
     if (threadIdx.x < k.parts) {  // at most 256
         const float *in = k.part_sums + 4 * (row * k.parts + threadIdx.x);
@@ -382,18 +443,19 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
         mine.t = in[2];
     }
     const Sums r = join_lanes<T>(mine, lds);
-    const char *x = static_cast<const char *>(k.logits) + row * k.stride * (DT != DT_F32 ? 2 : 4);
-    if (threadIdx.x == 0) put_row<DT>(k, row, x, r);
+    if (threadIdx.x == 0) put_row(k, row, given, r);
     if constexpr (TOP) {
-        __shared__ Selection sel;
+        __shared__ Selection<T> sel;
         const PutTop put(k, row, r);
-        const uint64_t *keys = k.part_keys + row * k.parts * k.top;
-        const uint32_t n = k.parts * k.top;
-        uint64_t best = 0;
-        for (uint32_t j = threadIdx.x; j < n; j += T) best = keys[j] > best ? keys[j] : best;
+#pragma unroll
+        for (int u = 0; u < U; ++u) best = first[u] > best ? first[u] : best;
+        for (uint32_t j = threadIdx.x + U * T; j < n; j += T) best = keys[j] > best ? keys[j] : best;
         const uint64_t bound = bound_of<T>(best, k.top, sel);
-        if (best >= bound)
-            for (uint32_t j = threadIdx.x; j < n; j += T) offer(keys[j], bound, sel);
+        if (best >= bound) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) offer(first[u], bound, sel);
+            for (uint32_t j = threadIdx.x + U * T; j < n; j += T) offer(keys[j], bound, sel);
+        }
         __syncthreads();
         if (sel.count <= LIST) put_ranked<T>(k.top, sel, put);
         else put_by_rounds<T>(k.top, n, sel, [&](uint32_t j) { return keys[j]; }, put);
@@ -404,7 +466,7 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
 template <int DT, bool VECTORS>
 __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
 {
-    constexpr int T = 256, VEC = DT == DT_F32 ? 4 : 8, U = 2;
+    constexpr int T = 256, VEC = DT == DT_F32 ? 4 : 8, U = 4;
     constexpr uint64_t ES = DT == DT_F32 ? 4 : 2;
     quiet_maxima();
     // the last rows first: the forward pass has read them last, and the caches hold them still
@@ -478,6 +540,7 @@ void launch(const LogProbsK &k, int threads, hipStream_t st)
         log_probs_join_kernel<DT, TOP><<<dim3((uint32_t)k.rows), dim3(256), 0, st>>>(k);
     } else if (threads == 64) {
         log_probs_kernel<DT, 64, TOP, false><<<grid, dim3(64), 0, st>>>(k);
+
     } else {
         log_probs_kernel<DT, 256, TOP, false><<<grid, dim3(256), 0, st>>>(k);
     }

@@ -62,19 +62,22 @@ bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool re
     const uint32_t groups = k.block / k.per, lanes = K_NORM_RESIDENT_THREADS / std::max<uint32_t>(1, k.block / (uint32_t)vec);
     if (lanes < 8 || groups > (uint32_t)K_NORM_RESIDENT_THREADS) return false;
     const bool mixed = k.per % (uint32_t)vec != 0;
+    // One chunk needs no exchange and no second launch: few pixels a lane where they are enough for that, many where they are half empty (one
+    // work-group that fills its registers is slower than four that exchange: 8x512x28x28 binary16 13.4 us against 9.6).  Images of several
+    // chunks: many pixels a lane, or few where that leaves compute units without work.
+    const bool in_gradient = residual && d.activation != BS_ACT_IDENTITY;
+    uint64_t chunks[2];
+    bool half_empty = false;
     for (const bool small : {false, true}) {
-        const int e = backward ? norm_resident_grad_pixels(vec, d.activation, residual && d.activation != BS_ACT_IDENTITY, small, mixed)
-                               : norm_resident_pixels(vec, residual, small, mixed);
-        const uint64_t chunks = ceil_div(k.P, (uint64_t)lanes * e);
-        if (chunks > (uint64_t)(vec == full ? 128 : vec == full / 2 ? 32 : 16) || chunks * groups > (uint64_t)K_NORM_WORDS) {
-            if (!small) return false;
-            break;  // few pixels a lane would be too many chunks: stay with many
-        }
-        k.chunk = (uint32_t)ceil_div(k.P, chunks);
-        k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
-        few = small;
-        if ((uint64_t)k.N * k.blocks * k.chunks >= 512) break;  // two work-groups for every compute unit
+        const int e = backward ? norm_resident_grad_pixels(vec, d.activation, in_gradient, small, mixed) : norm_resident_pixels(vec, residual, small, mixed);
+        chunks[small] = ceil_div(k.P, (uint64_t)lanes * e);
+        if (!small) half_empty = k.P <= (uint64_t)lanes * e / 2;
     }
+    const uint64_t most = std::min<uint64_t>(vec == full ? 128 : vec == full / 2 ? 32 : 16, (uint64_t)K_NORM_WORDS / groups);
+    if (chunks[0] > most) return false;
+    few = chunks[1] == 1 || (!half_empty && chunks[1] <= most && (uint64_t)k.N * k.blocks * chunks[0] < 512);
+    k.chunk = (uint32_t)ceil_div(k.P, chunks[few]);
+    k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
     k.groups = groups;
     k.lanes = lanes;
     k.last = k.P - (k.chunks - 1) * k.chunk;
