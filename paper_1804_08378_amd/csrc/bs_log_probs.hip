@@ -18,7 +18,7 @@ namespace bs {
 namespace {
 
 constexpr float LOG2E = 1.44269504088896341f;
-constexpr float FAR = -200.0f;      // exp is 0 from here on: stands for larger distances where they are multiplied by it
+constexpr float FAR = -300.0f;      // 2 to this power is 0: stands for larger distances where they are multiplied by it
 constexpr uint32_t LIST = 512;      // candidates for the top classes that a work-group keeps
 
 // exp for float32 results: the product with log2(e) in two parts, so that large arguments keep their last bits.
@@ -57,41 +57,63 @@ BS_DEV int64_t target_of(const LogProbsK &k, uint64_t row)
 }
 
 // ------------------------------------------------------------------------------------------------ sums
-struct Sums {
-    float base = 0.0f;         // reference: a value seen (0: none but -infinity and NaN so far)
-    float above = -INFINITY;   // the reference moves for values above this; -infinity: there is none yet
-    float s = 0.0f, t = 0.0f;  // sum of exp(x - base), of exp(x - base) (x - base)
+// Exponents in units of log2(e) x: one multiply-add an element.  The product is not rounded before the reference's is taken off, and the
+// factor's own rounding stretches all logits alike, by 1.3e-8; t is taken back by the factor's reciprocal.
+constexpr float UNIT = (float)(1.0 / (double)LOG2E);
+constexpr float UNSET = -2e38f;  // no reference yet; logits from here down (masks of the type's lowest value) count as far below any reference
 
-    BS_DEV void move(float to)
-    {
-        const bool first = above == -INFINITY;
-        const float d = first ? 0.0f : __builtin_fmaxf(base - to, FAR), f = first ? 0.0f : __builtin_amdgcn_exp2f(d * LOG2E);
-        t = f * __builtin_fmaf(s, d, t);
-        s *= f;
-        base = to;
-        above = to + 1.0f;
-    }
+struct Sums {
+    float ref = 0.0f, base = 0.0f;  // reference: a value seen, and its product with log2(e)
+    float above = UNSET;            // the reference moves for values above this
+    float s = 0.0f, t = 0.0f;       // sum of 2^d, of 2^d d,  d = log2(e) x - base
+
     template <int N>
     BS_DEV void add(const float (&v)[N], float most)
     {
-        if (most > above) move(most);
-        float e[N], w[N];
+        if (most > above) {
+            const bool first = above == UNSET;
+            const float to = most * LOG2E, d = first ? 0.0f : __builtin_fmaxf(base - to, FAR), f = first ? 0.0f : __builtin_amdgcn_exp2f(d);
+            t = f * __builtin_fmaf(s, d, t);
+            s *= f;
+            ref = most;
+            base = to;
+            above = most + 1.0f;
+        }
+        float e[N], w = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float d = v[i] - base;
-            e[i] = __builtin_amdgcn_exp2f(d * LOG2E);
-            w[i] = e[i] * max2(d, FAR);
+            const float d = __builtin_fmaf(v[i], LOG2E, -base);
+            e[i] = __builtin_amdgcn_exp2f(d);
+            w = __builtin_fmaf(e[i], max2(d, FAR), w);
         }
 #pragma unroll
         for (int n = N / 2; n; n /= 2)
 #pragma unroll
-            for (int i = 0; i < n; ++i) {
-                e[i] += e[i + n];
-                w[i] += w[i + n];
-            }
+            for (int i = 0; i < n; ++i) e[i] += e[i + n];
         s += e[0];
-        t += w[0];
+        t += w;
     }
+    BS_DEV bool any() const { return above != UNSET; }
+    // From the rounded product of the reference to the reference itself.
+    BS_DEV void settle()
+    {
+        const float off = __builtin_fmaf(ref, LOG2E, -base);
+        if (__builtin_fabsf(base) == INFINITY) return;  // (the sums are 0 or NaN)
+        const float f = __builtin_amdgcn_exp2f(-off);
+        t = f * __builtin_fmaf(-off, s, t);
+        s *= f;
+    }
+    // Settled sums against another, larger reference (there is one, or the sums are 0 or NaN and stay so).
+    BS_DEV void shift(float to)
+    {
+        const float d = any() ? __builtin_fmaxf((ref - to) * LOG2E, FAR) : FAR, f = __builtin_amdgcn_exp2f(d);
+        t = f * __builtin_fmaf(s, d, t);
+        s *= f;
+        ref = to;
+    }
+    BS_DEV float log_s() const { return logf(s); }
+    BS_DEV float entropy() const { return logf(s) - t / s * UNIT; }
+    BS_DEV bool none() const { return s == 0.0f; }  // every class masked
 };
 
 // One lane's value from another by a fixed pattern inside rows of 16 lanes.
@@ -122,40 +144,38 @@ BS_DEV float wave_max(float v)  // (NaN is left out)
     return max2(max2(lane_value(v, 0), lane_value(v, 16)), max2(lane_value(v, 32), lane_value(v, 48)));
 }
 
-// The work-group's sums from its lanes', in every lane.  lds: 3 * T / 64 floats.
+// The work-group's sums from its lanes' settled ones, in every lane.  lds: 3 * T / 64 floats.
 template <int T>
 BS_DEV Sums join_lanes(const Sums &mine, float *lds)
 {
-    const float base = wave_max(mine.above == -INFINITY ? -INFINITY : mine.base);
+    float ref = wave_max(mine.any() ? mine.ref : -INFINITY);
     Sums r = mine;
-    r.move(base == -INFINITY ? 0.0f : base);
+    r.shift(ref);
     r.s = wave_sum(r.s);
     r.t = wave_sum(r.t);
-    if (base == -INFINITY) r.above = -INFINITY;
     if constexpr (T > 64) {
         constexpr int W = T / 64;
         const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
         if (lane == 0) {
-            lds[wave] = base;
+            lds[wave] = ref;
             lds[W + wave] = r.s;
             lds[2 * W + wave] = r.t;
         }
         __syncthreads();
         // every wave joins the waves' results, one a lane
         Sums part;
-        const float its = lane < W ? lds[lane] : -INFINITY;
-        part.base = its;
-        part.above = its;
+        part.ref = lane < W ? lds[lane] : -INFINITY;
+        if (part.ref != -INFINITY) part.above = part.ref;
         part.s = lane < W ? lds[W + lane] : 0.0f;
         part.t = lane < W ? lds[2 * W + lane] : 0.0f;
-        const float all = wave_max(its);
-        part.move(all == -INFINITY ? 0.0f : all);
+        ref = wave_max(part.ref);
+        part.shift(ref);
         r.s = wave_sum(part.s);
         r.t = wave_sum(part.t);
-        r.base = all == -INFINITY ? 0.0f : all;
-        r.above = all;
         __syncthreads();
     }
+    r.ref = ref;
+    r.above = ref == -INFINITY ? UNSET : ref;
     return r;
 }
 
@@ -265,15 +285,15 @@ struct Given {
 
 BS_DEV void put_row(const LogProbsK &k, uint64_t row, const Given &given, const Sums &r)
 {
-    const bool none = r.s == 0.0f;  // every class masked
-    const float log_s = logf(r.s);
-    if (k.entropy) k.entropy[row] = none ? 0.0f : log_s - r.t / r.s;
-    if (k.lse) k.lse[row] = none ? -INFINITY : r.base + log_s;
+    const bool none = r.none();
+    const float log_s = r.log_s();
+    if (k.entropy) k.entropy[row] = none ? 0.0f : r.entropy();
+    if (k.lse) k.lse[row] = none ? -INFINITY : r.ref + log_s;
     if (k.logp) {
         float v;
         if (given.c == k.ignore_index) v = 0.0f;
         else if (given.c < 0 || given.c >= (int64_t)k.classes) v = __builtin_nanf("");
-        else v = none ? -INFINITY : (given.x - r.base) - log_s;
+        else v = none ? -INFINITY : (given.x - r.ref) - log_s;
         k.logp[row] = v;
     }
 }
@@ -281,15 +301,40 @@ BS_DEV void put_row(const LogProbsK &k, uint64_t row, const Given &given, const 
 struct PutTop {
     const LogProbsK &k;
     uint64_t row;
-    float base, log_s;
+    float ref, log_s;
     bool none;
-    BS_DEV PutTop(const LogProbsK &k_, uint64_t row_, const Sums &r) : k(k_), row(row_), base(r.base), log_s(logf(r.s)), none(r.s == 0.0f) {}
+    BS_DEV PutTop(const LogProbsK &k_, uint64_t row_, const Sums &r) : k(k_), row(row_), ref(r.ref), log_s(r.log_s()), none(r.none()) {}
     BS_DEV void operator()(uint32_t place, uint64_t key) const
     {
         k.top_index[row * k.top + place] = (int32_t)key_index(key);
-        k.top_logp[row * k.top + place] = none ? -INFINITY : (key_value(key) - base) - log_s;
+        k.top_logp[row * k.top + place] = none ? -INFINITY : (key_value(key) - ref) - log_s;
     }
 };
+
+// Sums of elements none of which is in the range that Sums::add works on: all of them masked, or all below it (rows that hold nothing but the
+// type's lowest value), or some above it.  The largest first, then differences from it.
+template <int DT, int T>
+BS_DEV Sums far_sums(const char *x, uint32_t n, float *lds)
+{
+    Sums mine;
+    float most = -INFINITY;
+    for (uint32_t j = threadIdx.x; j < n; j += T) most = max2(most, element<DT>(x, j));
+    most = wave_max(most);
+    if constexpr (T > 64) {
+        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = most;
+        __syncthreads();
+        for (int w = 0; w < T / 64; ++w) most = max2(most, lds[w]);
+        __syncthreads();
+    }
+    if (most == -INFINITY) return mine;
+    for (uint32_t j = threadIdx.x; j < n; j += T) {
+        const float d = (element<DT>(x, j) - most) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+        mine.s += e;
+        mine.t = __builtin_fmaf(e, max2(d, FAR), mine.t);
+    }
+    mine.ref = mine.above = most;
+    return join_lanes<T>(mine, lds);
+}
 
 // One part of one row (or, with PARTS false, the whole row) by a work-group of T threads.  A part begins at any element: the elements in
 // front of its first and behind its last whole 128-bit vector are a lane's each.
@@ -369,11 +414,13 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
         if (behind + u * T < vectors) whole_vector(rest[u], head + (behind + u * T) * VEC);
     if (tid >= head && tid < edges) take(odd, odd[0], edge);
 
-    const Sums r = join_lanes<T>(sums, lds);
+    sums.settle();
+    Sums r = join_lanes<T>(sums, lds);
+    if (r.none()) r = far_sums<DT, T>(x, n, lds);
     if constexpr (PARTS) {
         if (tid == 0) {
             float *out = k.part_sums + 4 * (uint64_t)blockIdx.x;
-            out[0] = r.above == -INFINITY ? -INFINITY : r.base;
+            out[0] = r.any() ? r.ref : -INFINITY;
             out[1] = r.s;
             out[2] = r.t;
         }
@@ -435,10 +482,8 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
     Sums mine;
     if (threadIdx.x < k.parts) {  // at most 256
         const float *in = k.part_sums + 4 * (row * k.parts + threadIdx.x);
-        if (in[0] != -INFINITY) {
-            mine.base = in[0];
-            mine.above = in[0];
-        }
+        mine.ref = in[0];
+        if (in[0] != -INFINITY) mine.above = in[0];
         mine.s = in[1];
         mine.t = in[2];
     }
@@ -463,7 +508,8 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-template <int DT, bool VECTORS>
+// STREAM: the logits go past the caches.
+template <int DT, bool VECTORS, bool STREAM>
 __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
 {
     constexpr int T = 256, VEC = DT == DT_F32 ? 4 : 8, U = 4;
@@ -481,10 +527,11 @@ __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
     if (c != k.ignore_index && (c < 0 || c >= (int64_t)k.classes)) g = __builtin_nanf("");
     const bool none = lse == -INFINITY;
     const uint32_t target = c >= first && c < (int64_t)(first + n) ? (uint32_t)(c - first) : 0xffffffffu;
-    const float gh = __builtin_fmaf(h, H, g);
+    // none: -p (0 - 0) of p = 2^-infinity, without a test in the loop
+    const float gh = none ? 0.0f : __builtin_fmaf(h, H, g), hd = none ? 0.0f : h, off = none ? INFINITY : lse;
     auto grad = [&](float v) {
-        const float d = v - lse, p = DT == DT_F32 ? exp_exact(d) : __builtin_amdgcn_exp2f(d * LOG2E);
-        return none ? 0.0f : -p * __builtin_fmaf(h, max2(d, FAR), gh);
+        const float d = v - off, p = DT == DT_F32 ? exp_exact(d) : __builtin_amdgcn_exp2f(d * LOG2E);
+        return -p * __builtin_fmaf(hd, max2(d, FAR), gh);
     };
     auto one = [&](uint32_t j) {
         float v[1] = {grad(element<DT>(x, j))};
@@ -516,7 +563,7 @@ __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
     for (; i + (U - 1) * T < vectors; i += U * T) {
         Raw<DT, VEC> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = load_raw<DT, VEC>(x + (i + u * T) * 16ull, 0);
+        for (int u = 0; u < U; ++u) raw[u] = load_raw<DT, VEC, STREAM>(x + (i + u * T) * 16ull, 0);
 #pragma unroll
         for (int u = 0; u < U; ++u) whole_vector(raw[u], i + u * T);
     }
@@ -550,8 +597,12 @@ template <int DT>
 void launch_backward(const LogProbsK &k, bool vectors, hipStream_t st)
 {
     const dim3 grid((uint32_t)(k.rows * k.parts)), block(256);
-    if (vectors) log_probs_backward_kernel<DT, true><<<grid, block, 0, st>>>(k);
-    else log_probs_backward_kernel<DT, false><<<grid, block, 0, st>>>(k);
+    // logits that the last cache (256 MiB) holds from the forward pass are read through it: 8192x32000 bfloat16 181 us cached, 174 streamed;
+    // 1001x10007 float32 15.0 and 17.4
+    const bool stream = k.rows * k.classes * (DT == DT_F32 ? 4 : 2) > (256ull << 20);
+    if (!vectors) log_probs_backward_kernel<DT, false, false><<<grid, block, 0, st>>>(k);
+    else if (stream) log_probs_backward_kernel<DT, true, true><<<grid, block, 0, st>>>(k);
+    else log_probs_backward_kernel<DT, true, false><<<grid, block, 0, st>>>(k);
 }
 
 }  // namespace

@@ -261,3 +261,22 @@ def test_offsets_beyond_32_bits():
     # 2^26 terms of equal size: chains of 2^18 a lane at most, each step's rounding half a unit: 2^18 * 2^-24 of that part of the sum, which is 1e-2 of all
     assert abs(float(r.lse[0]) - lse) < 1e-3 and abs(float(r.logp[0]) - (8 - lse)) < 1e-3
     assert r.top_index[0].tolist() == [12345, classes - 1, 0] and r.top_index[32].tolist() == [classes - 2, 12345, classes - 1]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_at_the_ends_of_the_range(dtype):
+    """Logits whose product with log2(e) is no float32 any more; masks of the type's lowest value next to real logits."""
+    low = torch.finfo(DTYPES[dtype]).min
+    for classes in (70, 5000, 120000):
+        x, t, g, h = make(6, classes, dtype, 30)
+        x[0, 0], x[0, classes - 1] = 3.0e38, 2.9e38
+        x[1] = low
+        x[2, :classes - 3] = low        # real logits come last
+        x[3, 1:] = -math.inf
+        x[3, 0] = low                   # one class left, the lowest of all
+        x[4] = 3.2e38
+        x[4, 5] = low
+        x[5, ::2] = low
+        t[0], t[2], t[3], t[4] = 0, classes - 1, 0, 1
+        h[0] = h[4] = 0  # (an entropy's gradient next to differences of 1e38: products with probabilities 0)
+        check(x, t, 5, g, h)
