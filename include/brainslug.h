@@ -508,6 +508,8 @@ typedef enum bs_activation {
  * each other, *_stride elements from one to the next: 0 = C (dense), more where the tensor is a channel slice of a larger one.
  * Storage types: dtype for every tensor, param_dtype (BS_F32 or dtype) for weight, bias and their gradients.
  */
+#define BS_GROUP_NORM_EXCHANGE_BYTES (4ull << 20)
+
 typedef struct bs_group_norm_desc {
     int64_t shape[4];
     int32_t groups;     /* divides C                    */
@@ -516,6 +518,10 @@ typedef struct bs_group_norm_desc {
     int32_t activation; /* bs_activation                */
     double eps;         /* finite, >= 0                 */
     int64_t x_stride, residual_stride, y_stride, grad_y_stride, grad_x_stride, grad_residual_stride;
+    void *exchange;          /* device, 8-byte aligned, or NULL: memory that the parts of an image hand sums through.  Zero-filled before its first
+                                use, used by these calls alone and by one at a time (one stream), it is zero again behind every call.  NULL, or
+                                too small for the call: the workspace serves, cleared by a launch of its own                              */
+    uint64_t exchange_bytes; /* its size; BS_GROUP_NORM_EXCHANGE_BYTES is enough for nearly every tensor */
     int32_t wait_polls; /* how often a work-group looks for the sums of an image's other parts before it computes them itself:
                            0 = default (some milliseconds), -1 = never looks; changes no result                              */
     int32_t reserved;

@@ -30,6 +30,7 @@ VARIANT_NAMES = {1: "stream", 2: "pool_direct", 3: "lds_tile", 4: "pool_rows", 5
 BS_LAYOUT_NCHW, BS_LAYOUT_NHWC = 0, 1
 BS_ACT_IDENTITY, BS_ACT_RELU, BS_ACT_SILU, BS_ACT_GELU = 0, 1, 2, 3
 BS_MAX_TOP = 32
+BS_GROUP_NORM_EXCHANGE_BYTES = 4 << 20
 STATUS_NAMES = {
     0: "BS_OK", 1: "BS_ERR_NULL", 2: "BS_ERR_SHAPE", 3: "BS_ERR_PARAM", 4: "BS_ERR_UNSUPPORTED",
     5: "BS_ERR_NOT_PLANNED", 6: "BS_ERR_NO_FIT", 7: "BS_ERR_ALIGN", 8: "BS_ERR_WORKSPACE",
@@ -89,7 +90,7 @@ class bs_group_norm_desc(C.Structure):
                 ("activation", C.c_int32), ("eps", C.c_double),
                 ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y_stride", C.c_int64),
                 ("grad_y_stride", C.c_int64), ("grad_x_stride", C.c_int64), ("grad_residual_stride", C.c_int64),
-                ("wait_polls", C.c_int32), ("reserved", C.c_int32)]
+                ("exchange", C.c_void_p), ("exchange_bytes", C.c_uint64), ("wait_polls", C.c_int32), ("reserved", C.c_int32)]
 
 
 class bs_log_probs_desc(C.Structure):

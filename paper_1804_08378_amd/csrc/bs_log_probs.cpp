@@ -35,7 +35,7 @@ void fill(const bs_log_probs_desc &d, LogProbsK &k)
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// Work-groups of a row: one where the rows alone fill the device; else parts of at least `least` classes, `wanted` work-groups in all.
+// Parts of a row, a work-group each: at least `least` classes, `wanted` work-groups in all.
 void split(LogProbsK &k, uint64_t least, uint64_t wanted)
 {
     const uint64_t parts = std::max<uint64_t>(1, std::min({ceil_div(wanted, k.rows), ceil_div(k.classes, least), (uint64_t)K_LOG_PROBS_MOST_PARTS}));
@@ -55,10 +55,15 @@ Space space(const LogProbsK &k)
     return s;
 }
 
+// Few long rows are cut into parts of at least 8 KiB and joined by a second launch, which costs 7 us: from 96 KiB a row on, up to 128 rows
+// (bfloat16, 20 alternatives, whole rows and parts: 1x32768 11.1 and 13.0 us, 1x65536 14.6 and 13.0, 1x131072 22.0 and 13.2, 128x131072 23.8 and
+// 21.1, 256x131072 26.2 and 26.5).
 void fill_forward(const bs_log_probs_desc &d, LogProbsK &k)
 {
     fill(d, k);
-    split(k, 2048, 512);
+    const uint64_t es = dtype_size(d.dtype);
+    const bool cut = k.rows <= 128 && k.classes * es >= (96 << 10);
+    split(k, cut ? 8192 / es : k.classes, 256);
 }
 
 bool aligned(const void *p, uint64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }

@@ -27,6 +27,7 @@ bs_status check_desc(const bs_group_norm_desc *d)
     if (d->groups < 1 || C % d->groups != 0) return BS_ERR_PARAM;
     if (d->shape[2] > limit || d->shape[3] > limit || d->shape[0] > limit || C > limit) return BS_ERR_UNSUPPORTED;
     if ((double)d->shape[1] * (double)d->shape[2] * (double)d->shape[3] > (double)limit) return BS_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(d->exchange) % 8 != 0) return BS_ERR_ALIGN;
     // grids are counted in 32 bits: images, groups
     if (d->shape[0] * (int64_t)d->groups > (1ll << 24) || d->shape[0] * C > limit) return BS_ERR_UNSUPPORTED;
     for (const int64_t s : {d->x_stride, d->residual_stride, d->y_stride, d->grad_y_stride, d->grad_x_stride, d->grad_residual_stride})
@@ -48,19 +49,18 @@ void split(const bs_group_norm_desc &d, NormK &k)
 }
 
 // The same for the kernels that keep their pixels in registers; false where they do not apply: a group too wide, or an image of more chunks
-// than a work-group joins (fewer where short vectors leave little in the registers, and the chunks' sums would be many).
+// than a work-group joins.
 bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool residual, NormK &k, bool &few)
 {
-    const int full = (int)(16 / dtype_size(d.dtype));
-    if (vec != full && vec != full / 2 && vec != 1) return false;
+    const uint64_t es = dtype_size(d.dtype);
     // the smallest block of whole groups and whole vectors that has a cache line of every pixel and divides the channels
     const uint64_t unit = std::lcm((uint64_t)k.per, (uint64_t)vec), units = k.C / unit;
     uint64_t m = 1;
-    while (m < units && (units % m != 0 || unit * m * dtype_size(d.dtype) < 128)) ++m;
+    while (m < units && (units % m != 0 || unit * m * es < 128)) ++m;
     k.block = (uint32_t)(unit * m);
     k.blocks = k.C / k.block;
     const uint32_t groups = k.block / k.per, lanes = K_NORM_RESIDENT_THREADS / std::max<uint32_t>(1, k.block / (uint32_t)vec);
-    if (lanes < 8 || groups > (uint32_t)K_NORM_RESIDENT_THREADS) return false;
+    if (lanes < 1 || groups > (uint32_t)K_NORM_RESIDENT_THREADS) return false;
     const bool mixed = k.per % (uint32_t)vec != 0;
     // One chunk needs no exchange and no second launch: few pixels a lane where they are enough for that, many where they are half empty (one
     // work-group that fills its registers is slower than four that exchange: 8x512x28x28 binary16 13.4 us against 9.6).  Images of several
@@ -73,9 +73,11 @@ bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool re
         chunks[small] = ceil_div(k.P, (uint64_t)lanes * e);
         if (!small) half_empty = k.P <= (uint64_t)lanes * e / 2;
     }
-    const uint64_t most = std::min<uint64_t>(vec == full ? 128 : vec == full / 2 ? 32 : 16, (uint64_t)K_NORM_WORDS / groups);
+    // backward, the chunks' sums of a channel stay small beside its pixels: 8 bytes for at least 256 of them, or few chunks
+    const uint64_t small_sums = backward ? std::max<uint64_t>(16, k.P * es / 256) : 128;
+    const uint64_t most = std::min({(uint64_t)128, small_sums, (uint64_t)K_NORM_WORDS / groups});
     if (chunks[0] > most) return false;
-    few = chunks[1] == 1 || (!half_empty && chunks[1] <= most && (uint64_t)k.N * k.blocks * chunks[0] < 512);
+    few = chunks[1] == 1 || (!half_empty && chunks[1] <= most && (uint64_t)k.N * k.blocks * chunks[0] < K_NORM_SLOTS);
     k.chunk = (uint32_t)ceil_div(k.P, chunks[few]);
     k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
     k.groups = groups;
@@ -99,12 +101,15 @@ struct Space {
     uint64_t pairs = 0, words = 0, part = 0, bytes = 0;  // offsets, size
 };
 
-Space space(const NormK &k, bool backward, bool resident)
+// Bytes of the exchange memory that a call needs: words, and a count for every channel block of an image.
+uint64_t exchange_bytes(const NormK &k) { return ((uint64_t)k.N * k.G * 8 * k.chunks) + (uint64_t)k.N * k.blocks * 4; }
+
+Space space(const NormK &k, bool backward, bool resident, bool exchange)
 {
     Space s;
     const uint64_t pairs = (uint64_t)k.N * k.G * 8;  // forward: the statistics, where the caller does not want them; backward: the groups' sums
     s.words = aligned(pairs);
-    s.part = s.words + (resident && k.chunks > 1 ? aligned(pairs * k.chunks) : 0);
+    s.part = s.words + (resident && k.chunks > 1 && !exchange ? aligned(pairs * k.chunks) : 0);
     s.bytes = s.part + (backward ? aligned((uint64_t)k.N * k.chunks * k.C * 8) : resident ? 0 : aligned(pairs * k.chunks * k.spans));
     return s;
 }
@@ -118,12 +123,22 @@ void sizes(const bs_group_norm_desc &d, NormK &k)
     k.per = k.C / k.G;
 }
 
-// Chooses the kernels and lays out the workspace.
-bool plan(const bs_group_norm_desc &d, int vec, bool backward, bool residual, NormK &k, Space &s, bool &few)
+// Chooses the kernels and lays out the workspace.  `vec`: the vectors that channels, strides and addresses allow; made smaller where the kernels
+// that keep their pixels in registers have no instance of them.
+bool plan(const bs_group_norm_desc &d, int &vec, bool backward, bool residual, NormK &k, Space &s, bool &few)
 {
+    const int full = (int)(16 / dtype_size(d.dtype));
+    if (vec != full && vec != full / 2) vec = 1;
     const bool resident = split_resident(d, vec, backward, residual, k, few);
     if (!resident) split(d, k);
-    s = space(k, backward, resident);
+    // The exchange memory saves a launch and costs every work-group a count: worth it for two rounds of them (both directions of 5x60x37x29
+    // binary16 25.6 us by launches, 21.5 through the memory; of 64x256x56x56 bfloat16, 13 rounds, 200 and 206).
+    const bool exchange = d.exchange && exchange_bytes(k) <= d.exchange_bytes && (uint64_t)k.N * k.blocks * k.chunks <= 2 * K_NORM_SLOTS;
+    s = space(k, backward, resident, exchange);
+    if (resident && exchange) {
+        k.words = static_cast<uint64_t *>(d.exchange);
+        k.departed = reinterpret_cast<uint32_t *>(k.words + (uint64_t)k.N * k.G * k.chunks);
+    }
     return resident;
 }
 
@@ -155,11 +170,11 @@ template <size_t NI, size_t NO>
 bs_status check_overlap(const TensorBytes (&in)[NI], const TensorBytes (&out)[NO])
 {
     for (size_t i = 0; i < NO; ++i) {
-        if (!out[i].p) continue;
+        if (!out[i].p || !out[i].image_bytes) continue;
         for (const TensorBytes &t : in)
             if (t.p && tensors_overlap(out[i], t)) return BS_ERR_ALIAS;
         for (size_t j = 0; j < i; ++j)
-            if (out[j].p && tensors_overlap(out[i], out[j])) return BS_ERR_ALIAS;
+            if (out[j].p && out[j].image_bytes && tensors_overlap(out[i], out[j])) return BS_ERR_ALIAS;
     }
     return BS_OK;
 }
@@ -180,7 +195,8 @@ uint64_t bs_group_norm_workspace_bytes(const bs_group_norm_desc *desc, int32_t b
             if (k.C % (uint32_t)vec != 0) continue;
             Space s;
             bool few;
-            plan(*desc, vec, backward != 0, residual, k, s, few);
+            int used = vec;
+            plan(*desc, used, backward != 0, residual, k, s, few);
             bytes = std::max(bytes, s.bytes);
         }
     }
@@ -199,7 +215,7 @@ bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const voi
     k.r = tensor(residual, desc->residual_stride, k);
     k.y = tensor(y, desc->y_stride, k);
     const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), pairs = (uint64_t)k.N * k.G * 8;
-    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.y});
+    int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.y});
     Space s;
     bool few = false;
     const bool resident = plan(*desc, vec, false, residual != nullptr, k, s, few);
@@ -208,7 +224,7 @@ bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const voi
         if (!element_aligned(p, es)) return BS_ERR_ALIGN;
     if (!element_aligned(weight, ps) || !element_aligned(bias, ps) || !element_aligned(stats, 8) || !element_aligned(workspace, 16)) return BS_ERR_ALIGN;
     const bs_status alias = check_overlap({bytes_of(k, k.x, es), bytes_of(k, k.r, es), bytes_of(weight, k.C * ps), bytes_of(bias, k.C * ps)},
-                                          {bytes_of(k, k.y, es), bytes_of(stats, pairs), bytes_of(workspace, s.bytes)});
+                                          {bytes_of(k, k.y, es), bytes_of(stats, pairs), bytes_of(workspace, s.bytes), bytes_of(desc->exchange, desc->exchange ? desc->exchange_bytes : 0)});
     if (alias != BS_OK) return alias;
     k.weight = weight;
     k.bias = bias;
@@ -216,11 +232,11 @@ bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const voi
     k.f32_params = desc->param_dtype == BS_F32;
     k.eps = (float)desc->eps;
     char *const ws = static_cast<char *>(workspace);
-    k.words = reinterpret_cast<uint64_t *>(ws + s.words);
+    if (!k.departed) k.words = reinterpret_cast<uint64_t *>(ws + s.words);
     k.polls = polls_of(*desc);
     if (resident) {
         k.stats = stats;
-        const bs_status st = k.chunks > 1 ? launch_norm_absent(k, stream) : BS_OK;
+        const bs_status st = k.chunks > 1 && !k.departed ? launch_norm_absent(k, stream) : BS_OK;
         return st != BS_OK ? st : launch_norm_resident(k, desc->dtype, vec, few, stream);
     }
     k.stats = stats ? stats : reinterpret_cast<float *>(ws + s.pairs);
@@ -247,7 +263,7 @@ bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, 
     k.dx = tensor(grad_x, desc->grad_x_stride, k);
     k.dr = tensor(grad_residual, desc->grad_residual_stride, k);
     const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), pairs = (uint64_t)k.N * k.G * 8;
-    const int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.dy, &k.dx, &k.dr});
+    int vec = vector_of(k, desc->dtype, {&k.x, &k.r, &k.dy, &k.dx, &k.dr});
     Space s;
     bool few = false;
     const bool resident = plan(*desc, vec, true, residual != nullptr, k, s, few);
@@ -260,7 +276,7 @@ bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, 
     const bs_status alias = check_overlap({bytes_of(k, k.x, es), bytes_of(k, k.r, es), bytes_of(weight, k.C * ps), bytes_of(bias, k.C * ps),
                                            bytes_of(stats, pairs), bytes_of(k, k.dy, es)},
                                           {bytes_of(k, k.dx, es), bytes_of(k, k.dr, es), bytes_of(grad_weight, k.C * ps), bytes_of(grad_bias, k.C * ps),
-                                           bytes_of(workspace, s.bytes)});
+                                           bytes_of(workspace, s.bytes), bytes_of(desc->exchange, desc->exchange ? desc->exchange_bytes : 0)});
     if (alias != BS_OK) return alias;
     k.weight = weight;
     k.bias = bias;
@@ -273,12 +289,12 @@ bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const void *x, 
     k.stats = const_cast<float *>(stats);
     k.sums = reinterpret_cast<float *>(ws + s.pairs);
     k.part = reinterpret_cast<float *>(ws + s.part);
-    k.words = reinterpret_cast<uint64_t *>(ws + s.words);
+    if (!k.departed) k.words = reinterpret_cast<uint64_t *>(ws + s.words);
     k.polls = polls_of(*desc);
     const bool tensors = grad_x || grad_residual, params = grad_weight || grad_bias;
     if (resident) {
         if (!params) k.part = nullptr;
-        bs_status st = k.chunks > 1 && tensors ? launch_norm_absent(k, stream) : BS_OK;
+        bs_status st = k.chunks > 1 && tensors && !k.departed ? launch_norm_absent(k, stream) : BS_OK;
         if (st == BS_OK && (tensors || params)) st = launch_norm_resident_grad(k, desc->dtype, vec, few, stream);
         if (st == BS_OK && params) st = launch_norm(NORM_GRAD_PARAMS, k, desc->dtype, vec, stream);
         return st;

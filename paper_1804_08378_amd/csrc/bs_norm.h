@@ -12,6 +12,7 @@ constexpr int K_NORM_THREADS = 256;        // work-group size of the kernels tha
 constexpr int K_NORM_BLOCK_CHANNELS = 256; // channels of a work-group at most: a lane keeps one vector of them
 
 constexpr int K_NORM_RESIDENT_THREADS = 512;  // work-group size of the kernels that keep their pixels in registers
+constexpr uint64_t K_NORM_SLOTS = 512;     // of them at a time: two of each of the 256 compute units
 constexpr int K_NORM_WORDS = 2048;         // words (groups of a block x chunks) that such a work-group can join
 constexpr uint32_t K_NORM_POLLS = 4096;    // polls of a word before a work-group computes its neighbours' sums itself: some milliseconds
 
@@ -40,11 +41,12 @@ struct NormK {
     uint32_t block, groups, lanes, polls;
     uint32_t last, chunk_each, last_each, slices, slices_wide;
     uint64_t *words;
+    uint32_t *departed;  // work-groups of a block that have collected their words; nullptr: the words were cleared by a launch and stay as they are
     FastDiv by_chunks, by_blocks, by_cvb, by_cols_wide, by_per, by_vectors;  // by_vectors: channel vectors of a group
 };
 
 enum NormPass { NORM_STATS, NORM_JOIN, NORM_APPLY, NORM_GRAD_SUMS, NORM_GRAD_JOIN, NORM_GRAD_PARAMS, NORM_GRAD_APPLY };
-// Enqueue one pass; vec: elements of a lane's vector (a power of two that divides C and every stride, addresses aligned to it).
+// Enqueue one pass; vec: elements of a lane's vector, 128 or 64 bits or one element (it divides C and every stride, addresses are aligned to it).
 // Pixels that a lane keeps in registers, as many as 128 of them hold without spilling (two work-groups of a compute unit).  few: the
 // instances for small images; mixed: vectors that reach over groups, which need the statistics of every channel beside them.
 constexpr int norm_resident_pixels(int vec, bool residual, bool few, bool mixed) { return few ? 4 : mixed && vec == 8 ? (residual ? 4 : 8) : residual ? 8 : 16; }
@@ -52,9 +54,8 @@ constexpr int norm_resident_grad_pixels(int vec, int activation, bool residual, 
 {
     const bool gelu = activation == BS_ACT_GELU;
     if (vec == 8) {
-        if (residual) return gelu ? 1 : few || mixed ? 2 : 3;
-        if (gelu) return mixed ? 1 : few ? 2 : 3;
-        return few ? 2 : mixed ? 4 : activation == BS_ACT_SILU ? 5 : 6;
+        if (residual) return mixed && activation == BS_ACT_GELU ? 1 : few || mixed ? 2 : 3;
+        return few ? 2 : mixed ? 4 : activation == BS_ACT_IDENTITY || activation == BS_ACT_RELU ? 6 : 5;
     }
     if (residual) return few || (mixed && vec > 1) ? 2 : vec == 1 ? 8 : 4;
     return few ? 2 : mixed || (vec == 4 && gelu) ? 6 : 8;

@@ -387,10 +387,10 @@ void launch_act(NormPass pass, const NormK &k, hipStream_t st)
 template <int DT>
 void launch_vec(NormPass pass, const NormK &k, int vec, hipStream_t st)
 {
-    if (vec == 1) launch_act<DT, 1>(pass, k, st);
-    else if (vec == 2) launch_act<DT, 2>(pass, k, st);
-    else if (vec == 4) launch_act<DT, 4>(pass, k, st);
-    else if constexpr (DT != DT_F32) launch_act<DT, 8>(pass, k, st);
+    constexpr int FULL = DT == DT_F32 ? 4 : 8;
+    if (vec == FULL) launch_act<DT, FULL>(pass, k, st);
+    else if (vec == FULL / 2) launch_act<DT, FULL / 2>(pass, k, st);
+    else launch_act<DT, 1>(pass, k, st);
 }
 
 }  // namespace

@@ -15,15 +15,15 @@
 namespace bs {
 
 constexpr int RT = K_NORM_RESIDENT_THREADS;
-constexpr uint64_t ABSENT = ~0ull;  // what a word holds before it is published
+constexpr uint64_t ABSENT = 0;  // what a word holds before it is published: words are stored with all bits turned
 
 BS_DEV uint64_t word_of(float a, float b)
 {
-    const uint64_t w = (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a);
-    return w == ABSENT ? 0x7fc000007fc00000ull : w;  // (two NaN, whatever their bits)
+    const uint64_t w = ~((uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a));
+    return w == ABSENT ? ~0x7fc000007fc00000ull : w;  // (two NaN, whatever their bits)
 }
-BS_DEV float word_low(uint64_t w) { return __uint_as_float((uint32_t)w); }
-BS_DEV float word_high(uint64_t w) { return __uint_as_float((uint32_t)(w >> 32)); }
+BS_DEV float word_low(uint64_t w) { return __uint_as_float(~(uint32_t)w); }
+BS_DEV float word_high(uint64_t w) { return __uint_as_float(~(uint32_t)(w >> 32)); }
 
 // Where a work-group and a lane stand.
 struct Spot {
@@ -166,6 +166,23 @@ BS_DEV bool collect(const NormK &k, const Spot &s, uint64_t *words, uint32_t *mi
     }
     __syncthreads();
     return *missing == 0;
+}
+
+// Behind collect: counts the work-group out.  The last one of a block's finds that nobody looks for its words any more, and clears them (at
+// the end, off the other lanes' way).  Every work-group has published before it counts itself out, so no word comes late; a look at a word has
+// brought its value before the barrier that collect ends with, so none comes behind the count.
+BS_DEV uint32_t depart(const NormK &k, const Spot &s)
+{
+    if (!k.departed || k.chunks == 1 || threadIdx.x != 0) return 0;
+    return __hip_atomic_fetch_add(k.departed + s.n * k.blocks + s.g0 / k.groups, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+BS_DEV void clear_words(const NormK &k, const Spot &s, uint32_t before)
+{
+    if (!k.departed || k.chunks == 1 || threadIdx.x >= 64) return;
+    if ((uint32_t)__builtin_amdgcn_readfirstlane((int)before) != k.chunks - 1) return;
+    uint64_t *all = k.words + ((uint64_t)s.n * k.G + s.g0) * k.chunks;
+    for (uint32_t i = threadIdx.x; i < k.groups * k.chunks; i += 64) __hip_atomic_store(all + i, ABSENT, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) __hip_atomic_store(k.departed + s.n * k.blocks + s.g0 / k.groups, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 }  // namespace bs

@@ -132,6 +132,7 @@ __global__ __launch_bounds__(RT, 4) void norm_resident_kernel(NormK k)
         }
         x.load(k.x, k, s, own, mine);
     }
+    const uint32_t before = depart(k, s);
     // join the chunks of a group
     for (uint32_t g = threadIdx.x / 16; g < k.groups; g += RT / 16) {
         const uint64_t *w = words + g * k.chunks;
@@ -154,7 +155,6 @@ __global__ __launch_bounds__(RT, 4) void norm_resident_kernel(NormK k)
         }
     }
     __syncthreads();
-    if (!mine) return;
     x.forget();
     if constexpr (RES) r.forget();
     float m[NG];
@@ -176,6 +176,7 @@ __global__ __launch_bounds__(RT, 4) void norm_resident_kernel(NormK k)
         for (int i = 0; i < VEC; ++i) v[i] = act<DT, ACT>(__builtin_fmaf(v[i] - m[NG > 1 ? i : 0], a[i], b[i]) + add[i]);
         store_elems<DT, VEC>(dst + u * step, 0, v);
     }
+    clear_words(k, s, before);
 }
 
 __global__ __launch_bounds__(256) void norm_absent_kernel(uint64_t *words, uint32_t n)

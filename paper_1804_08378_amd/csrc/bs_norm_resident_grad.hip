@@ -157,6 +157,7 @@ __global__ __launch_bounds__(RT, 4) void norm_resident_grad_kernel(NormK k)
         }
         o.load(k, s, own, mine);
     }
+    const uint32_t before = depart(k, s);
     for (uint32_t g = threadIdx.x / 16; g < k.groups; g += RT / 16) {
         const float cells = (float)k.P * (float)k.per;
         float a = 0.0f, b = 0.0f;
@@ -172,7 +173,6 @@ __global__ __launch_bounds__(RT, 4) void norm_resident_grad_kernel(NormK k)
         }
     }
     __syncthreads();
-    if (!mine) return;
     o.x.forget();
     o.dy.forget();
     if constexpr (RES) o.r.forget();
@@ -201,6 +201,7 @@ __global__ __launch_bounds__(RT, 4) void norm_resident_grad_kernel(NormK k)
         }
         __builtin_amdgcn_sched_barrier(0);
     }
+    clear_words(k, s, before);
 }
 
 template <int DT, int VEC, int ACT, bool RES>

@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 #include <ATen/core/PythonFallbackKernel.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <c10/util/SmallVector.h>
 #include <torch/csrc/Device.h>
@@ -555,6 +556,25 @@ bool read_float(PyObject *o, double &v)
     return PyFloat_Check(o);
 }
 
+// The memory that the parts of an image hand their sums through: kept for every device and stream, zero-filled once.  (Never destroyed: the
+// process may end after the device has gone.)
+void *exchange_of(const at::Device &dev, void *stream, const at::TensorOptions &like)
+{
+    // a recorded graph may run on any stream, next to later calls on this one: it gets none, and clears its workspace by a launch
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) return nullptr;
+    static std::mutex mutex;
+    static auto &kept = *new std::map<std::pair<int, void *>, at::Tensor>();
+    const std::pair<int, void *> key{dev.index(), stream};
+    {
+        std::lock_guard<std::mutex> lock(mutex);
+        const auto it = kept.find(key);
+        if (it != kept.end()) return it->second.data_ptr();
+    }
+    const at::Tensor t = at::zeros({(int64_t)BS_GROUP_NORM_EXCHANGE_BYTES}, like.dtype(at::kByte));  // (outside the lock, as every allocation)
+    std::lock_guard<std::mutex> lock(mutex);
+    return kept.emplace(key, t).first->second.data_ptr();
+}
+
 struct NormCall {
     bs_group_norm_desc d{};
     at::Tensor x, weight, bias, residual;
@@ -593,6 +613,13 @@ struct NormCall {
         return !t.defined() || (on_gpu(t, x.device()) && t.sizes() == x.sizes() && t.scalar_type() == x.scalar_type() && (stride = pixel_stride(t)) != 0);
     }
     at::Tensor empty() const { return at::empty(x.sizes(), like.memory_format(at::MemoryFormat::ChannelsLast)); }
+    // Small images are one part and need none.
+    void exchange(void *stream)
+    {
+        if (d.shape[1] * d.shape[2] * d.shape[3] < 8192) return;
+        d.exchange = exchange_of(x.device(), stream, like);
+        d.exchange_bytes = d.exchange ? BS_GROUP_NORM_EXCHANGE_BYTES : 0;
+    }
     static void *ptr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 };
 
@@ -629,10 +656,12 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
         pybind11::gil_scoped_release no_gil;
         y = c.empty();
         if (keep) stats = at::empty({c.x.size(0), c.d.groups, 2}, c.like.dtype(at::kFloat));
+        void *const stream = c10::hip::getCurrentHIPStream(c.x.device().index()).stream();
+        c.exchange(stream);
         const uint64_t bytes = g_operators.norm_bytes(&c.d, 0);
         const at::Tensor ws = workspace_of(bytes, c.like);
         const int rc = g_operators.norm(&c.d, c.x.data_ptr(), c.ptr(c.residual), c.ptr(c.weight), c.ptr(c.bias), y.data_ptr(), static_cast<float *>(c.ptr(stats)),
-                                        c.ptr(ws), bytes, c10::hip::getCurrentHIPStream(c.x.device().index()).stream());
+                                        c.ptr(ws), bytes, stream);
         if (rc != 0) throw CallFailed(rc, "bs_group_norm");
     } catch (const CallFailed &e) {
         return failed(e);
@@ -662,11 +691,12 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         if ((wanted & 2) && c.weight.defined()) gw = at::empty({c.x.size(1)}, c.weight.options());
         if ((wanted & 4) && c.bias.defined()) gb = at::empty({c.x.size(1)}, c.bias.options());
         if ((wanted & 8) && c.residual.defined()) gr = c.empty();
+        void *const stream = c10::hip::getCurrentHIPStream(c.x.device().index()).stream();
+        c.exchange(stream);
         const uint64_t bytes = g_operators.norm_bytes(&c.d, 1);
         const at::Tensor ws = workspace_of(bytes, c.like);
         const int rc = g_operators.norm_backward(&c.d, c.x.data_ptr(), c.ptr(c.residual), c.ptr(c.weight), c.ptr(c.bias), static_cast<const float *>(st.data_ptr()),
-                                                 dy.data_ptr(), c.ptr(gx), c.ptr(gr), c.ptr(gw), c.ptr(gb), c.ptr(ws), bytes,
-                                                 c10::hip::getCurrentHIPStream(c.x.device().index()).stream());
+                                                 dy.data_ptr(), c.ptr(gx), c.ptr(gr), c.ptr(gw), c.ptr(gb), c.ptr(ws), bytes, stream);
         if (rc != 0) throw CallFailed(rc, "bs_group_norm_backward");
     } catch (const CallFailed &e) {
         return failed(e);

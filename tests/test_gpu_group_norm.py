@@ -352,3 +352,63 @@ def test_launches_one_after_the_other_share_a_workspace():
         bs.bs_group_norm(d, x.data_ptr(), 0, 0, 0, y.data_ptr(), 0, ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(ys, want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("polls", [0, -1])
+def test_exchange_memory_is_zero_again(polls, dtype):
+    """Calls through exchange memory, of several shapes one after the other, with and without waiting: the bits of calls through the workspace,
+    and nothing is left in the memory."""
+    memory = torch.zeros(bs.BS_GROUP_NORM_EXCHANGE_BYTES // 8, dtype=torch.int64, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    for i, shape in enumerate([(2, 64, 60, 60, 32), (5, 256, 56, 56, 8), (1, 48, 100, 90, 4), (3, 64, 112, 112, 32), (2, 64, 60, 60, 32)]):
+        x, weight, bias, res, dy = tensors(shape, dtype, i, True)
+        d = F._norm_operands(x, shape[4], weight, bias, res, "silu", 1e-5, dy)[0]
+        results = []
+        for exchange in (0, memory.data_ptr()):
+            d.exchange, d.exchange_bytes, d.wait_polls = exchange, 8 * memory.numel() if exchange else 0, polls if exchange else 0
+            y, gx, gr = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+            st, gw, gb = torch.empty(shape[0], shape[4], 2, device="cuda"), torch.empty_like(weight), torch.empty_like(bias)
+            size = max(bs.bs_group_norm_workspace_bytes(d, b) for b in (False, True))
+            ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+            bs.bs_group_norm(d, x.data_ptr(), res.data_ptr(), weight.data_ptr(), bias.data_ptr(), y.data_ptr(), st.data_ptr(), ws.data_ptr(), size, stream)
+            bs.bs_group_norm_backward(d, x.data_ptr(), res.data_ptr(), weight.data_ptr(), bias.data_ptr(), st.data_ptr(), dy.data_ptr(), gx.data_ptr(),
+                                      gr.data_ptr(), gw.data_ptr(), gb.data_ptr(), ws.data_ptr(), size, stream)
+            torch.cuda.synchronize()
+            assert not memory.any()
+            results.append((y, st, gx, gr, gw, gb))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_graph_replays():
+    """A recorded forward and backward pass, replayed between eager calls on the same stream, each replay against the eager result."""
+    shape = (4, 128, 40, 40, 32)
+    x, weight, bias, res, dy = tensors(shape, "bf16", 2, True)
+    args = (shape[4], weight, bias, res, "gelu")
+
+    def step():
+        y, stats = F.group_norm_forward(x, *args)
+        return (y, *F.group_norm_backward(x, stats, dy, *args))
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step()
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(i)).to(x.dtype))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), i
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(2, 4096, 5, 5, 1), (1, 1536, 40, 30, 2), (2, 168, 62, 55, 8), (1, 2050, 9, 8, 1), (2, 22, 30, 31, 2), (1, 6000, 3, 4, 3), (3, 512, 9, 9, 512),
+                                   (1, 24, 260, 250, 24)])
+def test_wide_groups_and_many_groups(shape, dtype):
+    """Groups wider than a work-group's lanes, groups of one channel, vectors that reach over groups, channels that divide by two only."""
+    check(shape, dtype, "silu", True, seed=8)
+    check(shape, dtype, "gelu", False, seed=9)
