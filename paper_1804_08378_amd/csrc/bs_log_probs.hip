@@ -236,6 +236,7 @@ BS_DEV void put_ranked(uint32_t k, const Selection<T> &sel, PUT put)
     for (uint32_t i = threadIdx.x; i < n; i += T) {
         const uint64_t key = sel.list[i];
         uint32_t rank = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) rank += sel.list[j] > key;
         if (rank < k) put(rank, key);
     }

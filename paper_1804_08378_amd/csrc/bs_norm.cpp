@@ -69,7 +69,7 @@ bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool re
     uint64_t chunks[2];
     bool half_empty = false;
     for (const bool small : {false, true}) {
-        const int e = backward ? norm_resident_grad_pixels(vec, d.activation, in_gradient, small, mixed) : norm_resident_pixels(vec, residual, small, mixed);
+        const int e = backward ? norm_resident_grad_pixels(vec, es == 4, d.activation, in_gradient, small, mixed) : norm_resident_pixels(vec, es == 4, residual, small, mixed);
         chunks[small] = ceil_div(k.P, (uint64_t)lanes * e);
         if (!small) half_empty = k.P <= (uint64_t)lanes * e / 2;
     }
@@ -129,6 +129,7 @@ bool plan(const bs_group_norm_desc &d, int &vec, bool backward, bool residual, N
 {
     const int full = (int)(16 / dtype_size(d.dtype));
     if (vec != full && vec != full / 2) vec = 1;
+    if (vec == full && (backward || k.per % (uint32_t)full != 0)) vec = full / 2;
     const bool resident = split_resident(d, vec, backward, residual, k, few);
     if (!resident) split(d, k);
     // The exchange memory saves a launch and costs every work-group a count: worth it for two rounds of them (both directions of 5x60x37x29

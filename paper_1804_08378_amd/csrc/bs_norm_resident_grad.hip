@@ -208,12 +208,12 @@ template <int DT, int VEC, int ACT, bool RES>
 void launch(const NormK &k, bool few, hipStream_t st)
 {
     const dim3 grid(k.N * k.blocks * k.chunks), block(RT);
-    constexpr int MANY = norm_resident_grad_pixels(VEC, ACT, RES, false, false), FEW = norm_resident_grad_pixels(VEC, ACT, RES, true, false);
+    constexpr int MANY = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, false, false), FEW = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, true, false);
     if (VEC == 1 || k.per % VEC == 0) {
         if (few) norm_resident_grad_kernel<DT, VEC, FEW, ACT, RES, 1><<<grid, block, 0, st>>>(k);
         else norm_resident_grad_kernel<DT, VEC, MANY, ACT, RES, 1><<<grid, block, 0, st>>>(k);
     } else if constexpr (VEC > 1) {
-        constexpr int MIXED = norm_resident_grad_pixels(VEC, ACT, RES, false, true), MIXED_FEW = norm_resident_grad_pixels(VEC, ACT, RES, true, true);
+        constexpr int MIXED = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, false, true), MIXED_FEW = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, true, true);
         if (few) norm_resident_grad_kernel<DT, VEC, MIXED_FEW, ACT, RES, VEC><<<grid, block, 0, st>>>(k);
         else norm_resident_grad_kernel<DT, VEC, MIXED, ACT, RES, VEC><<<grid, block, 0, st>>>(k);
     }
