@@ -523,7 +523,7 @@ typedef struct bs_group_norm_desc {
                                 too small for the call: the workspace serves, cleared by a launch of its own                              */
     uint64_t exchange_bytes; /* its size; BS_GROUP_NORM_EXCHANGE_BYTES is enough for nearly every tensor */
     int32_t wait_polls; /* how often a work-group looks for the sums of an image's other parts before it computes them itself:
-                           0 = default (some milliseconds), -1 = never looks; changes no result                              */
+                           0 = default (a millisecond), -1 = never looks; changes no result                              */
     int32_t reserved;
 } bs_group_norm_desc;
 

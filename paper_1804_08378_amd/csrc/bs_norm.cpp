@@ -53,38 +53,51 @@ void split(const bs_group_norm_desc &d, NormK &k)
 bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool residual, NormK &k, bool &few)
 {
     const uint64_t es = dtype_size(d.dtype);
-    // the smallest block of whole groups and whole vectors that has a cache line of every pixel and divides the channels
+    const bool mixed = k.per % (uint32_t)vec != 0, in_gradient = residual && d.activation != BS_ACT_IDENTITY;
+    auto pixels = [&](bool small) {
+        return (uint64_t)(backward ? norm_resident_grad_pixels(vec, es == 4, d.activation, in_gradient, small, mixed)
+                                   : norm_resident_pixels(vec, es == 4, residual, small, mixed));
+    };
+    // backward, the chunks' sums of a channel stay small beside its pixels: 8 bytes for at least 256 of them, or few chunks
+    const uint64_t small_sums = backward ? std::max<uint64_t>(16, k.P * es / 256) : 128;
+    // A block: whole groups and whole vectors, a divisor of the channels, at least a cache line of every pixel.  Blocks that begin inside cache
+    // lines share them with their neighbours, and read them twice: in tensors of 16 MiB on the smallest block that does so for a sixth of its
+    // lines at most (9x288x83x83 binary16 forward 47.7 -> 25.7 us, 7x336x143x143 both directions 183 -> 157), in smaller ones the smallest of all
+    // (8x640x32x32 binary16 forward 12.7 us, 18.3 in such blocks, whose chunks are few pixels).
     const uint64_t unit = std::lcm((uint64_t)k.per, (uint64_t)vec), units = k.C / unit;
-    uint64_t m = 1;
-    while (m < units && (units % m != 0 || unit * m * es < 128)) ++m;
-    k.block = (uint32_t)(unit * m);
+    uint64_t most = 0, lanes = 0, groups = 0;
+    bool found = false;
+    const bool large = (uint64_t)k.N * k.P * k.C * es >= (16 << 20);
+    for (const bool whole_lines : {true, false}) {
+        if (whole_lines && !large) continue;
+        for (uint64_t m = 1; m <= units && !found; ++m) {
+            const uint64_t bytes = unit * m * es;
+            if (units % m != 0 || (m < units && bytes < 128)) continue;
+            const bool apart = m == units || (bytes % 128 == 0 && k.C * es % 128 == 0);
+            if (whole_lines && !apart && bytes < 6 * 112) continue;
+            lanes = K_NORM_RESIDENT_THREADS / std::max<uint64_t>(1, unit * m / (uint64_t)vec);
+            groups = unit * m / k.per;
+            if (lanes < (whole_lines ? 4 : 1) || groups > (uint64_t)K_NORM_RESIDENT_THREADS) break;
+            most = std::min({(uint64_t)128, small_sums, (uint64_t)K_NORM_WORDS / groups});
+            found = ceil_div(k.P, lanes * pixels(false)) <= most;
+            if (found) k.block = (uint32_t)(unit * m);
+        }
+    }
+    if (!found) return false;
     k.blocks = k.C / k.block;
-    const uint32_t groups = k.block / k.per, lanes = K_NORM_RESIDENT_THREADS / std::max<uint32_t>(1, k.block / (uint32_t)vec);
-    if (lanes < 1 || groups > (uint32_t)K_NORM_RESIDENT_THREADS) return false;
-    const bool mixed = k.per % (uint32_t)vec != 0;
     // One chunk needs no exchange and no second launch: few pixels a lane where they are enough for that, many where they are half empty (one
     // work-group that fills its registers is slower than four that exchange: 8x512x28x28 binary16 13.4 us against 9.6).  Images of several
     // chunks: many pixels a lane, or few where that leaves compute units without work.
-    const bool in_gradient = residual && d.activation != BS_ACT_IDENTITY;
-    uint64_t chunks[2];
-    bool half_empty = false;
-    for (const bool small : {false, true}) {
-        const int e = backward ? norm_resident_grad_pixels(vec, es == 4, d.activation, in_gradient, small, mixed) : norm_resident_pixels(vec, es == 4, residual, small, mixed);
-        chunks[small] = ceil_div(k.P, (uint64_t)lanes * e);
-        if (!small) half_empty = k.P <= (uint64_t)lanes * e / 2;
-    }
-    // backward, the chunks' sums of a channel stay small beside its pixels: 8 bytes for at least 256 of them, or few chunks
-    const uint64_t small_sums = backward ? std::max<uint64_t>(16, k.P * es / 256) : 128;
-    const uint64_t most = std::min({(uint64_t)128, small_sums, (uint64_t)K_NORM_WORDS / groups});
-    if (chunks[0] > most) return false;
+    const uint64_t chunks[2] = {ceil_div(k.P, lanes * pixels(false)), ceil_div(k.P, lanes * pixels(true))};
+    const bool half_empty = k.P <= lanes * pixels(false) / 2;
     few = chunks[1] == 1 || (!half_empty && chunks[1] <= most && (uint64_t)k.N * k.blocks * chunks[0] < K_NORM_SLOTS);
     k.chunk = (uint32_t)ceil_div(k.P, chunks[few]);
     k.chunks = (uint32_t)ceil_div(k.P, k.chunk);
-    k.groups = groups;
-    k.lanes = lanes;
+    k.groups = (uint32_t)groups;
+    k.lanes = (uint32_t)lanes;
     k.last = k.P - (k.chunks - 1) * k.chunk;
-    k.chunk_each = k.chunk / lanes;
-    k.last_each = k.last / lanes;
+    k.chunk_each = k.chunk / k.lanes;
+    k.last_each = k.last / k.lanes;
     const uint32_t cvb = k.block / (uint32_t)vec, root = (uint32_t)std::ceil(std::sqrt((double)lanes));
     k.slices = std::max<uint32_t>(1, std::min(root, K_NORM_RESIDENT_THREADS / cvb));
     k.slices_wide = std::max<uint32_t>(1, std::min(root, K_NORM_RESIDENT_THREADS / k.block));

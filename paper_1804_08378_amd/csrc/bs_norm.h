@@ -14,7 +14,7 @@ constexpr int K_NORM_BLOCK_CHANNELS = 256; // channels of a work-group at most: 
 constexpr int K_NORM_RESIDENT_THREADS = 512;  // work-group size of the kernels that keep their pixels in registers
 constexpr uint64_t K_NORM_SLOTS = 512;     // of them at a time: two of each of the 256 compute units
 constexpr int K_NORM_WORDS = 2048;         // words (groups of a block x chunks) that such a work-group can join
-constexpr uint32_t K_NORM_POLLS = 4096;    // polls of a word before a work-group computes its neighbours' sums itself: some milliseconds
+constexpr uint32_t K_NORM_POLLS = 1024;    // polls of a word before a work-group computes its neighbours' sums itself: about a millisecond
 
 // One tensor: N images of P pixels, `stride` elements from a pixel to the next (C where dense).
 struct NormTensor {

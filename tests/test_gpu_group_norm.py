@@ -412,3 +412,11 @@ def test_wide_groups_and_many_groups(shape, dtype):
     """Groups wider than a work-group's lanes, groups of one channel, vectors that reach over groups, channels that divide by two only."""
     check(shape, dtype, "silu", True, seed=8)
     check(shape, dtype, "gelu", False, seed=9)
+
+
+@pytest.mark.parametrize("shape,dtype", [((9, 288, 61, 63, 32), "f16"), ((3, 336, 99, 101, 12), "bf16"), ((5, 1216, 31, 29, 32), "f32"), ((40, 30, 90, 91, 6), "bf16"),
+                                         ((6, 95, 170, 90, 5), "f32")])
+def test_large_tensors_of_odd_groups(shape, dtype):
+    """Blocks of channels that begin inside cache lines."""
+    check(shape, dtype, "silu", True, seed=10)
+    check(shape, dtype, "relu", False, seed=11)
