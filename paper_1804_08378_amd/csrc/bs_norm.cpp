@@ -55,8 +55,8 @@ bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool re
     const uint64_t es = dtype_size(d.dtype);
     const bool mixed = k.per % (uint32_t)vec != 0, in_gradient = residual && d.activation != BS_ACT_IDENTITY;
     auto pixels = [&](bool small) {
-        return (uint64_t)(backward ? norm_resident_grad_pixels(vec, es == 4, d.activation, in_gradient, small, mixed)
-                                   : norm_resident_pixels(vec, es == 4, residual, small, mixed));
+        const int bytes = vec * (int)es;
+        return (uint64_t)(backward ? norm_resident_grad_pixels(bytes, in_gradient, small, mixed) : norm_resident_pixels(bytes, residual, small));
     };
     // backward, the chunks' sums of a channel stay small beside its pixels: 8 bytes for at least 256 of them, or few chunks
     const uint64_t small_sums = backward ? std::max<uint64_t>(16, k.P * es / 256) : 128;
@@ -136,8 +136,8 @@ void sizes(const bs_group_norm_desc &d, NormK &k)
     k.per = k.C / k.G;
 }
 
-// Chooses the kernels and lays out the workspace.  `vec`: the vectors that channels, strides and addresses allow; made smaller where the kernels
-// that keep their pixels in registers have no instance of them.
+// Chooses the kernels and lays out the workspace.  `vec`: the vectors that channels, strides and addresses allow; made smaller where there is no
+// instance of them (norm_resident_pixels says why).
 bool plan(const bs_group_norm_desc &d, int &vec, bool backward, bool residual, NormK &k, Space &s, bool &few)
 {
     const int full = (int)(16 / dtype_size(d.dtype));

@@ -46,30 +46,22 @@ struct NormK {
 };
 
 enum NormPass { NORM_STATS, NORM_JOIN, NORM_APPLY, NORM_GRAD_SUMS, NORM_GRAD_JOIN, NORM_GRAD_PARAMS, NORM_GRAD_APPLY };
-// Enqueue one pass; vec: elements of a lane's vector, 128 or 64 bits or one element (it divides C and every stride, addresses are aligned to it).
-// Pixels that a lane keeps in registers, as many as 128 of them hold without spilling (two work-groups of a compute unit).  few: the
-// instances for small images; mixed: vectors that reach over groups, which need the statistics of every channel beside them; wide: 32-bit
-// elements.  Parameters, sums and temporaries take registers for every channel of a vector, so short vectors leave more of them for pixels.
-constexpr int norm_resident_pixels(int vec, bool wide, bool residual, bool few, bool mixed)
+// Enqueue one pass; vec: elements of a lane's vector, 128 (forward only) or 64 bits or one element (it divides C and every stride, addresses are
+// aligned to it).
+// Pixels that a lane keeps in registers, as many as 128 of them hold without spilling (two work-groups of a compute unit).  bytes: of a lane's
+// vector; few: the instances for small images; mixed: vectors that reach over groups, which need the statistics of every channel beside them.
+// Parameters, sums and temporaries take registers for every channel of a vector, so that vectors of 64 bits leave more of them for pixels: backward
+// there are no longer ones, forward none that reach over groups.
+constexpr int norm_resident_pixels(int bytes, bool residual, bool few)
 {
-    const int bytes = vec * (wide ? 4 : 2);
     if (few) return 4;
-    if (bytes == 8) return residual ? 16 : 32;
-    if (vec == 8 && mixed) return residual ? 4 : 8;
-    return residual ? 8 : 16;
+    return (bytes == 8 ? 32 : 16) / (residual ? 2 : 1);
 }
-constexpr int norm_resident_grad_pixels(int vec, bool wide, int activation, bool residual, bool few, bool mixed)
+constexpr int norm_resident_grad_pixels(int bytes, bool residual, bool few, bool mixed)
 {
-    const int bytes = vec * (wide ? 4 : 2);
-    const bool gelu = activation == BS_ACT_GELU, plain = activation == BS_ACT_IDENTITY || activation == BS_ACT_RELU;
-    if (few) return vec == 8 && mixed && residual && gelu ? 1 : 2;
-    if (bytes == 8) return residual ? (mixed ? 8 : 10) : mixed ? 12 : 16;
-    if (vec == 8) {
-        if (residual) return mixed ? (gelu ? 1 : 2) : 3;
-        return mixed ? 4 : plain ? 6 : 5;
-    }
-    if (residual) return mixed ? 2 : vec == 1 ? 8 : 4;
-    return mixed || (vec == 4 && gelu) ? 6 : 8;
+    if (few) return 2;
+    if (bytes != 8) return 8;
+    return residual ? (mixed ? 8 : 10) : mixed ? 12 : 16;
 }
 bs_status launch_norm_absent(const NormK &k, void *stream);
 bs_status launch_norm_resident(const NormK &k, int32_t dtype, int vec, bool few, void *stream);

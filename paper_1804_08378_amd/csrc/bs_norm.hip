@@ -352,31 +352,27 @@ bs_status checked()
 template <int DT, int VEC, int ACT>
 void launch(NormPass pass, const NormK &k, hipStream_t st)
 {
+    constexpr bool FULL = VEC * (DT == DT_F32 ? 4 : 2) == 16;  // (not backward)
     const dim3 grid(k.N * k.chunks * k.blocks), block(T);
     switch (pass) {
     case NORM_STATS:
         if constexpr (ACT == 0) norm_stats_kernel<DT, VEC><<<grid, block, 0, st>>>(k);
         break;
-    case NORM_JOIN:
-        if constexpr (ACT == 0 && VEC == 1 && DT == 0) norm_join_kernel<<<dim3((k.N * k.G + T - 1) / T), block, 0, st>>>(k);
-        break;
     case NORM_APPLY: norm_apply_kernel<DT, VEC, ACT><<<grid, block, 0, st>>>(k); break;
-    case NORM_GRAD_SUMS: norm_grad_sums_kernel<DT, VEC, ACT><<<grid, block, 0, st>>>(k); break;
-    case NORM_GRAD_JOIN:
-        if constexpr (ACT == 0 && VEC == 1) norm_grad_join_kernel<DT><<<dim3(k.N * k.G), dim3(64), 0, st>>>(k);
+    case NORM_GRAD_SUMS:
+        if constexpr (!FULL) norm_grad_sums_kernel<DT, VEC, ACT><<<grid, block, 0, st>>>(k);
         break;
-    case NORM_GRAD_PARAMS:
-        if constexpr (ACT == 0 && VEC == 1) norm_grad_params_kernel<DT><<<dim3((k.C + 3) / 4), dim3(PT), 0, st>>>(k);
+    case NORM_GRAD_APPLY:
+        if constexpr (!FULL) norm_grad_apply_kernel<DT, VEC, ACT><<<grid, block, 0, st>>>(k);
         break;
-    case NORM_GRAD_APPLY: norm_grad_apply_kernel<DT, VEC, ACT><<<grid, block, 0, st>>>(k); break;
+    default: break;
     }
 }
 
 template <int DT, int VEC>
 void launch_act(NormPass pass, const NormK &k, hipStream_t st)
 {
-    const bool plain = pass == NORM_STATS || pass == NORM_JOIN || pass == NORM_GRAD_JOIN || pass == NORM_GRAD_PARAMS;
-    switch (plain ? BS_ACT_IDENTITY : (int)k.activation) {
+    switch (pass == NORM_STATS ? BS_ACT_IDENTITY : (int)k.activation) {
     case BS_ACT_IDENTITY: launch<DT, VEC, BS_ACT_IDENTITY>(pass, k, st); break;
     case BS_ACT_RELU: launch<DT, VEC, BS_ACT_RELU>(pass, k, st); break;
     case BS_ACT_SILU: launch<DT, VEC, BS_ACT_SILU>(pass, k, st); break;
@@ -385,10 +381,12 @@ void launch_act(NormPass pass, const NormK &k, hipStream_t st)
 }
 
 template <int DT>
-void launch_vec(NormPass pass, const NormK &k, int vec, hipStream_t st)
+void launch_type(NormPass pass, const NormK &k, int vec, hipStream_t st)
 {
     constexpr int FULL = DT == DT_F32 ? 4 : 8;
-    if (vec == FULL) launch_act<DT, FULL>(pass, k, st);
+    if (pass == NORM_GRAD_JOIN) norm_grad_join_kernel<DT><<<dim3(k.N * k.G), dim3(64), 0, st>>>(k);
+    else if (pass == NORM_GRAD_PARAMS) norm_grad_params_kernel<DT><<<dim3((k.C + 3) / 4), dim3(PT), 0, st>>>(k);
+    else if (vec == FULL) launch_act<DT, FULL>(pass, k, st);
     else if (vec == FULL / 2) launch_act<DT, FULL / 2>(pass, k, st);
     else launch_act<DT, 1>(pass, k, st);
 }
@@ -398,13 +396,10 @@ void launch_vec(NormPass pass, const NormK &k, int vec, hipStream_t st)
 bs_status launch_norm(NormPass pass, const NormK &k, int32_t dtype, int vec, void *stream)
 {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (pass == NORM_JOIN) launch_vec<DT_F32>(pass, k, 1, st);
-    else if (pass == NORM_GRAD_JOIN || pass == NORM_GRAD_PARAMS) vec = 1;
-    if (pass != NORM_JOIN) {
-        if (dtype == BS_F32) launch_vec<DT_F32>(pass, k, vec, st);
-        else if (dtype == BS_BF16) launch_vec<DT_BF16>(pass, k, vec, st);
-        else launch_vec<DT_F16>(pass, k, vec, st);
-    }
+    if (pass == NORM_JOIN) norm_join_kernel<<<dim3((k.N * k.G + T - 1) / T), dim3(T), 0, st>>>(k);
+    else if (dtype == BS_F32) launch_type<DT_F32>(pass, k, vec, st);
+    else if (dtype == BS_BF16) launch_type<DT_BF16>(pass, k, vec, st);
+    else launch_type<DT_F16>(pass, k, vec, st);
     return checked();
 }
 

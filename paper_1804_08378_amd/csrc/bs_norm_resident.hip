@@ -200,11 +200,9 @@ void launch(const NormK &k, hipStream_t st)
 template <int DT, int VEC, bool RES>
 void launch_res(const NormK &k, bool few, hipStream_t st)
 {
-    constexpr bool WIDE = DT == DT_F32;
-    constexpr int MANY = norm_resident_pixels(VEC, WIDE, RES, false, false), MIXED = norm_resident_pixels(VEC, WIDE, RES, false, true),
-                  FEW = norm_resident_pixels(VEC, WIDE, RES, true, false);
-    if (VEC == 1 || k.per % VEC == 0) few ? launch<DT, VEC, FEW, RES, 1>(k, st) : launch<DT, VEC, MANY, RES, 1>(k, st);
-    else if constexpr (VEC > 1) few ? launch<DT, VEC, FEW, RES, VEC>(k, st) : launch<DT, VEC, MIXED, RES, VEC>(k, st);
+    constexpr int BYTES = VEC * (DT == DT_F32 ? 4 : 2), MANY = norm_resident_pixels(BYTES, RES, false), FEW = norm_resident_pixels(BYTES, RES, true);
+    if (VEC == 1 || BYTES == 16 || k.per % VEC == 0) few ? launch<DT, VEC, FEW, RES, 1>(k, st) : launch<DT, VEC, MANY, RES, 1>(k, st);
+    else if constexpr (BYTES == 8) few ? launch<DT, VEC, FEW, RES, VEC>(k, st) : launch<DT, VEC, MANY, RES, VEC>(k, st);
 }
 
 template <int DT, int VEC>

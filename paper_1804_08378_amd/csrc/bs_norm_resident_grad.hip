@@ -208,13 +208,13 @@ template <int DT, int VEC, int ACT, bool RES>
 void launch(const NormK &k, bool few, hipStream_t st)
 {
     const dim3 grid(k.N * k.blocks * k.chunks), block(RT);
-    constexpr int MANY = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, false, false), FEW = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, true, false);
+    constexpr int BYTES = VEC * (DT == DT_F32 ? 4 : 2), MANY = norm_resident_grad_pixels(BYTES, RES, false, false), FEW = norm_resident_grad_pixels(BYTES, RES, true, false);
     if (VEC == 1 || k.per % VEC == 0) {
         if (few) norm_resident_grad_kernel<DT, VEC, FEW, ACT, RES, 1><<<grid, block, 0, st>>>(k);
         else norm_resident_grad_kernel<DT, VEC, MANY, ACT, RES, 1><<<grid, block, 0, st>>>(k);
     } else if constexpr (VEC > 1) {
-        constexpr int MIXED = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, false, true), MIXED_FEW = norm_resident_grad_pixels(VEC, DT == DT_F32, ACT, RES, true, true);
-        if (few) norm_resident_grad_kernel<DT, VEC, MIXED_FEW, ACT, RES, VEC><<<grid, block, 0, st>>>(k);
+        constexpr int MIXED = norm_resident_grad_pixels(BYTES, RES, false, true);
+        if (few) norm_resident_grad_kernel<DT, VEC, FEW, ACT, RES, VEC><<<grid, block, 0, st>>>(k);
         else norm_resident_grad_kernel<DT, VEC, MIXED, ACT, RES, VEC><<<grid, block, 0, st>>>(k);
     }
 }
@@ -234,9 +234,8 @@ void launch_act(const NormK &k, bool few, hipStream_t st)
 template <int DT>
 void launch_vec(const NormK &k, int vec, bool few, hipStream_t st)
 {
-    constexpr int FULL = DT == DT_F32 ? 4 : 8;
-    if (vec == FULL) launch_act<DT, FULL>(k, few, st);
-    else if (vec == FULL / 2) launch_act<DT, FULL / 2>(k, few, st);
+    constexpr int HALF = DT == DT_F32 ? 2 : 4;
+    if (vec == HALF) launch_act<DT, HALF>(k, few, st);
     else launch_act<DT, 1>(k, few, st);
 }
 

@@ -420,3 +420,21 @@ def test_large_tensors_of_odd_groups(shape, dtype):
     """Blocks of channels that begin inside cache lines."""
     check(shape, dtype, "silu", True, seed=10)
     check(shape, dtype, "relu", False, seed=11)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 16, 700, 821, 4), (2, 7, 620, 401, 7), (1, 1030, 120, 121, 2), (1, 12, 500, 1001, 1), (1, 64, 640, 641, 32)])
+def test_images_that_do_not_fit_the_registers(shape, dtype):
+    """Images of more parts than a work-group joins: statistics first, then the tensor once more.  (Chains of pixels are up to four times as long.)"""
+    print(f"[group norm] {shape} {dtype}", flush=True)
+    x, weight, bias, res, dy = tensors(shape, dtype, 12, True)
+    for residual, name in ((res, "silu"), (None, "gelu")):
+        args = (shape[4], weight, bias, residual, name)
+        ref = Reference(x, shape[4], weight, bias, residual, name, 1e-5)
+        y, stats = F.group_norm_forward(x, *args)
+        close(y, ref.y, 4 * 1.13 * ref.z_off + 2e-6 * ref.y.abs() + 1e-7, dtype, "y")
+        got = F.group_norm_backward(x, stats, dy, *args)
+        for g, (want, off), label in zip(got, ref.backward(dy), ("grad_x", "grad_weight", "grad_bias", "grad_residual")):
+            if g is not None:
+                close(g, want, 4 * off, "f32" if label in ("grad_weight", "grad_bias") else dtype, label)
+        assert all(a is None or torch.equal(a, b) for a, b in zip(got, F.group_norm_backward(x, stats, dy, *args)))
