@@ -539,7 +539,8 @@ BS_API uint64_t bs_group_norm_workspace_bytes(const bs_group_norm_desc *desc, in
  *   stats         device, N * groups pairs of floats (mean, 1 / sqrt(var + eps)), which the backward pass needs; NULL: not wanted
  *   workspace     device, 16-byte aligned, >= bs_group_norm_workspace_bytes(desc, 0)
  * Errors: BS_ERR_NULL, BS_ERR_SHAPE (dimension < 1, stride below C), BS_ERR_PARAM (groups, eps), BS_ERR_UNSUPPORTED (type, activation;
- *         an image of 2^31 elements, 2^24 groups of all images), BS_ERR_ALIGN, BS_ERR_WORKSPACE, BS_ERR_ALIAS, BS_ERR_HIP.
+ *         an image of 2^31 elements, over 2^22 images, 2^24 groups of all
+ *         images, 2^31 channels of all images), BS_ERR_ALIGN, BS_ERR_WORKSPACE, BS_ERR_ALIAS, BS_ERR_HIP.
  */
 BS_API bs_status bs_group_norm(const bs_group_norm_desc *desc, const void *x, const void *residual, const void *weight, const void *bias,
                                void *y, float *stats, void *workspace, uint64_t workspace_bytes, void *stream);

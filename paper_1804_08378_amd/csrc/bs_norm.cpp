@@ -29,7 +29,7 @@ bs_status check_desc(const bs_group_norm_desc *d)
     if ((double)d->shape[1] * (double)d->shape[2] * (double)d->shape[3] > (double)limit) return BS_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(d->exchange) % 8 != 0) return BS_ERR_ALIGN;
     // grids are counted in 32 bits: images, groups
-    if (d->shape[0] * (int64_t)d->groups > (1ll << 24) || d->shape[0] * C > limit) return BS_ERR_UNSUPPORTED;
+    if (d->shape[0] > (1ll << 22) || d->shape[0] * (int64_t)d->groups > (1ll << 24) || d->shape[0] * C > limit) return BS_ERR_UNSUPPORTED;
     for (const int64_t s : {d->x_stride, d->residual_stride, d->y_stride, d->grad_y_stride, d->grad_x_stride, d->grad_residual_stride})
         if (s != 0 && (s < C || s > limit)) return BS_ERR_SHAPE;
     return BS_OK;
@@ -79,7 +79,8 @@ bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool re
             groups = unit * m / k.per;
             if (lanes < (whole_lines ? 4 : 1) || groups > (uint64_t)K_NORM_RESIDENT_THREADS) break;
             most = std::min({(uint64_t)128, small_sums, (uint64_t)K_NORM_WORDS / groups});
-            found = ceil_div(k.P, lanes * pixels(false)) <= most;
+            const uint64_t chunks = ceil_div(k.P, lanes * pixels(false));
+            found = chunks <= most && (uint64_t)k.N * (units / m) * chunks < (1ull << 23);  // (the launch's lanes are counted in 32 bits)
             if (found) k.block = (uint32_t)(unit * m);
         }
     }

@@ -1,4 +1,5 @@
-// Argument blocks of the group-normalisation kernels (bs_norm.hip), shared with the host code that fills them (bs_norm.cpp).
+// Argument block and launches of the group-normalisation kernels (bs_norm.hip, bs_norm_resident.hip, bs_norm_resident_grad.hip), shared with the
+// host code that fills and calls them (bs_norm.cpp).
 #pragma once
 
 #include <cstdint>
@@ -48,6 +49,8 @@ struct NormK {
 enum NormPass { NORM_STATS, NORM_JOIN, NORM_APPLY, NORM_GRAD_SUMS, NORM_GRAD_JOIN, NORM_GRAD_PARAMS, NORM_GRAD_APPLY };
 // Enqueue one pass; vec: elements of a lane's vector, 128 (forward only) or 64 bits or one element (it divides C and every stride, addresses are
 // aligned to it).
+bs_status launch_norm(NormPass pass, const NormK &k, int32_t dtype, int vec, void *stream);
+
 // Pixels that a lane keeps in registers, as many as 128 of them hold without spilling (two work-groups of a compute unit).  bytes: of a lane's
 // vector; few: the instances for small images; mixed: vectors that reach over groups, which need the statistics of every channel beside them.
 // Parameters, sums and temporaries take registers for every channel of a vector, so that vectors of 64 bits leave more of them for pixels: backward
@@ -66,6 +69,5 @@ constexpr int norm_resident_grad_pixels(int bytes, bool residual, bool few, bool
 bs_status launch_norm_absent(const NormK &k, void *stream);
 bs_status launch_norm_resident(const NormK &k, int32_t dtype, int vec, bool few, void *stream);
 bs_status launch_norm_resident_grad(const NormK &k, int32_t dtype, int vec, bool few, void *stream);
-bs_status launch_norm(NormPass pass, const NormK &k, int32_t dtype, int vec, void *stream);
 
 }  // namespace bs

@@ -86,6 +86,14 @@ def test_group_norm_workspaces_stay_small(shape, groups):
         assert 0 < n <= max(4 << 20, tensor // 16 + 16 * shape[0] * max(groups, shape[1])), (n, tensor)
 
 
+def test_group_norm_takes_many_small_images():
+    """Launches count lanes in 32 bits: channel blocks grow where the images alone are millions."""
+    for shape, groups in (((1 << 20, 1024, 1, 1), 16), ((1 << 22, 256, 1, 1), 4), ((1 << 22, 511, 1, 1), 1), ((1 << 21, 64, 2, 2), 8)):
+        for dtype in (bs.BS_F32, bs.BS_F16):
+            assert bs.bs_group_norm_workspace_bytes(norm_desc(shape, groups, dtype), False) > 0
+    assert forward(norm_desc(((1 << 22) + 1, 8, 1, 1), 1)) == UNSUPPORTED
+
+
 def head(d, x=X, t=Y, lp=S, e=WS, lse=DY, tl=0, ti=0, ws=0, n=0):
     return status(bs.bs_log_probs, d, x, t, lp, e, lse, tl, ti, ws, n, 0)
 
