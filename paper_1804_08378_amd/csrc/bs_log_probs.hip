@@ -243,30 +243,27 @@ BS_DEV void put_ranked(uint32_t k, const Selection<T> &sel, PUT put)
     for (uint32_t i = n + threadIdx.x; i < k; i += T) put(i, 0);
 }
 
-// The same from any numbers, one after the other: every round finds the best below the last.  For rows with NaN or infinity, and where too
-// many candidates pass the bound.
-template <int T, typename GET, typename PUT>
-BS_DEV void put_by_rounds(uint32_t k, uint32_t n, Selection<T> &sel, GET get, PUT put)
+// As long as more than the list holds were offered, the k-th best of those in the list is the bound of the next scan: every scan leaves out
+// LIST - k of them or more, and of candidates in any mixed order 15 of 16.  Periodic rows, whose best classes belong to few lanes, come
+// here, and masked or equal classes where they are most of a row (400 x 128256 bfloat16, 32 best: 69 us, and 35 of
+// other rows).  scan(bound) offers every class again; the caller has synchronised.
+template <int T, typename SCAN>
+BS_DEV void tighten(uint32_t k, Selection<T> &sel, SCAN scan)
 {
-    uint64_t last = ~0ull;
-    for (uint32_t r = 0; r < k; ++r) {
-        uint64_t mine = 0;
-        for (uint32_t j = threadIdx.x; j < n; j += T) {
-            const uint64_t key = get(j);
-            if (key < last && key > mine) mine = key;
-        }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            const uint64_t other = __shfl_xor(mine, o);
-            mine = other > mine ? other : mine;
+    while (sel.count > LIST) {  // (the same in every lane)
+        for (uint32_t i = threadIdx.x; i < LIST; i += T) {
+            const uint64_t key = sel.list[i];
+            uint32_t rank = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < LIST; ++j) rank += sel.list[j] > key;
+            if (rank == k - 1) sel.bound = key;
         }
         __syncthreads();
-        if (threadIdx.x % 64 == 0) sel.lane[threadIdx.x / 64] = mine;
+        if (threadIdx.x == 0) sel.count = 0;
+        const uint64_t bound = sel.bound;
         __syncthreads();
-        last = sel.lane[0];
-#pragma unroll
-        for (int w = 1; w < T / 64; ++w) last = sel.lane[w] > last ? sel.lane[w] : last;
-        if (threadIdx.x == 0) put(r, last);
+        scan(bound);
+        __syncthreads();
     }
 }
 
@@ -435,30 +432,40 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
             if constexpr (PARTS) k.part_keys[(uint64_t)blockIdx.x * k.top + place] = key;
             else top(place, key);
         };
-        if (r.s == r.s) {  // (the same in every lane)
-            const uint64_t key = any ? rank_key(best, first + at) : 0;
-            uint64_t bound = bound_of<T>(key, k.top, sel);
-            if (bound) bound -= VEC - 1;  // the class is any of its vector
-            if (key >= bound && tid < vectors) sel.chosen[atomicAdd(&sel.lanes, 1u)] = (uint16_t)tid;
-            if (tid < edges) offer(rank_key(odd[0], first + edge), bound, sel);
-            __syncthreads();
-            // the chosen lanes' vectors once more, one a thread
-            const uint32_t each = (vectors + T - 1) / T, again = sel.lanes * each;
+        uint64_t key = any ? rank_key(best, first + at) : 0;
+        if (r.s != r.s) {  // (the same in every lane) NaN, which is above all here and which the comparisons have passed by
+            key = tid < edges ? rank_key(odd[0], first + edge) : 0;
+            for (uint32_t j = tid; j < vectors; j += T) {
+                float v[VEC];
+                unpack<DT, VEC>(load_raw<DT, VEC>(x + head * ES + j * 16ull, 0), v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const uint64_t other = rank_key(v[i], first + head + j * VEC + i);
+                    key = other > key ? other : key;
+                }
+            }
+        }
+        uint64_t bound = bound_of<T>(key, k.top, sel);
+        if (bound) bound -= VEC - 1;  // the class is any of its vector
+        if (key >= bound && tid < vectors) sel.chosen[atomicAdd(&sel.lanes, 1u)] = (uint16_t)tid;
+        __syncthreads();
+        // the chosen lanes' vectors once more, one a thread
+        const uint32_t each = (vectors + T - 1) / T, again = sel.lanes * each;
+        auto scan = [&](uint64_t from) {
+            if (tid < edges) offer(rank_key(odd[0], first + edge), from, sel);
             for (uint32_t e = tid; e < again; e += T) {
                 const uint32_t c = e / each, j = sel.chosen[c] + (e - c * each) * T;
                 if (j >= vectors) continue;
                 float v[VEC];
                 unpack<DT, VEC>(load_raw<DT, VEC>(x + head * ES + j * 16ull, 0), v);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) offer(rank_key(v[i], first + head + j * VEC + i), bound, sel);
+                for (int i = 0; i < VEC; ++i) offer(rank_key(v[i], first + head + j * VEC + i), from, sel);
             }
-            __syncthreads();
-            if (sel.count <= LIST) {
-                put_ranked<T>(k.top, sel, put);
-                return;
-            }
-        }
-        put_by_rounds<T>(k.top, n, sel, [&](uint32_t j) { return rank_key(element<DT>(x, j), first + j); }, put);
+        };
+        scan(bound);
+        __syncthreads();
+        tighten<T>(k.top, sel, scan);
+        put_ranked<T>(k.top, sel, put);
     }
 }
 
@@ -497,14 +504,16 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
         for (int u = 0; u < U; ++u) best = first[u] > best ? first[u] : best;
         for (uint32_t j = threadIdx.x + U * T; j < n; j += T) best = keys[j] > best ? keys[j] : best;
         const uint64_t bound = bound_of<T>(best, k.top, sel);
-        if (best >= bound) {
+        auto scan = [&](uint64_t from) {
+            if (best < from) return;
 #pragma unroll
-            for (int u = 0; u < U; ++u) offer(first[u], bound, sel);
-            for (uint32_t j = threadIdx.x + U * T; j < n; j += T) offer(keys[j], bound, sel);
-        }
+            for (int u = 0; u < U; ++u) offer(first[u], from, sel);
+            for (uint32_t j = threadIdx.x + U * T; j < n; j += T) offer(keys[j], from, sel);
+        };
+        scan(bound);
         __syncthreads();
-        if (sel.count <= LIST) put_ranked<T>(k.top, sel, put);
-        else put_by_rounds<T>(k.top, n, sel, [&](uint32_t j) { return keys[j]; }, put);
+        tighten<T>(k.top, sel, scan);
+        put_ranked<T>(k.top, sel, put);
     }
 }
 

@@ -280,3 +280,38 @@ def test_logits_at_the_ends_of_the_range(dtype):
         t[0], t[2], t[3], t[4] = 0, classes - 1, 0, 1
         h[0] = h[4] = 0  # (an entropy's gradient next to differences of 1e38: products with probabilities 0)
         check(x, t, 5, g, h)
+
+
+@pytest.mark.parametrize("classes", [20011, 140001])
+def test_best_classes_all_in_a_few_lanes(classes):
+    """Periods of 2048 and of 512 classes with eight good ones at their start: the bound that the lanes' bests give lets thousands of candidates pass."""
+    j = torch.arange(classes)
+    g = torch.Generator().manual_seed(5)
+    noise = torch.rand(4, classes, generator=g)
+    x = torch.stack([noise[0] + 5 * (j // 8 % 256 < 8), noise[1] + 5 * (j // 8 % 256 == 3), noise[2] + 5 * (j // 4 % 128 < 2), noise[3] + 5 * (j % 2048 < 300)]).cuda()
+    t = torch.zeros(4, dtype=torch.int64).cuda()
+    for dtype in DTYPES.values():
+        for top in (5, 32):
+            check(x.to(dtype), t, top)
+            check(x[:1].to(dtype), t[:1], top)
+
+
+@pytest.mark.parametrize("classes", [9001, 131072])
+def test_best_classes_of_rows_that_are_mostly_alike(classes):
+    """More classes pass the first bound than are kept: equal ones, masked ones, NaN, rising and falling rows."""
+    j = torch.arange(classes, dtype=torch.float32)
+    x, t, _, _ = make(9, classes, "f32", seed=8)
+    x[0] = 1.5
+    x[1] = -math.inf
+    x[1, classes - 7:] = 0.25
+    x[2, 1::3] = math.nan
+    x[3] = math.nan
+    x[4, classes - 20:] = math.nan
+    x[5, ::2] = math.inf
+    x[6] = (j / classes).cuda()
+    x[7] = (-j / classes).cuda()
+    x[8] = (j // 8 % 512 < 12).cuda() * j.cuda() / classes
+    for dtype in DTYPES.values():
+        for top in (1, 7, 32):
+            check(x.to(dtype), t, top)
+            check(x[2:3].to(dtype), t[2:3], top)
