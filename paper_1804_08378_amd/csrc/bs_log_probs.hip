@@ -310,13 +310,23 @@ struct PutTop {
 };
 
 // Sums of elements none of which is in the range that Sums::add works on: all of them masked, or all below it (rows that hold nothing but the
-// type's lowest value), or some above it.  The largest first, then differences from it.
+// type's lowest value), or some above it.  The largest first, then differences from it: two passes more (8192 x 32000 bfloat16: 218 us where every
+// row is at the lowest value, 147 at -infinity, 95 otherwise; a load at a time 423 and 242).
 template <int DT, int T>
 BS_DEV Sums far_sums(const char *x, uint32_t n, float *lds)
 {
+    constexpr uint32_t U = 8;  // loads under way
     Sums mine;
     float most = -INFINITY;
-    for (uint32_t j = threadIdx.x; j < n; j += T) most = max2(most, element<DT>(x, j));
+    uint32_t j = threadIdx.x;
+    for (; j + (U - 1) * T < n; j += U * T) {
+        float v[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) v[u] = element<DT>(x, j + u * T);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) most = max2(most, v[u]);
+    }
+    for (; j < n; j += T) most = max2(most, element<DT>(x, j));
     most = wave_max(most);
     if constexpr (T > 64) {
         if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = most;
@@ -325,11 +335,19 @@ BS_DEV Sums far_sums(const char *x, uint32_t n, float *lds)
         __syncthreads();
     }
     if (most == -INFINITY) return mine;
-    for (uint32_t j = threadIdx.x; j < n; j += T) {
-        const float d = (element<DT>(x, j) - most) * LOG2E, e = __builtin_amdgcn_exp2f(d);
+    auto add = [&](float v) {
+        const float d = (v - most) * LOG2E, e = __builtin_amdgcn_exp2f(d);
         mine.s += e;
         mine.t = __builtin_fmaf(e, max2(d, FAR), mine.t);
+    };
+    for (j = threadIdx.x; j + (U - 1) * T < n; j += U * T) {
+        float v[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) v[u] = element<DT>(x, j + u * T);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) add(v[u]);
     }
+    for (; j < n; j += T) add(element<DT>(x, j));
     mine.ref = mine.above = most;
     return join_lanes<T>(mine, lds);
 }
