@@ -59,8 +59,14 @@ BS_DEV int64_t target_of(const LogProbsK &k, uint64_t row)
 // ------------------------------------------------------------------------------------------------ sums
 // Exponents in units of log2(e) x: one multiply-add an element.  The product is not rounded before the reference's is taken off, and the
 // factor's own rounding stretches all logits alike, by 1.3e-8; t is taken back by the factor's reciprocal.
+//
+// The reference's product is rounded, and settle() takes that rounding out again: by a factor near 1 where references are below NEAR, but the
+// factor leaves the range of float32 where they are 2^31.  So a lane takes no reference of a value beyond FINITE: below -FINITE (masks) classes
+// count 0, which is exact next to any other, 64 from them at least; above it everything counts 0 until far_sums() has the largest.  That takes
+// over too where the work-group's reference is beyond NEAR.
 constexpr float UNIT = (float)(1.0 / (double)LOG2E);
-constexpr float UNSET = -2e38f;  // no reference yet; logits from here down (masks of the type's lowest value) count as far below any reference
+constexpr float NEAR = 1048576.0f, FINITE = 1073741824.0f;
+constexpr float UNSET = -FINITE;  // no reference yet
 
 struct Sums {
     float ref = 0.0f, base = 0.0f;  // reference: a value seen, and its product with log2(e)
@@ -72,7 +78,8 @@ struct Sums {
     {
         if (most > above) {
             const bool first = above == UNSET;
-            const float to = most * LOG2E, d = first ? 0.0f : __builtin_fmaxf(base - to, FAR), f = first ? 0.0f : __builtin_amdgcn_exp2f(d);
+            const float to = most > FINITE ? INFINITY : most * LOG2E;
+            const float d = first ? 0.0f : __builtin_fmaxf(base - to, FAR), f = first ? 0.0f : __builtin_amdgcn_exp2f(d);
             t = f * __builtin_fmaf(s, d, t);
             s *= f;
             ref = most;
@@ -94,6 +101,12 @@ struct Sums {
         t += w;
     }
     BS_DEV bool any() const { return above != UNSET; }
+    // Sums that are complete, against this reference (-infinity: there is none).
+    BS_DEV void against(float reference)
+    {
+        ref = reference;
+        above = reference == -INFINITY ? UNSET : INFINITY;
+    }
     // From the rounded product of the reference to the reference itself.
     BS_DEV void settle()
     {
@@ -114,6 +127,7 @@ struct Sums {
     BS_DEV float log_s() const { return logf(s); }
     BS_DEV float entropy() const { return logf(s) - t / s * UNIT; }
     BS_DEV bool none() const { return s == 0.0f; }  // every class masked
+    BS_DEV bool far() const { return none() || (__builtin_fabsf(ref) > NEAR && s == s); }  // joined: far_sums() has to take over
 };
 
 // One lane's value from another by a fixed pattern inside rows of 16 lanes.
@@ -164,8 +178,7 @@ BS_DEV Sums join_lanes(const Sums &mine, float *lds)
         __syncthreads();
         // every wave joins the waves' results, one a lane
         Sums part;
-        part.ref = lane < W ? lds[lane] : -INFINITY;
-        if (part.ref != -INFINITY) part.above = part.ref;
+        part.against(lane < W ? lds[lane] : -INFINITY);
         part.s = lane < W ? lds[W + lane] : 0.0f;
         part.t = lane < W ? lds[2 * W + lane] : 0.0f;
         ref = wave_max(part.ref);
@@ -174,8 +187,7 @@ BS_DEV Sums join_lanes(const Sums &mine, float *lds)
         r.t = wave_sum(part.t);
         __syncthreads();
     }
-    r.ref = ref;
-    r.above = ref == -INFINITY ? UNSET : ref;
+    r.against(ref);
     return r;
 }
 
@@ -309,8 +321,8 @@ struct PutTop {
     }
 };
 
-// Sums of elements none of which is in the range that Sums::add works on: all of them masked, or all below it (rows that hold nothing but the
-// type's lowest value), or some above it.  The largest first, then differences from it: two passes more (8192 x 32000 bfloat16: 218 us where every
+// Sums of elements whose largest is not in the range that Sums::add works on: all of them masked, or all far below zero (rows that hold nothing
+// but the value that masks), or some far above it.  The largest first, then differences from it: two passes more (8192 x 32000 bfloat16: 218 us where every
 // row is at the lowest value, 147 at -infinity, 95 otherwise; a load at a time 423 and 242).
 template <int DT, int T>
 BS_DEV Sums far_sums(const char *x, uint32_t n, float *lds)
@@ -348,7 +360,7 @@ BS_DEV Sums far_sums(const char *x, uint32_t n, float *lds)
         for (uint32_t u = 0; u < U; ++u) add(v[u]);
     }
     for (; j < n; j += T) add(element<DT>(x, j));
-    mine.ref = mine.above = most;
+    mine.against(most);
     return join_lanes<T>(mine, lds);
 }
 
@@ -432,7 +444,7 @@ __global__ __launch_bounds__(T) void log_probs_kernel(LogProbsK k)
 
     sums.settle();
     Sums r = join_lanes<T>(sums, lds);
-    if (r.none()) r = far_sums<DT, T>(x, n, lds);
+    if (r.far()) r = far_sums<DT, T>(x, n, lds);
     if constexpr (PARTS) {
         if (tid == 0) {
             float *out = k.part_sums + 4 * (uint64_t)blockIdx.x;
@@ -508,8 +520,7 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(LogProbsK k)
     Sums mine;
     if (threadIdx.x < k.parts) {  // at most 256
         const float *in = k.part_sums + 4 * (row * k.parts + threadIdx.x);
-        mine.ref = in[0];
-        if (in[0] != -INFINITY) mine.above = in[0];
+        mine.against(in[0]);
         mine.s = in[1];
         mine.t = in[2];
     }
