@@ -61,7 +61,7 @@ def up_to_date() -> bool:
             os.path.join(CSRC, "bs_torch.cpp"), os.path.join(ROOT, "include", "brainslug.h")))):
         return False
     t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, h) for h in JIT_HEADERS + ["bs_internal.h", "bs_rows_tables.h", "bs_nhwc_device.h", "bs_bwd_device.h", "bs_strip_device.h", "bs_backward_keys.h", "bs_norm.h", "bs_norm_device.h", "bs_norm_resident.h", "bs_log_probs.h"]]
+    deps = sources() + [os.path.join(CSRC, h) for h in JIT_HEADERS + ["bs_internal.h", "bs_rows_tables.h", "bs_nhwc_device.h", "bs_bwd_device.h", "bs_strip_device.h", "bs_backward_keys.h", "bs_norm.h", "bs_exp_device.h", "bs_norm_device.h", "bs_norm_resident.h", "bs_log_probs.h"]]
     deps.append(os.path.join(ROOT, "include", "brainslug.h"))
     return all(os.path.getmtime(d) <= t for d in deps)
 

@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include "bs_device.h"
+#include "bs_exp_device.h"
 #include "bs_internal.h"
 #include "bs_log_probs.h"
 
@@ -20,15 +21,6 @@ namespace {
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float FAR = -300.0f;      // 2 to this power is 0: stands for larger distances where they are multiplied by it
 constexpr uint32_t LIST = 512;      // candidates for the top classes that a work-group keeps
-
-// exp for float32 results: the product with log2(e) in two parts, so that large arguments keep their last bits.
-BS_DEV float exp_exact(float v)
-{
-    const float hi = v * LOG2E;
-    const float lo = __builtin_fmaf(v, LOG2E, -hi) + v * 1.92596299112661746e-8f;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return __builtin_fabsf(hi) < 160.0f ? __builtin_fmaf(e, lo * 0.693147180559945309f, e) : e;  // (beyond: 0, infinity or NaN)
-}
 
 template <int DT>
 BS_DEV float element(const char *p, uint64_t i)

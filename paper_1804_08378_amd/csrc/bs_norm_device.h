@@ -2,20 +2,12 @@
 #pragma once
 
 #include "bs_device.h"
+#include "bs_exp_device.h"
 #include "bs_norm.h"
 
 namespace bs {
 
 // ------------------------------------------------------------------------------------------------ activations
-// exp for float32 results: the product with log2(e) in two parts, so that large arguments keep their last bits.
-BS_DEV float exp_exact(float v)
-{
-    const float hi = v * 1.44269504088896341f;
-    const float lo = __builtin_fmaf(v, 1.44269504088896341f, -hi) + v * 1.92596299112661746e-8f;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return __builtin_fabsf(hi) < 160.0f ? __builtin_fmaf(e, lo * 0.693147180559945309f, e) : e;  // (beyond: 0, infinity or NaN)
-}
-
 // 16-bit results hide the last bits of the exponential and of the reciprocal; float32 ones do not.
 template <int DT>
 BS_DEV float sigmoid(float z)
