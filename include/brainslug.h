@@ -575,7 +575,7 @@ typedef struct bs_log_probs_desc {
     int32_t dtype;                       /* bs_dtype of logits and their gradient             */
     int32_t target_bytes;                /* 4 (int32) or 8 (int64)                            */
     int32_t top;                         /* 0 .. min(classes, BS_MAX_TOP)                     */
-    int32_t reserved;
+    int32_t lse_bytes;                   /* 4 or 0 (float) or 8 (double)                      */
 } bs_log_probs_desc;
 
 /* Device bytes bs_log_probs needs as workspace (0: none). */
@@ -585,13 +585,18 @@ BS_API uint64_t bs_log_probs_workspace_bytes(const bs_log_probs_desc *desc);
  * Enqueue the forward pass on `stream`.  Never synchronises, never allocates.
  *   logits                device, aligned to the element size (rows may begin at any element)
  *   targets               device, one per row; NULL: no given classes (logp must be NULL)
- *   logp, entropy, lse    device, a float per row each, any may be NULL; lse and entropy are what the backward pass needs
+ *   logp, entropy         device, a float per row each, either may be NULL
+ *   lse                   device, a float or a double per row (lse_bytes), or NULL; lse and entropy are what the backward pass needs.  A
+ *                         float rounds away half a unit in the last place of |lse|, which every probability of the backward pass is then off by
+ *                         (relative); a double keeps them as precise as logp at any level of the logits.  From 2^30 on, where the logarithm
+ *                         of the sum of a row's exponentials relative to its maximum is below the last place of a double, the double holds it
+ *                         times a power of two, below the last place of a float: as a number it is lse rounded to a float
  *   top_logp, top_index   device, rows x top; not used with top == 0
  *   workspace             device, 16-byte aligned, >= bs_log_probs_workspace_bytes(desc)
- * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, classes < 1, stride below classes), BS_ERR_PARAM (top, target_bytes), BS_ERR_UNSUPPORTED
+ * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, classes < 1, stride below classes), BS_ERR_PARAM (top, target_bytes, lse_bytes), BS_ERR_UNSUPPORTED
  *         (type; over 2^30 classes, 2^23 rows), BS_ERR_ALIGN, BS_ERR_WORKSPACE, BS_ERR_ALIAS, BS_ERR_HIP.
  */
-BS_API bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const void *targets, float *logp, float *entropy, float *lse,
+BS_API bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const void *targets, float *logp, float *entropy, void *lse,
                               float *top_logp, int32_t *top_index, void *workspace, uint64_t workspace_bytes, void *stream);
 
 /*
@@ -599,7 +604,7 @@ BS_API bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits,
  * (a float per row; either may be NULL: zero).  grad_logits may be the logits themselves (same address and stride); otherwise it shares no
  * byte with an input.  Errors: those of bs_log_probs.
  */
-BS_API bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logits, const void *targets, const float *lse,
+BS_API bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logits, const void *targets, const void *lse,
                                        const float *entropy, const float *grad_logp, const float *grad_entropy, void *grad_logits, void *stream);
 
 /*

@@ -96,7 +96,7 @@ class bs_group_norm_desc(C.Structure):
 class bs_log_probs_desc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("classes", C.c_int64), ("row_stride", C.c_int64), ("grad_row_stride", C.c_int64),
                 ("ignore_index", C.c_int64), ("dtype", C.c_int32), ("target_bytes", C.c_int32), ("top", C.c_int32),
-                ("reserved", C.c_int32)]
+                ("lse_bytes", C.c_int32)]
 
 
 _lib = None

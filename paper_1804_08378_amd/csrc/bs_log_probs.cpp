@@ -17,6 +17,7 @@ bs_status check_desc(const bs_log_probs_desc *d)
     if (d->classes > (1ll << 30) || d->rows > (1ll << 23)) return BS_ERR_UNSUPPORTED;
     if (d->top < 0 || d->top > BS_MAX_TOP || d->top > d->classes) return BS_ERR_PARAM;
     if (d->target_bytes != 4 && d->target_bytes != 8) return BS_ERR_PARAM;
+    if (d->lse_bytes != 0 && d->lse_bytes != 4 && d->lse_bytes != 8) return BS_ERR_PARAM;
     for (const int64_t s : {d->row_stride, d->grad_row_stride})
         if (s != 0 && (s < d->classes || s > (1ll << 40))) return BS_ERR_SHAPE;
     return BS_OK;
@@ -31,7 +32,10 @@ void fill(const bs_log_probs_desc &d, LogProbsK &k)
     k.grad_stride = (uint64_t)(d.grad_row_stride ? d.grad_row_stride : d.classes);
     k.ignore_index = d.ignore_index;
     k.wide_targets = d.target_bytes == 8;
+    k.wide_lse = d.lse_bytes == 8;
 }
+
+uint64_t lse_bytes(const LogProbsK &k) { return k.wide_lse ? 8 : 4; }
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
@@ -96,7 +100,7 @@ uint64_t bs_log_probs_workspace_bytes(const bs_log_probs_desc *desc)
     return space(k).bytes;
 }
 
-bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const void *targets, float *logp, float *entropy, float *lse,
+bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const void *targets, float *logp, float *entropy, void *lse,
                        float *top_logp, int32_t *top_index, void *workspace, uint64_t workspace_bytes, void *stream)
 {
     const bs_status checked = check_desc(desc);
@@ -108,13 +112,13 @@ bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const 
     const Space room = space(k);
     const uint64_t es = dtype_size(desc->dtype);
     if (room.bytes && (!workspace || workspace_bytes < room.bytes)) return BS_ERR_WORKSPACE;
-    if (!aligned(logits, es) || !aligned(targets, (uint64_t)desc->target_bytes) || !aligned(workspace, 16)) return BS_ERR_ALIGN;
-    for (const void *p : {(const void *)logp, (const void *)entropy, (const void *)lse, (const void *)top_logp, (const void *)top_index})
+    if (!aligned(logits, es) || !aligned(targets, (uint64_t)desc->target_bytes) || !aligned(lse, lse_bytes(k)) || !aligned(workspace, 16)) return BS_ERR_ALIGN;
+    for (const void *p : {(const void *)logp, (const void *)entropy, (const void *)top_logp, (const void *)top_index})
         if (!aligned(p, 4)) return BS_ERR_ALIGN;
     if (!desc->top) top_logp = nullptr, top_index = nullptr;
     const uint64_t n = k.rows * 4;
     const bs_status alias = check_overlap({rows_of(logits, k, k.stride, es), bytes_of(targets, k.rows * (uint64_t)desc->target_bytes)},
-                                          {bytes_of(logp, n), bytes_of(entropy, n), bytes_of(lse, n), bytes_of(top_logp, n * k.top), bytes_of(top_index, n * k.top),
+                                          {bytes_of(logp, n), bytes_of(entropy, n), bytes_of(lse, k.rows * lse_bytes(k)), bytes_of(top_logp, n * k.top), bytes_of(top_index, n * k.top),
                                            bytes_of(workspace, room.bytes)});
     if (alias != BS_OK) return alias;
     k.logits = logits;
@@ -130,7 +134,7 @@ bs_status bs_log_probs(const bs_log_probs_desc *desc, const void *logits, const 
     return launch_log_probs(k, desc->dtype, k.classes * es <= 64 * 16 * 4 ? 64 : 256, stream);
 }
 
-bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logits, const void *targets, const float *lse, const float *entropy,
+bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logits, const void *targets, const void *lse, const float *entropy,
                                 const float *grad_logp, const float *grad_entropy, void *grad_logits, void *stream)
 {
     const bs_status checked = check_desc(desc);
@@ -140,19 +144,19 @@ bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void *logit
     LogProbsK k{};
     fill(*desc, k);
     const uint64_t es = dtype_size(desc->dtype);
-    if (!aligned(logits, es) || !aligned(grad_logits, es) || !aligned(targets, (uint64_t)desc->target_bytes)) return BS_ERR_ALIGN;
-    for (const float *p : {lse, entropy, grad_logp, grad_entropy})
+    if (!aligned(logits, es) || !aligned(grad_logits, es) || !aligned(targets, (uint64_t)desc->target_bytes) || !aligned(lse, lse_bytes(k))) return BS_ERR_ALIGN;
+    for (const float *p : {entropy, grad_logp, grad_entropy})
         if (!aligned(p, 4)) return BS_ERR_ALIGN;
     const uint64_t n = k.rows * 4;
     // the gradient may take the logits' place: every element is read before it is written, by the same lane
     const bool in_place = grad_logits == logits && k.stride == k.grad_stride;
     const bs_status alias = check_overlap({in_place ? bytes_of(nullptr, 0) : rows_of(logits, k, k.stride, es), bytes_of(targets, k.rows * (uint64_t)desc->target_bytes),
-                                           bytes_of(lse, n), bytes_of(entropy, n), bytes_of(grad_logp, n), bytes_of(grad_entropy, n)},
+                                           bytes_of(lse, k.rows * lse_bytes(k)), bytes_of(entropy, n), bytes_of(grad_logp, n), bytes_of(grad_entropy, n)},
                                           {rows_of(grad_logits, k, k.grad_stride, es)});
     if (alias != BS_OK) return alias;
     k.logits = logits;
     k.targets = grad_logp ? targets : nullptr;
-    k.lse = const_cast<float *>(lse);
+    k.lse = const_cast<void *>(lse);
     k.entropy = const_cast<float *>(entropy);
     k.grad_logp = grad_logp;
     k.grad_entropy = grad_entropy;

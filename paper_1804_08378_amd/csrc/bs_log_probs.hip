@@ -272,6 +272,17 @@ BS_DEV void tighten(uint32_t k, Selection<T> &sel, SCAN scan)
 }
 
 // ------------------------------------------------------------------------------------------------ a row's results
+// lse = ref + log s for the backward pass, which needs the difference of a logit from it: as one float it would lose of log s what lies below
+// the last place of ref, and with it the size of every probability.  A double keeps it: times a power of two from 2^30 on, which leaves it
+// below half a unit of the float's last place (log s is at most 21), so that the float in the double is ref.
+BS_DEV int raised(float ref) { return max(0, __builtin_amdgcn_frexp_expf(ref) - 31); }
+BS_DEV double join_lse(float ref, float log_s) { return (double)ref + ldexp((double)log_s, raised(ref)); }
+BS_DEV void split_lse(double lse, float &hi, float &lo)
+{
+    hi = (float)lse;
+    lo = (float)ldexp(lse - (double)hi, -raised(hi));
+}
+
 // The row's given class: requested before anything else of the row, used behind everything.
 struct Given {
     int64_t c = 0;
@@ -290,7 +301,8 @@ BS_DEV void put_row(const LogProbsK &k, uint64_t row, const Given &given, const 
     const bool none = r.none();
     const float log_s = r.log_s();
     if (k.entropy) k.entropy[row] = none ? 0.0f : r.entropy();
-    if (k.lse) k.lse[row] = none ? -INFINITY : r.ref + log_s;
+    if (k.lse && k.wide_lse) static_cast<double *>(k.lse)[row] = none ? -INFINITY : join_lse(r.ref, log_s);
+    else if (k.lse) static_cast<float *>(k.lse)[row] = none ? -INFINITY : r.ref + log_s;
     if (k.logp) {
         float v;
         if (given.c == k.ignore_index) v = 0.0f;
@@ -552,7 +564,10 @@ __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
     const uint32_t first = (bid - (uint32_t)row * k.parts) * k.part, n = min(k.classes - first, k.part);
     const char *x = static_cast<const char *>(k.logits) + (row * k.stride + first) * ES;
     char *dx = static_cast<char *>(k.grad_logits) + (row * k.grad_stride + first) * ES;
-    const float lse = k.lse[row], H = k.entropy ? k.entropy[row] : 0.0f, h = k.grad_entropy ? k.grad_entropy[row] : 0.0f;
+    float lse, low = 0.0f;  // and what a float loses of it
+    if (k.wide_lse) split_lse(static_cast<const double *>(k.lse)[row], lse, low);
+    else lse = static_cast<const float *>(k.lse)[row];
+    const float H = k.entropy ? k.entropy[row] : 0.0f, h = k.grad_entropy ? k.grad_entropy[row] : 0.0f;
     const int64_t c = k.targets ? target_of(k, row) : k.ignore_index;
     float g = k.grad_logp && c != k.ignore_index ? k.grad_logp[row] : 0.0f;
     if (c != k.ignore_index && (c < 0 || c >= (int64_t)k.classes)) g = __builtin_nanf("");
@@ -560,9 +575,13 @@ __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
     const uint32_t target = c >= first && c < (int64_t)(first + n) ? (uint32_t)(c - first) : 0xffffffffu;
     // none: -p (0 - 0) of p = 2^-infinity, without a test in the loop
     const float gh = none ? 0.0f : __builtin_fmaf(h, H, g), hd = none ? 0.0f : h, off = none ? INFINITY : lse;
+    low = none ? 0.0f : low;
+    // 16-bit results hide the last bits of the exponential; low takes part in its multiply-add
+    const float low2 = -low * LOG2E, gh_low = DT == DT_F32 ? gh : __builtin_fmaf(-hd, low, gh);
     auto grad = [&](float v) {
-        const float d = v - off, p = DT == DT_F32 ? exp_exact(d) : __builtin_amdgcn_exp2f(d * LOG2E);
-        return -p * __builtin_fmaf(hd, max2(d, FAR), gh);
+        const float d = DT == DT_F32 ? (v - off) - low : v - off;
+        const float p = DT == DT_F32 ? exp_exact(d) : __builtin_amdgcn_exp2f(__builtin_fmaf(d, LOG2E, low2));
+        return -p * __builtin_fmaf(hd, max2(d, FAR), gh_low);
     };
     auto one = [&](uint32_t j) {
         float v[1] = {grad(element<DT>(x, j))};

@@ -727,7 +727,7 @@ struct HeadCall {
         d.classes = logits.size(1);
         d.top = (int32_t)k;
         d.dtype = dtype_code(logits.scalar_type());
-        d.target_bytes = 8;
+        d.target_bytes = d.lse_bytes = 8;
         if (d.dtype < 0 || d.rows < 1 || d.classes < 1 || (d.row_stride = row_stride(logits)) < 0) return false;
         if (targets.defined()) {
             if (!on_gpu(targets, logits.device()) || targets.dim() != 1 || targets.size(0) != d.rows || !targets.is_contiguous()) return false;
@@ -736,9 +736,9 @@ struct HeadCall {
         }
         return true;
     }
-    bool per_row(const at::Tensor &t) const
+    bool per_row(const at::Tensor &t, at::ScalarType type = at::kFloat) const
     {
-        return !t.defined() || (on_gpu(t, logits.device()) && t.scalar_type() == at::kFloat && t.dim() == 1 && t.size(0) == d.rows && t.is_contiguous());
+        return !t.defined() || (on_gpu(t, logits.device()) && t.scalar_type() == type && t.dim() == 1 && t.size(0) == d.rows && t.is_contiguous());
     }
 };
 
@@ -754,7 +754,7 @@ PyObject *log_probs(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::TensorOptions f32 = c.logits.options().dtype(at::kFloat);
         if (c.targets.defined()) logp = at::empty({c.d.rows}, f32);
         entropy = at::empty({c.d.rows}, f32);
-        lse = at::empty({c.d.rows}, f32);
+        lse = at::empty({c.d.rows}, f32.dtype(at::kDouble));
         if (c.d.top) {
             top_logp = at::empty({c.d.rows, c.d.top}, f32);
             top_index = at::empty({c.d.rows, c.d.top}, f32.dtype(at::kInt));
@@ -762,7 +762,7 @@ PyObject *log_probs(PyObject *, PyObject *const *args, Py_ssize_t n)
         const uint64_t bytes = g_operators.head_bytes(&c.d);
         const at::Tensor ws = workspace_of(bytes, f32);
         auto p = [](const at::Tensor &t) { return static_cast<float *>(NormCall::ptr(t)); };
-        const int rc = g_operators.head(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), p(logp), p(entropy), p(lse), p(top_logp),
+        const int rc = g_operators.head(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), p(logp), p(entropy), NormCall::ptr(lse), p(top_logp),
                                         static_cast<int32_t *>(NormCall::ptr(top_index)), NormCall::ptr(ws), bytes,
                                         c10::hip::getCurrentHIPStream(c.logits.device().index()).stream());
         if (rc != 0) throw CallFailed(rc, "bs_log_probs");
@@ -783,12 +783,12 @@ PyObject *log_probs_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     const bool fits = n == 7 && c.read(args[0], args[1], zero, args[6]) && optional_tensor(args[2], lse) && optional_tensor(args[3], entropy) &&
                       optional_tensor(args[4], g) && optional_tensor(args[5], h);
     Py_XDECREF(zero);
-    if (!fits || !lse.defined() || !c.per_row(lse) || !c.per_row(entropy) || !c.per_row(g) || !c.per_row(h)) Py_RETURN_NONE;
+    if (!fits || !lse.defined() || !c.per_row(lse, at::kDouble) || !c.per_row(entropy) || !c.per_row(g) || !c.per_row(h)) Py_RETURN_NONE;
     try {
         pybind11::gil_scoped_release no_gil;
         out = at::empty({c.d.rows, c.d.classes}, c.logits.options());
         auto p = [](const at::Tensor &t) { return static_cast<const float *>(NormCall::ptr(t)); };
-        const int rc = g_operators.head_backward(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), p(lse), p(entropy), p(g), p(h), out.data_ptr(),
+        const int rc = g_operators.head_backward(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), NormCall::ptr(lse), p(entropy), p(g), p(h), out.data_ptr(),
                                                  c10::hip::getCurrentHIPStream(c.logits.device().index()).stream());
         if (rc != 0) throw CallFailed(rc, "bs_log_probs_backward");
     } catch (const CallFailed &e) {

@@ -226,7 +226,7 @@ class GroupNormAct(nn.GroupNorm):
 # ------------------------------------------------------------------------------------------------ log probabilities
 class LogProbs(NamedTuple):
     """Per row: log probability of the given class (None without targets), entropy, top alternatives, most probable first (None for top = 0),
-    and the logarithm of the sum of exponentials that `log_probs_backward` needs."""
+    and the logarithm of the sum of exponentials, float64, that `log_probs_backward` needs."""
     logp: Optional[torch.Tensor]
     entropy: torch.Tensor
     top_logp: Optional[torch.Tensor]
@@ -246,7 +246,7 @@ def _head_operands(logits, targets, top, ignore_index):
             raise ValueError("log_probs: targets hold one int64 or int32 class a row, on the logits' device")
         targets = targets.contiguous()
     d.target_bytes = 4 if targets is not None and targets.dtype == torch.int32 else 8
-    d.ignore_index, d.top = int(ignore_index), int(top)
+    d.ignore_index, d.top, d.lse_bytes = int(ignore_index), int(top), 8
     return d, targets
 
 
@@ -276,7 +276,7 @@ def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -1
         rows, dev = logits.shape[0], logits.device
         f32 = dict(dtype=torch.float32, device=dev)
         logp = torch.empty(rows, **f32) if targets is not None else None
-        entropy, lse = torch.empty(rows, **f32), torch.empty(rows, **f32)
+        entropy, lse = torch.empty(rows, **f32), torch.empty(rows, dtype=torch.float64, device=dev)
         top_logp = torch.empty((rows, top), **f32) if top else None
         top_index = torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None
         n = bs.bs_log_probs_workspace_bytes(d)
@@ -288,8 +288,8 @@ def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -1
 
 def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entropy=None, ignore_index: int = -100,
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Gradient with respect to the logits from those of `logp` and `entropy` (a float a row; None: zero).  `out=logits` writes it over
-    the logits."""
+    """Gradient with respect to the logits from those of `logp` and `entropy` (a float a row; None: zero).  `lse` as `log_probs_forward` gives
+    it; rounded to float32 it is taken too, and probabilities are off by that rounding.  `out=logits` writes the gradient over the logits."""
     native = _native_calls()
     if native and out is None:
         done = native.log_probs_backward(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index)
@@ -300,10 +300,12 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
         rows = logits.shape[0]
         given = []
         for t in (lse, entropy, grad_logp, grad_entropy):
-            if t is not None and (tuple(t.shape) != (rows,) or t.dtype != torch.float32 or t.device != logits.device):
-                raise ValueError("log_probs_backward: lse, entropy and their gradients hold one float32 a row, on the logits' device")
+            if t is not None and (tuple(t.shape) != (rows,) or t.device != logits.device or
+                                  not (t.dtype == torch.float32 or (t is lse and t.dtype == torch.float64))):
+                raise ValueError("log_probs_backward: lse, entropy and their gradients hold one float32 (lse: or float64) a row, on the logits' device")
             given.append(t.contiguous() if t is not None else None)
         lse, entropy, grad_logp, grad_entropy = given
+        d.lse_bytes = lse.element_size()
         if out is None:
             out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
         elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or _row_stride(out) is None:

@@ -2,42 +2,52 @@
 the logits.
 
 Tolerances.  u = 2^-24.  Everything is a function of the differences from the row's maximum, which 32 bits hold to u of themselves.  A sum of
-positive terms is off by under 300 u = 2e-5, so a log probability by 2e-5 and 4 u of itself, the entropy by 2e-5 (1 + entropy).
+positive terms is off by under 300 u = 2e-5, so a log probability by 2e-5 and 4 u of itself, the entropy by 2e-5 (1 + entropy), a probability
+by twice the first (the sums of both passes) relative to itself.  The gradient's terms are products of these.
 """
 import math
 
 import pytest
 import torch
 
+from paper_1804_08378_amd import brainslug as bs
 from paper_1804_08378_amd import functional as F
 
 pytestmark = pytest.mark.gpu
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+ROUNDING = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 U, SUMS = 2.0 ** -24, 2e-5
 
 
-def definition(x, t):
-    """(values, tolerances) of logp and entropy; rows with at least one class that is not at -infinity."""
-    x, t = x.cpu().double(), t.cpu()
+def definition(x, t, g, h):
+    """(values, tolerances) of logp, entropy and grad_logits; rows with at least one class that is not at -infinity."""
+    x, t, g, h = x.cpu().double(), t.cpu(), g.cpu().double()[:, None], h.cpu().double()[:, None]
     d = x - x.amax(1, keepdim=True)
     logp = d - torch.log(torch.exp(d).sum(1, keepdim=True))
     p = torch.exp(logp)
-    entropy = (p * torch.where(p > 0, logp.abs(), 0.0)).sum(1)
+    size = torch.where(p > 0, logp.abs(), 0.0)
+    entropy = (p * size).sum(1, keepdim=True)
+    dx = -g * p + h * p * (size - entropy)
+    dx.scatter_add_(1, t[:, None], g)
+    rel = 2 * SUMS + 8 * U * size
+    dx_off = p * (g.abs() * rel + h.abs() * (rel * (size + entropy + 1) + 2 * SUMS * (1 + entropy))) + 4 * U * dx.abs() + 1e-37
     mine = logp.gather(1, t[:, None])[:, 0]
-    return {"logp": (mine, SUMS + 4 * U * mine.abs()), "entropy": (entropy, SUMS * (1 + entropy))}, logp
+    return {"logp": (mine, SUMS + 4 * U * mine.abs()), "entropy": (entropy[:, 0], SUMS * (1 + entropy[:, 0])), "grad": (dx, dx_off)}, logp
 
 
-def close(got, want, off, label):
+def close(got, want, off, label, rounding=U):
     got = got.detach().cpu().double()
-    bound = off + U * 1.01 * (want.abs() + off)
+    bound = off + rounding * 1.01 * (want.abs() + off) + (2.0 ** -25 if rounding == 2.0 ** -11 else 0)
     bad = ~((got == want) | ((got - want).abs() <= bound))
     assert not bad.any(), (label, int(bad.sum()), torch.nonzero(bad)[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
 
 
-def check(x, t, top=0, label=""):
+def check(x, t, top=0, seed=0, label=""):
     print(f"[log probs] {tuple(x.shape)} {x.dtype} top {top} {label}", flush=True)
-    want, logp = definition(x, t)
+    gen = torch.Generator().manual_seed(seed + 1)
+    g, h = torch.randn(x.shape[0], generator=gen).cuda(), torch.randn(x.shape[0], generator=gen).cuda() * 0.3
+    want, logp = definition(x, t, g, h)
     r = F.log_probs_forward(x, t, top)
     close(r.logp, *want["logp"], "logp")
     close(r.entropy, *want["entropy"], "entropy")
@@ -46,6 +56,7 @@ def check(x, t, top=0, label=""):
         assert torch.equal(r.top_index.cpu().long(), index), "alternatives"
         best = logp.gather(1, index)
         close(r.top_logp, best, SUMS + 4 * U * torch.nan_to_num(best, neginf=0.0).abs(), "top_logp")
+    close(F.log_probs_backward(x, t, r.lse, r.entropy, g, h), *want["grad"], "grad", ROUNDING[x.dtype])
     return r
 
 
@@ -107,6 +118,14 @@ def test_rows_of_one_value(dtype):
             r = F.log_probs_forward(x, t)
             want = torch.full((3,), math.log(n))
             assert torch.allclose(r.entropy.cpu(), want, rtol=2e-5, atol=0) and torch.allclose(r.logp.cpu(), -want, rtol=2e-5, atol=0), value
+            g = torch.tensor([1.0, -2.0, 0.5]).cuda()
+            dx = F.log_probs_backward(x, t, r.lse, r.entropy, g, None).double().cpu()
+            off = 1.01 * ROUNDING[x.dtype] + 5e-5
+            for row in range(3):
+                share = float(g[row]) / n
+                others = torch.cat([dx[row, :t[row]], dx[row, t[row] + 1:]])
+                assert ((others + share).abs() <= off * abs(share) + 2.0 ** -25 * (dtype == "f16")).all(), (value, float(others[0]), -share)
+                assert abs(float(dx[row, t[row]]) - float(g[row]) * (1 - 1 / n)) <= off * abs(float(g[row]))
 
 
 def test_real_logits_among_far_ones_of_both_signs():
@@ -127,3 +146,63 @@ def test_real_logits_among_far_ones_of_both_signs():
         t = torch.tensor([2, classes - 3, 5, 0, 0, 7]).cuda()
         for dtype in (torch.float32, torch.bfloat16):
             check(x.to(dtype).cuda(), t, 5)
+
+
+@pytest.mark.parametrize("level", [0.0, 30.0, 1000.0, 2.0e6, 1.0e9])
+def test_float32_probabilities_do_not_depend_on_the_level(level):
+    """The gradient with respect to shifted logits, whose differences are the same numbers: equal to a few units of the exponent's rounding."""
+    g = torch.Generator().manual_seed(9)
+    step = max(2.0 ** -10, 2.0 ** (math.frexp(level)[1] - 23)) if level else 2.0 ** -10  # a spacing that floats at the level have
+    base = torch.round(torch.randn(50, 4001, generator=g) * 2 / step) * step
+    x = (base.double() + level).float().cuda()
+    t = torch.randint(0, 4001, (50,), generator=g).cuda()
+    r = F.log_probs_forward(x, t)
+    one = torch.ones(50, device="cuda")
+    dx = F.log_probs_backward(x, t, r.lse, r.entropy, one, None).double().cpu()
+    p = torch.softmax(x.cpu().double(), 1)
+    want = -p
+    want.scatter_add_(1, t.cpu()[:, None], torch.ones(50, 1).double())
+    # p: the sum's error (chains of 32 terms, then 6 joins: 40 u) and the exponent's (8 u of it, at most 20 here: 160 u)
+    assert float(((dx - want).abs() / (200 * U * p + 4 * U * want.abs())).max()) <= 1
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_lse_as_a_float(dtype):
+    """Four bytes a row: the double's value, rounded; the gradient from it is off by that rounding."""
+    g = torch.Generator().manual_seed(2)
+    x = (torch.randn(9, 3001, generator=g) * 3 + 20).to(DTYPES[dtype]).cuda()
+    x[3] = -math.inf
+    t = torch.randint(0, 3001, (9,), generator=g).cuda()
+    one = torch.ones(9, device="cuda")
+    r = F.log_probs_forward(x, t)
+    d = bs.bs_log_probs_desc()
+    d.rows, d.classes, d.dtype, d.target_bytes, d.ignore_index = 9, 3001, F._DTYPES[x.dtype], 8, -100
+    lse = torch.full((10,), 77.0, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    bs.bs_log_probs(d, x.data_ptr(), 0, 0, 0, lse.data_ptr(), 0, 0, 0, 0, stream)
+    assert torch.equal(lse[9:], torch.full((1,), 77.0, device="cuda")) and r.lse.dtype == torch.float64
+    assert ((lse[:9].double() - r.lse).abs() <= U * r.lse.abs())[r.lse != -math.inf].all() and lse[3] == r.lse[3] == -math.inf
+    exact = F.log_probs_backward(x, t, r.lse, r.entropy, one).double()
+    rounded = F.log_probs_backward(x, t, lse[:9], r.entropy, one).double()
+    assert ((exact - rounded).abs() <= (64 * U + 2.02 * ROUNDING[x.dtype]) * exact.abs() + 2.0 ** -24 * (dtype == "f16")).all()
+    dx = torch.empty_like(x)
+    bs.bs_log_probs_backward(d, x.data_ptr(), t.data_ptr(), lse.data_ptr(), 0, one.data_ptr(), 0, dx.data_ptr(), stream)
+    assert torch.equal(dx.double(), rounded)
+    with pytest.raises(ValueError, match="float64"):
+        F.log_probs_backward(x, t, lse[:9].half(), r.entropy, one)
+    with pytest.raises(ValueError, match="float32"):
+        F.log_probs_backward(x, t, r.lse, r.entropy.double(), one)
+
+
+def test_lse_sizes_that_are_refused():
+    d = bs.bs_log_probs_desc()
+    d.rows, d.classes, d.dtype, d.target_bytes, d.ignore_index = 4, 100, bs.BS_F32, 8, -100
+    x, t, logp, lse = (1 << 28, (1 << 28) + (1 << 20), (1 << 28) + (2 << 20), (1 << 28) + (3 << 20))  # stand for buffers, never followed
+    for size, at, status in ((3, lse, 3), (16, lse, 3), (-8, lse, 3), (8, lse + 4, 7), (4, lse + 2, 7), (8, logp - 24, 12), (8, x + 392, 12)):
+        d.lse_bytes = size
+        with pytest.raises(bs.BrainSlugError) as e:
+            bs.bs_log_probs(d, x, t, logp, 0, at, 0, 0, 0, 0, 0)
+        assert e.value.status == status, (size, at)
+        with pytest.raises(bs.BrainSlugError) as e:
+            bs.bs_log_probs_backward(d, x, t, at, 0, logp, 0, x, 0) if status != 12 else bs.bs_log_probs_backward(d, x, t, x + 392, 0, logp, 0, x, 0)
+        assert e.value.status == status, (size, at)
