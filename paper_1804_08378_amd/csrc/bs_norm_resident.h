@@ -169,14 +169,18 @@ BS_DEV bool collect(const NormK &k, const Spot &s, uint64_t *words, uint32_t *mi
                 else *missing = 1;  // (its own word is there already)
             }
         }
+        // A barrier does not wait for the waves' stores: every wave's words have to be in memory before any wave counts the work-group out.  (The
+        // words are stored through the L2 caches, so that they are when the wave's count of stores is 0; a release would write back all of the L2
+        // cache for them: 8x512x28x28 binary16 22.1 us.)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     __syncthreads();
     return *missing == 0;
 }
 
 // Behind collect: counts the work-group out.  The last one of a block's finds that nobody looks for its words any more, and clears them (at
-// the end, off the other lanes' way).  Every work-group has published before it counts itself out, so no word comes late; a look at a word has
-// brought its value before the barrier that collect ends with, so none comes behind the count.
+// the end, off the other lanes' way).  Every wave has waited for its words' stores, and a look at a word has brought its value, before the
+// barrier that collect ends with and so before the count: no word and no look comes late, whether or not the work-group went on waiting.
 BS_DEV uint32_t depart(const NormK &k, const Spot &s)
 {
     if (!k.departed || k.chunks == 1 || threadIdx.x != 0) return 0;
