@@ -556,15 +556,19 @@ bool read_float(PyObject *o, double &v)
     return PyFloat_Check(o);
 }
 
-// The memory that the parts of an image hand their sums through: kept for every device and stream, zero-filled once.  (Never destroyed: the
-// process may end after the device has gone.)
-void *exchange_of(const at::Device &dev, void *stream, const at::TensorOptions &like)
+// The memory that the parts of an image hand their sums through: kept for every stream of torch's own (a device's default stream and its pools,
+// which live as long as the process), zero-filled once.  (Never destroyed: the process may end after the device has gone.)
+void *exchange_of(const at::Device &dev, const c10::hip::HIPStream &stream, const at::TensorOptions &like)
 {
     // a recorded graph may run on any stream, next to later calls on this one: it gets none, and clears its workspace by a launch
     if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) return nullptr;
+    // so does a stream that torch did not make, whose id is its handle: a handle can stand for several streams (a thread's own default stream) or
+    // come back for another one while the work of the first still runs
+    const c10::StreamId id = stream.id();
+    if (id != 0 && reinterpret_cast<void *>(id) == static_cast<void *>(stream.stream())) return nullptr;
     static std::mutex mutex;
-    static auto &kept = *new std::map<std::pair<int, void *>, at::Tensor>();
-    const std::pair<int, void *> key{dev.index(), stream};
+    static auto &kept = *new std::map<std::pair<int, c10::StreamId>, at::Tensor>();
+    const std::pair<int, c10::StreamId> key{dev.index(), id};
     {
         std::lock_guard<std::mutex> lock(mutex);
         const auto it = kept.find(key);
@@ -614,7 +618,7 @@ struct NormCall {
     }
     at::Tensor empty() const { return at::empty(x.sizes(), like.memory_format(at::MemoryFormat::ChannelsLast)); }
     // Small images are one part and need none.
-    void exchange(void *stream)
+    void exchange(const c10::hip::HIPStream &stream)
     {
         if (d.shape[1] * d.shape[2] * d.shape[3] < 8192) return;
         d.exchange = exchange_of(x.device(), stream, like);
@@ -656,12 +660,12 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
         pybind11::gil_scoped_release no_gil;
         y = c.empty();
         if (keep) stats = at::empty({c.x.size(0), c.d.groups, 2}, c.like.dtype(at::kFloat));
-        void *const stream = c10::hip::getCurrentHIPStream(c.x.device().index()).stream();
+        const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(c.x.device().index());
         c.exchange(stream);
         const uint64_t bytes = g_operators.norm_bytes(&c.d, 0);
         const at::Tensor ws = workspace_of(bytes, c.like);
         const int rc = g_operators.norm(&c.d, c.x.data_ptr(), c.ptr(c.residual), c.ptr(c.weight), c.ptr(c.bias), y.data_ptr(), static_cast<float *>(c.ptr(stats)),
-                                        c.ptr(ws), bytes, stream);
+                                        c.ptr(ws), bytes, stream.stream());
         if (rc != 0) throw CallFailed(rc, "bs_group_norm");
     } catch (const CallFailed &e) {
         return failed(e);
@@ -691,12 +695,12 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         if ((wanted & 2) && c.weight.defined()) gw = at::empty({c.x.size(1)}, c.weight.options());
         if ((wanted & 4) && c.bias.defined()) gb = at::empty({c.x.size(1)}, c.bias.options());
         if ((wanted & 8) && c.residual.defined()) gr = c.empty();
-        void *const stream = c10::hip::getCurrentHIPStream(c.x.device().index()).stream();
+        const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(c.x.device().index());
         c.exchange(stream);
         const uint64_t bytes = g_operators.norm_bytes(&c.d, 1);
         const at::Tensor ws = workspace_of(bytes, c.like);
         const int rc = g_operators.norm_backward(&c.d, c.x.data_ptr(), c.ptr(c.residual), c.ptr(c.weight), c.ptr(c.bias), static_cast<const float *>(st.data_ptr()),
-                                                 dy.data_ptr(), c.ptr(gx), c.ptr(gr), c.ptr(gw), c.ptr(gb), c.ptr(ws), bytes, stream);
+                                                 dy.data_ptr(), c.ptr(gx), c.ptr(gr), c.ptr(gw), c.ptr(gb), c.ptr(ws), bytes, stream.stream());
         if (rc != 0) throw CallFailed(rc, "bs_group_norm_backward");
     } catch (const CallFailed &e) {
         return failed(e);

@@ -1,4 +1,6 @@
 """The memory that the parts of an image hand sums through: calls one behind the other, those whose work-groups wait and those whose do not."""
+import ctypes
+
 import pytest
 import torch
 
@@ -42,3 +44,44 @@ def test_calls_follow_each_other_through_one_memory(shape, dtype):
     assert not memory.any()
     for i, out in enumerate(outs):
         assert all(torch.equal(a, b) for a, b in zip(out, want[i % 3])), i
+
+
+def test_streams_that_torch_did_not_make():
+    """A handle from elsewhere keeps no memory: it may stand for several streams, or for another one tomorrow.  Results are the same bits."""
+    hip = ctypes.CDLL("libamdhip64.so")
+    x, weight, bias, res, dy = tensors((2, 64, 60, 60, 8), "bf16", 0, True)
+    args = (8, weight, bias, res, "silu")
+
+    def both():
+        y, stats = F.group_norm_forward(x, *args)
+        return (y, stats, *F.group_norm_backward(x, stats, dy, *args))
+
+    want = both()
+    torch.cuda.synchronize()
+    handles, kept = [], []
+    for _ in range(3):
+        handle = ctypes.c_void_p()
+        assert hip.hipStreamCreate(ctypes.byref(handle)) == 0
+        handles.append(handle)
+        before = torch.cuda.memory_allocated()
+        with torch.cuda.stream(torch.cuda.ExternalStream(handle.value)):
+            got = both()
+            torch.cuda.current_stream().synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del got
+        kept.append(torch.cuda.memory_allocated() - before)
+    for handle in handles:
+        assert hip.hipStreamDestroy(handle) == 0
+    assert kept == [0, 0, 0]
+
+
+def test_streams_of_torch_keep_the_memory_once():
+    """The default stream and a stream of torch's pool, called again: nothing more is kept."""
+    x = tensors((2, 64, 60, 60, 8), "bf16", 0, False)[0]
+    for stream in (torch.cuda.default_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(stream):
+            F.group_norm(x, 8)
+            before = torch.cuda.memory_allocated()
+            F.group_norm(x, 8)
+            assert torch.cuda.memory_allocated() == before
+    torch.cuda.synchronize()
