@@ -11,6 +11,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/PythonFallbackKernel.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
@@ -497,7 +498,8 @@ PyObject *set_error(PyObject *, PyObject *cls)
 }
 
 // ---------------------------------------------------------------------------------------------------- operators without a plan
-// Group normalisation and log probabilities (functional.py): the same bargain, every function returns None for what is not the plain case.
+// Group normalisation and log probabilities (functional.py): the same bargain, every function returns None for what is not the plain case.  The
+// tensors' device is the current one while a call runs: a default stream's handle names no device.
 struct Operators {
     decltype(&bs_group_norm_workspace_bytes) norm_bytes;
     decltype(&bs_group_norm) norm;
@@ -658,6 +660,7 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
     at::Tensor y, stats;
     try {
         pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.x.device());
         y = c.empty();
         if (keep) stats = at::empty({c.x.size(0), c.d.groups, 2}, c.like.dtype(at::kFloat));
         const c10::hip::HIPStream stream = c10::hip::getCurrentHIPStream(c.x.device().index());
@@ -691,6 +694,7 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     at::Tensor gx, gw, gb, gr;
     try {
         pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.x.device());
         if (wanted & 1) gx = c.empty();
         if ((wanted & 2) && c.weight.defined()) gw = at::empty({c.x.size(1)}, c.weight.options());
         if ((wanted & 4) && c.bias.defined()) gb = at::empty({c.x.size(1)}, c.bias.options());
@@ -755,6 +759,7 @@ PyObject *log_probs(PyObject *, PyObject *const *args, Py_ssize_t n)
     at::Tensor logp, entropy, lse, top_logp, top_index;
     try {
         pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.logits.device());
         const at::TensorOptions f32 = c.logits.options().dtype(at::kFloat);
         if (c.targets.defined()) logp = at::empty({c.d.rows}, f32);
         entropy = at::empty({c.d.rows}, f32);
@@ -790,6 +795,7 @@ PyObject *log_probs_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (!fits || !lse.defined() || !c.per_row(lse, at::kDouble) || !c.per_row(entropy) || !c.per_row(g) || !c.per_row(h)) Py_RETURN_NONE;
     try {
         pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.logits.device());
         out = at::empty({c.d.rows, c.d.classes}, c.logits.options());
         auto p = [](const at::Tensor &t) { return static_cast<const float *>(NormCall::ptr(t)); };
         const int rc = g_operators.head_backward(&c.d, c.logits.data_ptr(), NormCall::ptr(c.targets), NormCall::ptr(lse), p(entropy), p(g), p(h), out.data_ptr(),

@@ -2,8 +2,8 @@
 activation (channels last), and the log probabilities at a classifier's end, both with their gradients.
 
 `group_norm` and `log_probs` are differentiable functions; `GroupNormAct` is the normalisation as a module.  The `_forward` / `_backward`
-pairs are the single passes, for programs that keep their own tape.  Everything runs on torch's current stream through the C ABI
-(`bs_group_norm`, `bs_log_probs` in include/brainslug.h); there is no fallback: tensors the library cannot take raise.
+pairs are the single passes, for programs that keep their own tape.  Everything runs on the current stream of the tensors' device through the
+C ABI (`bs_group_norm`, `bs_log_probs` in include/brainslug.h); there is no fallback: tensors the library cannot take raise.
 """
 from __future__ import annotations
 
@@ -133,8 +133,9 @@ def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stat
         return out, stats  # no images
     n = bs.bs_group_norm_workspace_bytes(d, False)
     ws = _workspace(n, x)
-    bs.bs_group_norm(d, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), out.data_ptr(), _ptr(stats), _ptr(ws), n,
-                     torch.cuda.current_stream(x.device).cuda_stream)
+    with torch.cuda.device(x.device):
+        bs.bs_group_norm(d, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), out.data_ptr(), _ptr(stats), _ptr(ws), n,
+                         torch.cuda.current_stream(x.device).cuda_stream)
     return out, stats
 
 
@@ -173,8 +174,9 @@ def group_norm_backward(x, stats, grad, groups: int, weight=None, bias=None, res
             return gx, gw, gb, gr
         n = bs.bs_group_norm_workspace_bytes(d, True)
         ws = _workspace(n, x)
-        bs.bs_group_norm_backward(d, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), stats.data_ptr(), grad.data_ptr(), _ptr(gx), _ptr(gr),
-                                  _ptr(gw), _ptr(gb), _ptr(ws), n, torch.cuda.current_stream(x.device).cuda_stream)
+        with torch.cuda.device(x.device):
+            bs.bs_group_norm_backward(d, x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), stats.data_ptr(), grad.data_ptr(), _ptr(gx), _ptr(gr),
+                                      _ptr(gw), _ptr(gb), _ptr(ws), n, torch.cuda.current_stream(x.device).cuda_stream)
         return gx, gw, gb, gr
 
 
@@ -281,8 +283,9 @@ def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -1
         top_index = torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None
         n = bs.bs_log_probs_workspace_bytes(d)
         ws = _workspace(n, logits)
-        bs.bs_log_probs(d, logits.data_ptr(), _ptr(targets), _ptr(logp), entropy.data_ptr(), lse.data_ptr(), _ptr(top_logp), _ptr(top_index),
-                        _ptr(ws), n, torch.cuda.current_stream(dev).cuda_stream)
+        with torch.cuda.device(dev):
+            bs.bs_log_probs(d, logits.data_ptr(), _ptr(targets), _ptr(logp), entropy.data_ptr(), lse.data_ptr(), _ptr(top_logp), _ptr(top_index),
+                            _ptr(ws), n, torch.cuda.current_stream(dev).cuda_stream)
         return LogProbs(logp, entropy, top_logp, top_index, lse)
 
 
@@ -312,8 +315,9 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
             raise ValueError("log_probs_backward: out must have the logits' shape, type and device, its classes contiguous")
         d.grad_row_stride = _row_stride(out)
         logits, d.row_stride = _readable_rows(logits)
-        bs.bs_log_probs_backward(d, logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy),
-                                 out.data_ptr(), torch.cuda.current_stream(logits.device).cuda_stream)
+        with torch.cuda.device(logits.device):
+            bs.bs_log_probs_backward(d, logits.data_ptr(), _ptr(targets), lse.data_ptr(), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy),
+                                     out.data_ptr(), torch.cuda.current_stream(logits.device).cuda_stream)
         return out
 
 
