@@ -3,7 +3,8 @@ activation (channels last), and the log probabilities at a classifier's end, bot
 
 `group_norm` and `log_probs` are differentiable functions; `GroupNormAct` is the normalisation as a module.  The `_forward` / `_backward`
 pairs are the single passes, for programs that keep their own tape.  Everything runs on the current stream of the tensors' device through the
-C ABI (`bs_group_norm`, `bs_log_probs` in include/brainslug.h); there is no fallback: tensors the library cannot take raise.
+C ABI (`bs_group_norm`, `bs_log_probs` in include/brainslug.h); there is no fallback: tensors the library cannot take raise.  What overrides
+torch's functions overrides these too: `torch.fx` records a call of one of them as one node, so `optimize_graph` and `capture` take models with them.
 """
 from __future__ import annotations
 
@@ -12,6 +13,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 from torch import nn
+from torch.overrides import handle_torch_function, has_torch_function_variadic
 
 from . import brainslug as bs
 
@@ -144,6 +146,8 @@ def group_norm_forward(x, groups: int, weight=None, bias=None, residual=None, ac
     """`(y, stats)`: the forward pass and, N x groups x 2 float32, the means and reciprocal deviations that `group_norm_backward` needs.
     `x` and `residual` are channels last, or channel slices of such tensors (read in place; other memory orders are copied first); `y` is
     channels last, or written to `out`."""
+    if has_torch_function_variadic(x, weight, bias, residual):
+        return handle_torch_function(group_norm_forward, (x, weight, bias, residual), x, groups, weight, bias, residual, activation, eps, out)
     with torch.no_grad():
         return _run_norm(x, groups, weight, bias, residual, activation, eps, out, True)
 
@@ -152,6 +156,9 @@ def group_norm_backward(x, stats, grad, groups: int, weight=None, bias=None, res
                         need=(True, True, True, True)):
     """`(grad_x, grad_weight, grad_bias, grad_residual)` from the gradient `grad` of `group_norm_forward`'s result; `need` says which of
     them are wanted (those of absent operands are None)."""
+    if has_torch_function_variadic(x, stats, grad, weight, bias, residual):
+        return handle_torch_function(group_norm_backward, (x, stats, grad, weight, bias, residual), x, stats, grad, groups, weight, bias, residual,
+                                     activation, eps, need)
     native, act = _native_calls(), ACTIVATIONS.get(activation)
     if native and act is not None:
         done = native.group_norm_backward(x, stats, grad, groups, weight, bias, residual, act, eps, need[0] | need[1] << 1 | need[2] << 2 | need[3] << 3)
@@ -201,7 +208,10 @@ class _GroupNorm(torch.autograd.Function):
 def group_norm(x, groups: int, weight=None, bias=None, residual=None, activation: str = "identity", eps: float = 1e-5, out: Optional[torch.Tensor] = None):
     """act(group_norm(x) * weight + bias + residual), channels last; differentiable in every tensor.  See `group_norm_forward`; `out` is
     for calls that autograd does not record."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual)):
+    if has_torch_function_variadic(x, weight, bias, residual):
+        return handle_torch_function(group_norm, (x, weight, bias, residual), x, groups, weight, bias, residual, activation, eps, out)
+    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad) or
+                                    (residual is not None and residual.requires_grad)):
         if out is not None:
             raise RuntimeError("group_norm: out is for calls that autograd does not record")
         return _GroupNorm.apply(x, weight, bias, residual, groups, activation, eps)
@@ -267,6 +277,8 @@ def _readable_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
 def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -100) -> LogProbs:
     """Log probabilities of `targets`, entropy and `top` best classes of every row of `logits` (rows x classes; rows may lie further apart
     than they are long).  What masked classes, empty rows and ignored targets give stands at bs_log_probs in include/brainslug.h."""
+    if has_torch_function_variadic(logits, targets):
+        return handle_torch_function(log_probs_forward, (logits, targets), logits, targets, top, ignore_index)
     native = _native_calls()
     if native:
         done = native.log_probs(logits, targets, top, ignore_index)
@@ -293,6 +305,9 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient with respect to the logits from those of `logp` and `entropy` (a float a row; None: zero).  `lse` as `log_probs_forward` gives
     it; rounded to float32 it is taken too, and probabilities are off by that rounding.  `out=logits` writes the gradient over the logits."""
+    if has_torch_function_variadic(logits, targets, lse, entropy, grad_logp, grad_entropy):
+        return handle_torch_function(log_probs_backward, (logits, targets, lse, entropy, grad_logp, grad_entropy), logits, targets, lse, entropy,
+                                     grad_logp, grad_entropy, ignore_index, out)
     native = _native_calls()
     if native and out is None:
         done = native.log_probs_backward(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index)
@@ -344,6 +359,8 @@ class _LogProbs(torch.autograd.Function):
 
 def log_probs(logits, targets=None, top: int = 0, ignore_index: int = -100) -> LogProbs:
     """`log_probs_forward`, differentiable in `logp` and `entropy`: a cross entropy is `-log_probs(logits, targets).logp.mean()`."""
+    if has_torch_function_variadic(logits, targets):
+        return handle_torch_function(log_probs, (logits, targets), logits, targets, top, ignore_index)
     if torch.is_grad_enabled() and logits.requires_grad:
         return LogProbs(*_LogProbs.apply(logits, targets, top, ignore_index))
     return log_probs_forward(logits, targets, top, ignore_index)

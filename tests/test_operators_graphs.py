@@ -1,0 +1,146 @@
+"""Models with the operators in `torch.fx`, `optimize_graph` and `capture`."""
+import importlib.util
+import os
+
+import pytest
+import torch
+from torch import fx, nn
+
+from paper_1804_08378_amd import functional as F
+from paper_1804_08378_amd.frontend import BrainSlugStack, capture, optimize_graph
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def classifier():
+    spec = importlib.util.spec_from_file_location("train_from_scratch", os.path.join(ROOT, "examples", "train_from_scratch.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    torch.manual_seed(0)
+    return m.Classifier(width=16).eval()
+
+
+class Mixed(nn.Module):
+    """Layers that become a stack in front of and behind a group normalisation with a residual operand, and answers at the end."""
+
+    def __init__(self):
+        super().__init__()
+        self.conv = nn.Conv2d(3, 16, 3, padding=1)
+        self.bn, self.pool = nn.BatchNorm2d(16), nn.MaxPool2d(2)
+        self.norm = F.GroupNormAct(4, 16, "silu")
+        self.bn2 = nn.BatchNorm2d(16)
+        self.fc = nn.Linear(16, 40)
+
+    def forward(self, x, targets):
+        x = self.pool(torch.relu(self.bn(self.conv(x))))
+        x = self.norm(x, x * 0.5)
+        x = torch.relu(self.bn2(x))
+        r = F.log_probs(self.fc(x.mean((2, 3))), targets, top=3)
+        return r.logp, r.entropy, r.top_index
+
+
+def calls(gm, function):
+    return [n for n in gm.graph.nodes if n.op == "call_function" and n.target is function]
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_models_are_traced(grad):
+    """A call is one node; the layers around it are found as they are without it."""
+    with torch.set_grad_enabled(grad):
+        gm = optimize_graph(classifier())
+        assert len(calls(gm, F.group_norm)) == 9 and not gm.optimized_stacks
+        gm = optimize_graph(Mixed().eval())
+        assert len(calls(gm, F.group_norm)) == len(calls(gm, F.log_probs)) == 1
+        assert [len(s.layers) for s in gm.optimized_stacks] == [3, 2]
+
+
+def test_single_passes_are_traced():
+    def both(x, stats, dy, logits, t, lse, h):
+        y, s = F.group_norm_forward(x, 4, activation="relu")
+        gx = F.group_norm_backward(x, stats, dy, 4, activation="relu")[0]
+        r = F.log_probs_forward(logits, t, 2)
+        return y, s, gx, r.lse, F.log_probs_backward(logits, t, lse, h, h)
+
+    gm = fx.symbolic_trace(both)
+    assert all(len(calls(gm, f)) == 1 for f in (F.group_norm_forward, F.group_norm_backward, F.log_probs_forward, F.log_probs_backward))
+
+
+class WithoutProducts(nn.Module):
+    """Nothing but element-wise layers, poolings and the operators: equal bits from call to call."""
+
+    def __init__(self):
+        super().__init__()
+        self.norm = F.GroupNormAct(8, 64, "gelu")
+        self.bn, self.pool = nn.BatchNorm2d(64), nn.AvgPool2d(2)
+        self.norm2 = F.GroupNormAct(4, 64, "relu")
+
+    def forward(self, x):
+        y = self.pool(torch.relu(self.bn(self.norm(x))))
+        r = F.log_probs(self.norm2(y, y).amax((2, 3)), None, top=5)
+        return torch.cat([r.top_logp, r.top_index.float(), r.entropy[:, None]], 1)
+
+
+@pytest.mark.gpu
+def test_rewritten_and_captured_models_answer_alike():
+    torch.manual_seed(1)
+    model = WithoutProducts().cuda().eval()
+    gm = optimize_graph(model)
+    assert len(gm.optimized_stacks) == 1
+    x = torch.randn(4, 64, 40, 40, device="cuda").contiguous(memory_format=torch.channels_last)
+    with torch.no_grad():
+        want = gm(x)
+        off = (want[:, :5] - model(x)[:, :5]).abs().max()
+        assert float(off) <= 1e-5  # the stack's roundings: a few units of values of size 1
+        graph = capture(model, x)
+        for i in range(4):
+            y = torch.randn(x.shape, generator=torch.Generator().manual_seed(i)).cuda().contiguous(memory_format=torch.channels_last)
+            assert torch.equal(graph(y).clone(), gm(y)), i
+
+
+@pytest.mark.gpu
+def test_a_captured_classifier():
+    """Convolutions do not give equal bits from call to call: results of size 1 behind ten layers of float32, compared to 1e-5."""
+    torch.manual_seed(1)
+    model = classifier().cuda().to(memory_format=torch.channels_last)
+    x = torch.randn(4, 3, 32, 32, device="cuda").contiguous(memory_format=torch.channels_last)
+    with torch.no_grad():
+        assert float((optimize_graph(model)(x) - model(x)).abs().max()) <= 1e-5
+        graph = capture(model, x)
+        for i in range(3):
+            y = torch.randn(x.shape, generator=torch.Generator().manual_seed(i)).cuda().contiguous(memory_format=torch.channels_last)
+            assert float((graph(y) - model(y)).abs().max()) <= 1e-5, i
+
+
+@pytest.mark.gpu
+def test_a_rewritten_model_trains():
+    """Gradients of the rewritten model are those of the model: BatchNorm in inference mode, its chain a stack; float32, so that the two forms
+    of the chain differ by roundings only (1e-5 of a gradient's norm)."""
+    torch.manual_seed(2)
+    model = Mixed().cuda().eval().to(memory_format=torch.channels_last)
+    for bn in (model.bn, model.bn2):
+        bn.weight.requires_grad_(False)
+        bn.bias.requires_grad_(False)
+    x = torch.randn(6, 3, 16, 16, device="cuda").contiguous(memory_format=torch.channels_last)
+    t = torch.arange(6, device="cuda")
+    gm = optimize_graph(model)
+    assert any(isinstance(m, BrainSlugStack) for m in gm.modules())
+    grads = []
+    for m in (model, gm):
+        logp, entropy, index = m(x, t)
+        loss = -logp.mean() - 0.1 * entropy.mean()
+        params = [model.conv.weight, model.norm.weight, model.norm.bias, model.fc.weight]
+        grads.append((index, *torch.autograd.grad(loss, params)))
+    assert torch.equal(grads[0][0], grads[1][0])
+    for a, b in zip(grads[0][1:], grads[1][1:]):
+        assert float((a - b).norm()) <= 1e-5 * float(a.norm()) + 1e-9
+
+
+class Marked(torch.Tensor):
+    pass
+
+
+@pytest.mark.gpu
+def test_tensor_subclasses_stay():
+    x = torch.randn(2, 8, 5, 5, device="cuda").contiguous(memory_format=torch.channels_last)
+    y = F.group_norm(x.as_subclass(Marked), 2)
+    assert type(y) is Marked and torch.equal(y.as_subclass(torch.Tensor), F.group_norm(x, 2))
