@@ -20,6 +20,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <array>
 #include <cstdint>
@@ -523,14 +524,18 @@ PyObject *set_operators(PyObject *, PyObject *args)
 
 int32_t dtype_code(at::ScalarType t) { return t == at::kFloat ? BS_F32 : t == at::kBFloat16 ? BS_BF16 : t == at::kHalf ? BS_F16 : -1; }
 
-// A tensor argument that may be None; false: neither (no error set).
+// Whoever records or derives operations on tensors has to see the Python code's answer: torch.jit.trace, forward-mode derivatives.
+bool dual(const at::Tensor &t) { return t._fw_grad(0).defined(); }
+bool recorders_active() { return modes_active() || torch::jit::tracer::isTracing(); }
+
+// A tensor argument that may be None; false: neither (no error set), or one with a forward-mode derivative.
 bool optional_tensor(PyObject *o, at::Tensor &t)
 {
     if (o == Py_None) return true;
     const at::Tensor *p = tensor_of(o);
     if (!p) return false;
     t = *p;
-    return t.defined();
+    return t.defined() && !dual(t);
 }
 bool on_gpu(const at::Tensor &t, const at::Device &dev) { return t.is_cuda() && t.has_storage() && t.device() == dev; }
 
@@ -590,7 +595,7 @@ struct NormCall {
     bool read(PyObject *xo, PyObject *groups, PyObject *wo, PyObject *bo, PyObject *ro, PyObject *act, PyObject *eps)
     {
         const at::Tensor *xp = tensor_of(xo);
-        if (!g_operators.norm || !xp || modes_active() || !xp->defined() || !xp->is_cuda() || !xp->has_storage() || xp->dim() != 4) return false;
+        if (!g_operators.norm || !xp || recorders_active() || !xp->defined() || dual(*xp) || !xp->is_cuda() || !xp->has_storage() || xp->dim() != 4) return false;
         x = *xp;
         int64_t g, a;
         if (!read_int(groups, g) || !read_int(act, a) || !read_float(eps, d.eps) || g < 1 || g > x.size(1)) return false;
@@ -686,7 +691,7 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (n != 10 || !c.read(args[0], args[3], args[4], args[5], args[6], args[7], args[8])) Py_RETURN_NONE;
     const at::Tensor *stats = tensor_of(args[1]), *grad = tensor_of(args[2]);
     int64_t wanted;
-    if (!stats || !grad || !stats->defined() || !grad->defined() || !read_int(args[9], wanted) || !c.beside(*grad, c.d.grad_y_stride)) Py_RETURN_NONE;
+    if (!stats || !grad || !stats->defined() || !grad->defined() || dual(*stats) || dual(*grad) || !read_int(args[9], wanted) || !c.beside(*grad, c.d.grad_y_stride)) Py_RETURN_NONE;
     if (!on_gpu(*stats, c.x.device()) || stats->scalar_type() != at::kFloat || !stats->is_contiguous() || stats->dim() != 3 || stats->size(0) != c.x.size(0) ||
         stats->size(1) != c.d.groups || stats->size(2) != 2)
         Py_RETURN_NONE;
@@ -727,7 +732,7 @@ struct HeadCall {
     bool read(PyObject *lo, PyObject *to, PyObject *top, PyObject *ignore)
     {
         const at::Tensor *lp = tensor_of(lo);
-        if (!g_operators.head || !lp || modes_active() || !lp->defined() || !lp->is_cuda() || !lp->has_storage() || lp->dim() != 2) return false;
+        if (!g_operators.head || !lp || recorders_active() || !lp->defined() || dual(*lp) || !lp->is_cuda() || !lp->has_storage() || lp->dim() != 2) return false;
         logits = *lp;
         int64_t k;
         if (!optional_tensor(to, targets) || !read_int(top, k) || k < 0 || k > BS_MAX_TOP || !read_int(ignore, d.ignore_index)) return false;

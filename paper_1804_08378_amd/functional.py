@@ -13,6 +13,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 from torch import nn
+from torch.autograd import forward_ad
 from torch.overrides import handle_torch_function, has_torch_function_variadic
 
 from . import brainslug as bs
@@ -28,8 +29,8 @@ _native = None  # the native calls (csrc/bs_torch.cpp), False: not built for thi
 
 
 def _native_calls():
-    """Every one of them takes the plain case -- tensors that are read in place, on one device, without dispatch modes -- and returns None for
-    any other, which the Python code takes or refuses."""
+    """Every one of them takes the plain case -- tensors that are read in place, on one device, without dispatch modes, forward-mode derivatives
+    or tracing -- and returns None for any other, which the Python code takes or refuses."""
     global _native
     if _native is None:
         with bs._native_lock:
@@ -53,6 +54,14 @@ def _dtype(t: torch.Tensor, what: str) -> int:
 def _on_gpu(t: torch.Tensor, what: str) -> None:
     if not t.is_cuda:
         raise RuntimeError(f"{what} needs tensors on the GPU")
+
+
+def _refuse_recorders(what: str, *tensors: Optional[torch.Tensor]) -> None:
+    """Results are written through pointers: whoever records or derives operations on tensors would see an empty tensor and nothing else."""
+    if torch.jit.is_tracing():
+        raise RuntimeError(f"{what}: torch.jit.trace records calls of group_norm and log_probs, not the single passes, nor calls with out")
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError(f"{what} has no forward-mode derivatives")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> int:
@@ -116,12 +125,17 @@ def _norm_operands(x, groups, weight, bias, residual, activation, eps, grad=None
     return d, x, residual, grad
 
 
-def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stats):
+def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stats, recorded=False):
+    """`recorded`: called by the node that a recorder sees."""
     native, act = _native_calls(), ACTIVATIONS.get(activation)
     if native and out is None and act is not None:
         done = native.group_norm(x, groups, weight, bias, residual, act, eps, keep_stats)
         if done is not None:
             return done if keep_stats else (done, None)
+    if not recorded:
+        if torch.jit.is_tracing() and not keep_stats and out is None:
+            return _GroupNorm.apply(x, weight, bias, residual, groups, activation, eps), None
+        _refuse_recorders("group_norm", x, weight, bias, residual)
     d, x, residual, _ = _norm_operands(x, groups, weight, bias, residual, activation, eps)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device, memory_format=torch.channels_last)
@@ -164,6 +178,7 @@ def group_norm_backward(x, stats, grad, groups: int, weight=None, bias=None, res
         done = native.group_norm_backward(x, stats, grad, groups, weight, bias, residual, act, eps, need[0] | need[1] << 1 | need[2] << 2 | need[3] << 3)
         if done is not None:
             return done
+    _refuse_recorders("group_norm_backward", x, stats, grad, weight, bias, residual)
     with torch.no_grad():
         d, x, residual, grad = _norm_operands(x, groups, weight, bias, residual, activation, eps, grad)
         if tuple(stats.shape) != (x.shape[0], groups, 2) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != x.device:
@@ -192,7 +207,7 @@ class _GroupNorm(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, residual, groups, activation, eps):
-        y, stats = _run_norm(x, groups, weight, bias, residual, activation, eps, None, True)
+        y, stats = _run_norm(x, groups, weight, bias, residual, activation, eps, None, True, recorded=True)
         ctx.save_for_backward(x, weight, bias, residual, stats)
         ctx.args = groups, activation, eps
         return y
@@ -279,11 +294,20 @@ def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -1
     than they are long).  What masked classes, empty rows and ignored targets give stands at bs_log_probs in include/brainslug.h."""
     if has_torch_function_variadic(logits, targets):
         return handle_torch_function(log_probs_forward, (logits, targets), logits, targets, top, ignore_index)
+    return _run_log_probs(logits, targets, top, ignore_index)
+
+
+def _run_log_probs(logits, targets, top, ignore_index, recorded=False, traced=False) -> LogProbs:
+    """`recorded`: called by the node that a recorder sees; `traced`: make that node where torch.jit.trace records."""
     native = _native_calls()
     if native:
         done = native.log_probs(logits, targets, top, ignore_index)
         if done is not None:
             return LogProbs(*done)
+    if not recorded:
+        if traced and torch.jit.is_tracing():
+            return LogProbs(*_LogProbs.apply(logits, targets, top, ignore_index))
+        _refuse_recorders("log_probs", logits)
     with torch.no_grad():
         d, targets = _head_operands(logits, targets, top, ignore_index)
         logits, d.row_stride = _readable_rows(logits)
@@ -313,6 +337,7 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
         done = native.log_probs_backward(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index)
         if done is not None:
             return done
+    _refuse_recorders("log_probs_backward", logits, lse, entropy, grad_logp, grad_entropy)
     with torch.no_grad():
         d, targets = _head_operands(logits, targets, 0, ignore_index)
         rows = logits.shape[0]
@@ -341,7 +366,7 @@ class _LogProbs(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, targets, top, ignore_index):
-        r = log_probs_forward(logits, targets, top, ignore_index)
+        r = _run_log_probs(logits, targets, top, ignore_index, recorded=True)
         ctx.save_for_backward(logits, targets, r.lse, r.entropy)
         ctx.ignore_index = ignore_index
         ctx.set_materialize_grads(False)
@@ -363,4 +388,4 @@ def log_probs(logits, targets=None, top: int = 0, ignore_index: int = -100) -> L
         return handle_torch_function(log_probs, (logits, targets), logits, targets, top, ignore_index)
     if torch.is_grad_enabled() and logits.requires_grad:
         return LogProbs(*_LogProbs.apply(logits, targets, top, ignore_index))
-    return log_probs_forward(logits, targets, top, ignore_index)
+    return _run_log_probs(logits, targets, top, ignore_index, traced=True)
