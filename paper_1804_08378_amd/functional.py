@@ -9,6 +9,7 @@ torch's functions overrides these too: `torch.fx` records a call of one of them 
 from __future__ import annotations
 
 import ctypes as C
+import operator
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -49,6 +50,14 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     if code is None:
         raise TypeError(f"{what}: float32, bfloat16 and float16 tensors, not {t.dtype}")
     return code
+
+
+def _integer(v, what: str, bits: int = 32) -> int:
+    """Fields of the C descriptions cut numbers off without a word."""
+    v = operator.index(v)
+    if not -1 << bits - 1 <= v < 1 << bits - 1:
+        raise ValueError(f"{what}: {v} does not fit {bits} bits")
+    return v
 
 
 def _on_gpu(t: torch.Tensor, what: str) -> None:
@@ -103,7 +112,7 @@ def _norm_operands(x, groups, weight, bias, residual, activation, eps, grad=None
         raise ValueError(f"group_norm: activation {activation!r}, not one of {', '.join(ACTIVATIONS)}")
     d = bs.bs_group_norm_desc()
     d.dtype = _dtype(x, "group_norm")
-    d.groups, d.activation, d.eps = int(groups), ACTIVATIONS[activation], float(eps)
+    d.groups, d.activation, d.eps = _integer(groups, "group_norm: groups"), ACTIVATIONS[activation], float(eps)
     d.shape[:] = x.shape
     d.param_dtype = bs.BS_F32
     params = [p for p in (weight, bias) if p is not None]
@@ -144,7 +153,7 @@ def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stat
         if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or step is None:
             raise ValueError("group_norm: out must have x's shape, type and device, channels last or a channel slice of such a tensor")
         d.y_stride = step
-    stats = torch.empty((x.shape[0], max(1, int(groups)), 2), dtype=torch.float32, device=x.device) if keep_stats else None
+    stats = torch.empty((x.shape[0], max(1, min(d.groups, x.shape[1])), 2), dtype=torch.float32, device=x.device) if keep_stats else None
     if x.numel() == 0 and x.shape[0] == 0:
         return out, stats  # no images
     n = bs.bs_group_norm_workspace_bytes(d, False)
@@ -273,7 +282,7 @@ def _head_operands(logits, targets, top, ignore_index):
             raise ValueError("log_probs: targets hold one int64 or int32 class a row, on the logits' device")
         targets = targets.contiguous()
     d.target_bytes = 4 if targets is not None and targets.dtype == torch.int32 else 8
-    d.ignore_index, d.top, d.lse_bytes = int(ignore_index), int(top), 8
+    d.ignore_index, d.top, d.lse_bytes = _integer(ignore_index, "log_probs: ignore_index", 64), _integer(top, "log_probs: top"), 8
     return d, targets
 
 
