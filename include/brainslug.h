@@ -563,8 +563,8 @@ BS_API bs_status bs_group_norm_backward(const bs_group_norm_desc *desc, const vo
  * in one pass over the logits, and the gradient of logp and entropy.  Sums are float32.
  * A class at -infinity (masked) has probability 0 and adds nothing to the entropy.  In a row where every class is masked, logp and top_logp
  * are -infinity, the entropy is 0 and the gradient 0.  NaN or +infinity among the logits makes the row's results NaN; NaN ranks first.
- * A target equal to ignore_index has logp 0 and no gradient; any other target outside 0 .. classes - 1 has logp and gradient NaN
- * (nothing is read through it).
+ * A target equal to ignore_index has logp 0 and no gradient; any other target outside 0 .. classes - 1 has logp and gradient NaN,
+ * also where every class is masked (nothing is read through it).
  */
 #define BS_MAX_TOP 32
 

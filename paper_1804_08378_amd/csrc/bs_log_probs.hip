@@ -570,11 +570,12 @@ __global__ __launch_bounds__(256) void log_probs_backward_kernel(LogProbsK k)
     const float H = k.entropy ? k.entropy[row] : 0.0f, h = k.grad_entropy ? k.grad_entropy[row] : 0.0f;
     const int64_t c = k.targets ? target_of(k, row) : k.ignore_index;
     float g = k.grad_logp && c != k.ignore_index ? k.grad_logp[row] : 0.0f;
-    if (c != k.ignore_index && (c < 0 || c >= (int64_t)k.classes)) g = __builtin_nanf("");
+    const bool bad = c != k.ignore_index && (c < 0 || c >= (int64_t)k.classes);
+    if (bad) g = __builtin_nanf("");
     const bool none = lse == -INFINITY;
     const uint32_t target = c >= first && c < (int64_t)(first + n) ? (uint32_t)(c - first) : 0xffffffffu;
-    // none: -p (0 - 0) of p = 2^-infinity, without a test in the loop
-    const float gh = none ? 0.0f : __builtin_fmaf(h, H, g), hd = none ? 0.0f : h, off = none ? INFINITY : lse;
+    // none: -p (0 - 0) of p = 2^-infinity, without a test in the loop; a target that is no class makes NaN there too
+    const float gh = none ? (bad ? g : 0.0f) : __builtin_fmaf(h, H, g), hd = none ? 0.0f : h, off = none ? INFINITY : lse;
     low = none ? 0.0f : low;
     // 16-bit results hide the last bits of the exponential; low takes part in its multiply-add
     const float low2 = -low * LOG2E, gh_low = DT == DT_F32 ? gh : __builtin_fmaf(-hd, low, gh);

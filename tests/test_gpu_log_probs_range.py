@@ -206,3 +206,16 @@ def test_lse_sizes_that_are_refused():
         with pytest.raises(bs.BrainSlugError) as e:
             bs.bs_log_probs_backward(d, x, t, at, 0, logp, 0, x, 0) if status != 12 else bs.bs_log_probs_backward(d, x, t, x + 392, 0, logp, 0, x, 0)
         assert e.value.status == status, (size, at)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("classes", [70, 5003, 60001])
+def test_targets_that_are_no_class_in_masked_rows(dtype, classes):
+    """NaN like everywhere else; ignored targets and classes of such rows: no gradient."""
+    x = torch.full((5, classes), -math.inf, dtype=DTYPES[dtype], device="cuda")
+    t = torch.tensor([0, classes, -1, -100, classes - 1]).cuda()
+    r = F.log_probs_forward(x, t)
+    dx = F.log_probs_backward(x, t, r.lse, r.entropy, torch.ones(5, device="cuda"), torch.ones(5, device="cuda"))
+    for i, bad in enumerate((False, True, True, False, False)):
+        assert bool(torch.isnan(r.logp[i])) == bad and r.entropy[i] == 0
+        assert torch.isnan(dx[i]).all() if bad else not dx[i].any(), i
