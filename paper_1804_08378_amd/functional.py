@@ -153,6 +153,7 @@ def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stat
         if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or step is None:
             raise ValueError("group_norm: out must have x's shape, type and device, channels last or a channel slice of such a tensor")
         d.y_stride = step
+        torch.autograd.graph.increment_version(out)  # (written through its pointer, which autograd does not see)
     stats = torch.empty((x.shape[0], max(1, min(d.groups, x.shape[1])), 2), dtype=torch.float32, device=x.device) if keep_stats else None
     if x.numel() == 0 and x.shape[0] == 0:
         return out, stats  # no images
@@ -362,6 +363,8 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
             out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
         elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or _row_stride(out) is None:
             raise ValueError("log_probs_backward: out must have the logits' shape, type and device, its classes contiguous")
+        else:
+            torch.autograd.graph.increment_version(out)  # (written through its pointer, which autograd does not see)
         d.grad_row_stride = _row_stride(out)
         logits, d.row_stride = _readable_rows(logits)
         with torch.cuda.device(logits.device):

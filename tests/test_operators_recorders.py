@@ -103,3 +103,26 @@ def test_single_passes_are_not_traced():
                     (lambda v: F.log_probs_backward(v, t, r.lse, r.entropy, r.entropy), logits)):
         with torch.no_grad(), pytest.raises(RuntimeError, match="trace"):
             torch.jit.trace(call, v, check_trace=False)
+
+
+def test_results_written_over_a_tensor_that_autograd_keeps():
+    """`out` counts as a change in place: the gradient that needs the old values is refused, not computed from the new ones."""
+    x, w, b, logits, t = operands()
+    r = F.log_probs_forward(logits, t)
+
+    def kept(v):
+        v = v.clone(memory_format=torch.preserve_format)
+        return v, (v * torch.ones_like(v).requires_grad_(True)).sum()
+
+    for like, write in ((x, lambda v: F.group_norm(x, 4, w, b, out=v)), (x, lambda v: F.group_norm_forward(x, 4, w, b, out=v)),
+                        (logits, lambda v: F.log_probs_backward(logits, t, r.lse, r.entropy, r.entropy, out=v)),
+                        (logits, lambda v: F.log_probs_backward(v, t, r.lse, r.entropy, r.entropy, out=v))):
+        v, loss = kept(like)
+        loss.backward()  # nothing written: taken
+        v, loss = kept(like)
+        write(v)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():
+        v = torch.empty_like(x)
+        assert torch.equal(F.group_norm(x, 4, w, b, out=v), F.group_norm(x, 4, w, b))
