@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/PythonFallbackKernel.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
@@ -524,9 +525,9 @@ PyObject *set_operators(PyObject *, PyObject *args)
 
 int32_t dtype_code(at::ScalarType t) { return t == at::kFloat ? BS_F32 : t == at::kBFloat16 ? BS_BF16 : t == at::kHalf ? BS_F16 : -1; }
 
-// Whoever records or derives operations on tensors has to see the Python code's answer: torch.jit.trace, forward-mode derivatives.
+// Whoever records, overrides or derives operations on tensors has to see the Python code's answer: torch.jit.trace, modes, forward-mode derivatives.
 bool dual(const at::Tensor &t) { return t._fw_grad(0).defined(); }
-bool recorders_active() { return modes_active() || torch::jit::tracer::isTracing(); }
+bool recorders_active() { return modes_active() || at::impl::torch_function_mode_enabled() || torch::jit::tracer::isTracing(); }
 
 // A tensor argument that may be None; false: neither (no error set), or one with a forward-mode derivative.
 bool optional_tensor(PyObject *o, at::Tensor &t)

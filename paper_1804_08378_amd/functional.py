@@ -30,8 +30,8 @@ _native = None  # the native calls (csrc/bs_torch.cpp), False: not built for thi
 
 
 def _native_calls():
-    """Every one of them takes the plain case -- tensors that are read in place, on one device, without dispatch modes, forward-mode derivatives
-    or tracing -- and returns None for any other, which the Python code takes or refuses."""
+    """Every one of them takes the plain case -- tensors (no subclasses) that are read in place, on one device, without modes, forward-mode
+    derivatives or tracing -- and returns None for any other, which the Python code hands on, takes or refuses."""
     global _native
     if _native is None:
         with bs._native_lock:
@@ -142,6 +142,8 @@ def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stat
         if done is not None:
             return done if keep_stats else (done, None)
     if not recorded:
+        if has_torch_function_variadic(x, weight, bias, residual):  # (group_norm has looked already)
+            return handle_torch_function(group_norm_forward, (x, weight, bias, residual), x, groups, weight, bias, residual, activation, eps, out)
         if torch.jit.is_tracing() and not keep_stats and out is None:
             return _GroupNorm.apply(x, weight, bias, residual, groups, activation, eps), None
         _refuse_recorders("group_norm", x, weight, bias, residual)
@@ -170,8 +172,6 @@ def group_norm_forward(x, groups: int, weight=None, bias=None, residual=None, ac
     """`(y, stats)`: the forward pass and, N x groups x 2 float32, the means and reciprocal deviations that `group_norm_backward` needs.
     `x` and `residual` are channels last, or channel slices of such tensors (read in place; other memory orders are copied first); `y` is
     channels last, or written to `out`."""
-    if has_torch_function_variadic(x, weight, bias, residual):
-        return handle_torch_function(group_norm_forward, (x, weight, bias, residual), x, groups, weight, bias, residual, activation, eps, out)
     with torch.no_grad():
         return _run_norm(x, groups, weight, bias, residual, activation, eps, out, True)
 
@@ -180,14 +180,14 @@ def group_norm_backward(x, stats, grad, groups: int, weight=None, bias=None, res
                         need=(True, True, True, True)):
     """`(grad_x, grad_weight, grad_bias, grad_residual)` from the gradient `grad` of `group_norm_forward`'s result; `need` says which of
     them are wanted (those of absent operands are None)."""
-    if has_torch_function_variadic(x, stats, grad, weight, bias, residual):
-        return handle_torch_function(group_norm_backward, (x, stats, grad, weight, bias, residual), x, stats, grad, groups, weight, bias, residual,
-                                     activation, eps, need)
     native, act = _native_calls(), ACTIVATIONS.get(activation)
     if native and act is not None:
         done = native.group_norm_backward(x, stats, grad, groups, weight, bias, residual, act, eps, need[0] | need[1] << 1 | need[2] << 2 | need[3] << 3)
         if done is not None:
             return done
+    if has_torch_function_variadic(x, stats, grad, weight, bias, residual):
+        return handle_torch_function(group_norm_backward, (x, stats, grad, weight, bias, residual), x, stats, grad, groups, weight, bias, residual,
+                                     activation, eps, need)
     _refuse_recorders("group_norm_backward", x, stats, grad, weight, bias, residual)
     with torch.no_grad():
         d, x, residual, grad = _norm_operands(x, groups, weight, bias, residual, activation, eps, grad)
@@ -302,8 +302,6 @@ def _readable_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
 def log_probs_forward(logits, targets=None, top: int = 0, ignore_index: int = -100) -> LogProbs:
     """Log probabilities of `targets`, entropy and `top` best classes of every row of `logits` (rows x classes; rows may lie further apart
     than they are long).  What masked classes, empty rows and ignored targets give stands at bs_log_probs in include/brainslug.h."""
-    if has_torch_function_variadic(logits, targets):
-        return handle_torch_function(log_probs_forward, (logits, targets), logits, targets, top, ignore_index)
     return _run_log_probs(logits, targets, top, ignore_index)
 
 
@@ -315,6 +313,8 @@ def _run_log_probs(logits, targets, top, ignore_index, recorded=False, traced=Fa
         if done is not None:
             return LogProbs(*done)
     if not recorded:
+        if has_torch_function_variadic(logits, targets):  # (log_probs has looked already)
+            return handle_torch_function(log_probs_forward, (logits, targets), logits, targets, top, ignore_index)
         if traced and torch.jit.is_tracing():
             return LogProbs(*_LogProbs.apply(logits, targets, top, ignore_index))
         _refuse_recorders("log_probs", logits)
@@ -339,14 +339,14 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient with respect to the logits from those of `logp` and `entropy` (a float a row; None: zero).  `lse` as `log_probs_forward` gives
     it; rounded to float32 it is taken too, and probabilities are off by that rounding.  `out=logits` writes the gradient over the logits."""
-    if has_torch_function_variadic(logits, targets, lse, entropy, grad_logp, grad_entropy):
-        return handle_torch_function(log_probs_backward, (logits, targets, lse, entropy, grad_logp, grad_entropy), logits, targets, lse, entropy,
-                                     grad_logp, grad_entropy, ignore_index, out)
     native = _native_calls()
     if native and out is None:
         done = native.log_probs_backward(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index)
         if done is not None:
             return done
+    if has_torch_function_variadic(logits, targets, lse, entropy, grad_logp, grad_entropy):
+        return handle_torch_function(log_probs_backward, (logits, targets, lse, entropy, grad_logp, grad_entropy), logits, targets, lse, entropy,
+                                     grad_logp, grad_entropy, ignore_index, out)
     _refuse_recorders("log_probs_backward", logits, lse, entropy, grad_logp, grad_entropy)
     with torch.no_grad():
         d, targets = _head_operands(logits, targets, 0, ignore_index)

@@ -144,3 +144,31 @@ def test_tensor_subclasses_stay():
     x = torch.randn(2, 8, 5, 5, device="cuda").contiguous(memory_format=torch.channels_last)
     y = F.group_norm(x.as_subclass(Marked), 2)
     assert type(y) is Marked and torch.equal(y.as_subclass(torch.Tensor), F.group_norm(x, 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_modes_see_every_call(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(F, "_native", False)
+
+    class Seen(torch.overrides.TorchFunctionMode):
+        def __init__(self):
+            super().__init__()
+            self.calls = []
+
+        def __torch_function__(self, func, types, args=(), kwargs=None):
+            if func.__module__ == F.__name__:
+                self.calls.append(func)
+            return func(*args, **(kwargs or {}))
+
+    x, logits, t = torch.randn(2, 8, 5, 5, device="cuda"), torch.randn(3, 50, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    with Seen() as mode, Seen() as inner:
+        y = F.group_norm(x, 2)
+        same, stats = F.group_norm_forward(x, 2)
+        F.group_norm_backward(x, stats, y, 2)
+        r = F.log_probs(logits, t, 3)
+        F.log_probs_forward(logits, t)
+        F.log_probs_backward(logits, t, r.lse, r.entropy, r.entropy)
+    assert mode.calls == inner.calls == [F.group_norm, F.group_norm_forward, F.group_norm_backward, F.log_probs, F.log_probs_forward, F.log_probs_backward]
+    assert torch.equal(y, same) and torch.equal(y, F.group_norm(x, 2)) and torch.equal(r.lse, F.log_probs(logits, t, 3).lse)
