@@ -638,7 +638,6 @@ void launch(const LogProbsK &k, int threads, hipStream_t st)
         log_probs_join_kernel<DT, TOP><<<dim3((uint32_t)k.rows), dim3(256), 0, st>>>(k);
     } else if (threads == 64) {
         log_probs_kernel<DT, 64, TOP, false><<<grid, dim3(64), 0, st>>>(k);
-
     } else {
         log_probs_kernel<DT, 256, TOP, false><<<grid, dim3(256), 0, st>>>(k);
     }

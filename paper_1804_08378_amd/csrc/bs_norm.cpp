@@ -61,9 +61,10 @@ bool split_resident(const bs_group_norm_desc &d, int vec, bool backward, bool re
     // backward, the chunks' sums of a channel stay small beside its pixels: 8 bytes for at least 256 of them, or few chunks
     const uint64_t small_sums = backward ? std::max<uint64_t>(16, k.P * es / 256) : 128;
     // A block: whole groups and whole vectors, a divisor of the channels, at least a cache line of every pixel.  Blocks that begin inside cache
-    // lines share them with their neighbours, and read them twice: in tensors of 16 MiB on the smallest block that does so for a sixth of its
-    // lines at most (9x288x83x83 binary16 forward 47.7 -> 25.7 us, 7x336x143x143 both directions 183 -> 157), in smaller ones the smallest of all
-    // (8x640x32x32 binary16 forward 12.7 us, 18.3 in such blocks, whose chunks are few pixels).
+    // lines share them with their neighbours, and read them twice (a block that begins at any 16 bytes touches 128 - 16 = 112 bytes more than
+    // its own on average): in tensors of 16 MiB on the smallest block for which that is a sixth of it at most (9x288x83x83 binary16 forward
+    // 47.7 -> 25.7 us, 7x336x143x143 both directions 183 -> 157), in smaller ones the smallest of all (8x640x32x32 binary16 forward 12.7 us,
+    // 18.3 in such blocks, whose chunks are few pixels).
     const uint64_t unit = std::lcm((uint64_t)k.per, (uint64_t)vec), units = k.C / unit;
     uint64_t most = 0, lanes = 0, groups = 0;
     bool found = false;

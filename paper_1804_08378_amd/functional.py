@@ -245,7 +245,8 @@ def group_norm(x, groups: int, weight=None, bias=None, residual=None, activation
 
 class GroupNormAct(nn.GroupNorm):
     """`nn.GroupNorm` (same parameters, same state dict) with an activation behind it and an optional residual operand in front of the
-    activation: `m(x)`, `m(x, residual)`."""
+    activation: `m(x)`, `m(x, residual)`.  Unlike it, x is 4-D, the parameters are contiguous, and the result is channels last whatever x's
+    memory order (other orders than channels last are copied first)."""
 
     def __init__(self, num_groups: int, num_channels: int, activation: str = "relu", eps: float = 1e-5, affine: bool = True, device=None, dtype=None):
         super().__init__(num_groups, num_channels, eps, affine, device=device, dtype=dtype)
