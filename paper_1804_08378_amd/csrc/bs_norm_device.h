@@ -17,7 +17,8 @@ BS_DEV float sigmoid(float z)
 }
 
 // The normal distribution function and its derivative times z.  16-bit results: the complementary error function by the rational approximation
-// of Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7, the exponential shared with the density):
+// of Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7, the exponential shared with the density; of GELU
+// a tenth of a unit in binary16's last place above -3, up to one unit between -5 and -3, under a unit of bfloat16's above -6):
 // both directions of 32x64x68x68 bfloat16 in 8 groups 72.6 us with erff.
 template <int DT>
 BS_DEV float normal(float z, float &density_z)
