@@ -1,0 +1,318 @@
+"""Layer normalisation, gated activations and activation checkpoints in 8 bits, as cases to be measured.
+
+`layer_norm`: rows of features; an optional addend is added first (the sum, rounded to the tensors' type, is a result too), then every row is
+normalised, weight and bias per feature.  `activate`: act(x) * gate, or act(x).  `pack8`: tensors held in 8 bits and brought back.
+
+Held in 8 bits: blocks of 32 neighbouring elements of a row share a step, the power of two 2^(E - 133), E the smallest number for which the block's
+largest magnitude rounds to 127 steps at most (no larger than the type's own largest exponent has it); elements are whole numbers of steps, ties
+to even.  With `held`, the backward pass of the first two reads its operands from that form and uses the values as they are.
+
+Mode "run" is a forward pass, mode "train" a forward and a backward pass that returns the results and every gradient.
+A case of layer_norm: op, rows, features, addend, params (type of weight and bias), held, dtype, mode.  A case of activate: op, rows, features, act,
+gate, held, dtype, mode.  A case of pack8: op, rows, features, dtype.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+ES = {"f32": 4, "bf16": 2, "f16": 2}
+EPS = 1e-5
+BLOCK = 32                                     # elements that share a step
+LARGEST = {"f32": 254, "bf16": 254, "f16": 142}  # E of the type's largest numbers
+
+
+def _norm(name, rows, features, dtype="f32", mode="run", addend=False, held=False, params="f32"):
+    case = {"op": "layer_norm", "rows": rows, "features": features, "addend": addend, "params": params, "held": held, "dtype": dtype, "mode": mode}
+    return {"name": name, **case} if name else case
+
+
+def _act(name, rows, features, act, dtype="f32", mode="run", gate=False, held=False):
+    case = {"op": "activate", "rows": rows, "features": features, "act": act, "gate": gate, "held": held, "dtype": dtype, "mode": mode}
+    return {"name": name, **case} if name else case
+
+
+def _pack(name, rows, features, dtype):
+    case = {"op": "pack8", "rows": rows, "features": features, "dtype": dtype}
+    return {"name": name, **case} if name else case
+
+
+def listed():
+    return [
+        # one token of a decoding step, behind an addition: a call whose time is its launch
+        _norm("norm_run_token_bf16", 1, 4096, "bf16", addend=True),
+        # a long prompt, or a batch of them, behind an addition
+        _norm("norm_run_prompt_bf16", 8192, 4096, "bf16", addend=True),
+        # a training step's rows, float32
+        _norm("norm_train_f32", 8192, 1024, "f32", "train"),
+        # the same in 16 bits with the addition in front, its operand kept in 8 bits for the backward pass
+        _norm("norm_train_held_bf16", 16384, 2048, "bf16", "train", addend=True, held=True),
+        # the pixels of a batch of images, channels last: very many short rows
+        _norm("norm_train_pixels_bf16", 200704, 256, "bf16", "train"),
+        # odd sizes: rows that begin at any element, parameters in the tensors' type
+        _norm("norm_train_odd_f16", 1001, 771, "f16", "train", addend=True, held=True, params="f16"),
+        # one token between the two products of a gated layer; x and gate are halves of one product's result
+        _act("act_run_token_bf16", 1, 8192, "silu", "bf16", gate=True),
+        # the gated layer of a training step, both operands kept in 8 bits: the most bytes of all
+        _act("act_train_held_bf16", 8192, 8192, "silu", "bf16", "train", gate=True, held=True),
+        # no gate, float32, odd sizes: the last block of a row is short
+        _act("act_train_odd_f32", 3001, 4099, "gelu", "f32", "train", held=True),
+        # one feature map of a small request or a small network
+        _pack("pack_small_f32", 60, 1073, "f32"),
+        # a feature map of a batch in training, channels last, that a convolution keeps for its weight's gradient
+        _pack("pack_map_bf16", 200704, 256, "bf16"),
+        # a text's hidden states at an odd width
+        _pack("pack_odd_f16", 2047, 5003, "f16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op, dtype, mode = rng.choice(["layer_norm", "layer_norm", "activate", "pack8"]), rng.choice(list(DTYPES)), rng.choice(["run", "train"])
+    # rows of a few features make the gradient through their statistics a difference of nearly equal numbers
+    features = _log(rng, 16, 32768)
+    if rng.random() < 0.5:
+        features = max(16, features // 64 * 64)
+    # no more bytes than the largest listed case has, with seven tensors at most against its six
+    rows = max(1, min(_log(rng, 1, 200000), (110 << 20) // (features * ES[dtype])))
+    held = mode == "train" and rng.random() < 0.6
+    if op == "layer_norm":
+        return _norm(None, rows, features, dtype, mode, rng.random() < 0.5, held, rng.choice(["f32", dtype]))
+    if op == "activate":
+        # a ReLU's gradient jumps at 0, where a rounding decides: in training the smooth activations
+        return _act(None, rows, features, rng.choice(["silu", "gelu"] + ["relu"] * (mode == "run")), dtype, mode, rng.random() < 0.6, held)
+    return _pack(None, rows, features, dtype)
+
+
+def prepare(case, seed):
+    """x with a mean and a spread of its own in every feature, a few of them much wider than the rest, as hidden states have them."""
+    g = torch.Generator(device="cuda").manual_seed(seed * 1000003 + 29)
+    dt, rows, n = DTYPES[case["dtype"]], case["rows"], case["features"]
+
+    def make(spread=1.0):
+        return torch.randn(rows, n, generator=g, device="cuda").mul_(spread).to(dt)
+
+    wide = torch.where(torch.rand(n, generator=g, device="cuda") < 0.01, 8.0, 1.0)
+    spread = (torch.rand(n, generator=g, device="cuda") + 0.5) * wide
+    s = {"case": case}
+    if case["op"] == "layer_norm":
+        mean, pt = torch.randn(n, generator=g, device="cuda") * 0.2, DTYPES[case["params"]]
+        s["x"] = torch.randn(rows, n, generator=g, device="cuda").mul_(spread).add_(mean).to(dt)
+        s["addend"] = make(0.5) if case["addend"] else None
+        s["weight"] = (torch.rand(n, generator=g, device="cuda") + 0.5).to(pt)
+        s["bias"] = (torch.randn(n, generator=g, device="cuda") * 0.1).to(pt)
+        s["grad"] = make() if case["mode"] == "train" else None
+        s["grad_total"] = make() if case["mode"] == "train" and case["addend"] else None
+    elif case["op"] == "activate":
+        if case["gate"]:  # the result of one product, in halves
+            joint = torch.randn(rows, 2 * n, generator=g, device="cuda").mul_(1.5).to(dt)
+            s["x"], s["gate"] = joint[:, :n], joint[:, n:]
+        else:
+            s["x"], s["gate"] = make(1.5), None
+        s["grad"] = make() if case["mode"] == "train" else None
+    else:
+        s["x"] = make(spread)
+    return s
+
+
+# ------------------------------------------------------------------------------------------------ plain forms
+def _power(e):
+    """2^e as float32, from its bits: e between -126 and 127."""
+    return ((e + 127) << 23).view(torch.float32)
+
+
+def _held(x, dtype):
+    """The values that x stands for in 8 bits, float32."""
+    rows, n = x.shape
+    short = -n % BLOCK
+    x = x.float()
+    if short:
+        x = torch.cat([x, x.new_zeros(rows, short)], 1)
+    x = x.view(rows, -1, BLOCK)
+    top = x.abs().amax(2, keepdim=True)
+    e = ((top.view(torch.int32) + 0x10000) >> 23).clamp(max=LARGEST[dtype]) - 133
+    half = e // 2  # in two steps: a power of two and its reciprocal are not always both float32 numbers
+    codes = torch.round(x * _power(-half) * _power(half - e)).clamp(-127, 127)
+    return (codes * _power(half) * _power(e - half)).view(rows, -1)[:, :n]
+
+
+def _plain_norm(s):
+    case = s["case"]
+    dt, pt, n = DTYPES[case["dtype"]], DTYPES[case["params"]], case["features"]
+    total = s["x"] if s["addend"] is None else (s["x"].float() + s["addend"].float()).to(dt)
+    x, weight = total.float(), s["weight"].float()
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    rstd = 1 / torch.sqrt((d * d).mean(1, keepdim=True) + EPS)
+    out = {"y": (d * rstd * weight + s["bias"].float()).to(dt)}
+    if s["addend"] is not None:
+        out["total"] = total
+    if case["mode"] == "run":
+        return out
+    xh = ((_held(total, case["dtype"]) if case["held"] else x) - mean) * rstd
+    dy = s["grad"].float()
+    dxh = dy * weight
+    dx = rstd * (dxh - dxh.mean(1, keepdim=True) - xh * (dxh * xh).mean(1, keepdim=True))
+    if s["grad_total"] is not None:
+        dx = dx + s["grad_total"].float()
+    return {**out, "grad_x": dx.to(dt), "grad_weight": (dy * xh).sum(0).to(pt), "grad_bias": dy.sum(0).to(pt)}
+
+
+def _activation(act, z):
+    """The activation and its derivative."""
+    if act == "relu":
+        return torch.where(z > 0, z, 0.0), (z > 0).float()
+    if act == "silu":
+        p = 1 / (1 + torch.exp(-z))
+        return z * p, p * (1 + z * (1 - p))
+    below = 0.5 * (1 + torch.erf(z * math.sqrt(0.5)))
+    return z * below, below + z * torch.exp(-0.5 * z * z) * (1 / math.sqrt(2 * math.pi))
+
+
+def _plain_act(s):
+    case = s["case"]
+    dt = DTYPES[case["dtype"]]
+    y, _ = _activation(case["act"], s["x"].float())
+    if s["gate"] is not None:
+        y = y * s["gate"].float()
+    out = {"y": y.to(dt)}
+    if case["mode"] == "run":
+        return out
+    kept = [None if t is None else _held(t, case["dtype"]) if case["held"] else t.float() for t in (s["x"], s["gate"])]
+    value, slope = _activation(case["act"], kept[0])
+    dy = s["grad"].float()
+    if kept[1] is None:
+        return {**out, "grad_x": (dy * slope).to(dt)}
+    return {**out, "grad_x": (dy * slope * kept[1]).to(dt), "grad_gate": (dy * value).to(dt)}
+
+
+def _plain_pack(s):
+    return {"values": _held(s["x"], s["case"]["dtype"]).to(DTYPES[s["case"]["dtype"]])}
+
+
+# ------------------------------------------------------------------------------------------------ the framework's operators
+def _own_norm(s):
+    from paper_1804_08378_amd import functional as F
+
+    case = s["case"]
+    r = F.layer_norm_forward(s["x"], s["weight"], s["bias"], s["addend"], EPS, checkpoint=case["held"])
+    out = {"y": r.y} if s["addend"] is None else {"y": r.y, "total": r.total}
+    if case["mode"] == "run":
+        return out
+    kept = r.kept if case["held"] else s["x"] if s["addend"] is None else r.total
+    gx, gw, gb = F.layer_norm_backward(kept, r.stats, s["grad"], s["weight"], s["bias"], s["grad_total"])
+    return {**out, "grad_x": gx, "grad_weight": gw, "grad_bias": gb}
+
+
+def _own_act(s):
+    from paper_1804_08378_amd import functional as F
+
+    case = s["case"]
+    r = F.activate_forward(s["x"], case["act"], s["gate"], checkpoint=case["held"])
+    out = {"y": r.y}
+    if case["mode"] == "run":
+        return out
+    x, gate = (r.x, r.gate) if case["held"] else (s["x"], s["gate"])
+    gx, gg = F.activate_backward(x, s["grad"], case["act"], gate)
+    return {**out, "grad_x": gx} if gg is None else {**out, "grad_x": gx, "grad_gate": gg}
+
+
+def _own_pack(s):
+    from paper_1804_08378_amd import functional as F
+
+    return {"values": F.unpack8(F.pack8(s["x"]), s["x"].dtype)}
+
+
+def run(state):
+    if own:
+        return {"layer_norm": _own_norm, "activate": _own_act, "pack8": _own_pack}[state["case"]["op"]](state)
+    return {"layer_norm": _plain_norm, "activate": _plain_act, "pack8": _plain_pack}[state["case"]["op"]](state)
+
+
+def work(case):
+    """Inputs read once, results written once.  Operations per element: addition 1, statistics 4, normalisation and affine 4, the backward pass 14;
+    activation and gate 6, the backward pass 10; to 8 bits 4, back 1."""
+    cells, n, es, train = case["rows"] * case["features"], case["features"], ES[case["dtype"]], case.get("mode") == "train"
+    held = 5 * int(case.get("held", False))
+    if case["op"] == "layer_norm":
+        a, ps = int(case["addend"]), ES[case["params"]]
+        tensors = (4 + 3 * a) if train else (2 + 2 * a)
+        return {"bytes": cells * es * tensors + n * ps * (4 if train else 2), "flops": cells * (8 + a + (14 + held) * train)}
+    if case["op"] == "activate":
+        tensors = (4 + 2 * int(case["gate"])) if train else (2 + int(case["gate"]))
+        return {"bytes": cells * es * tensors, "flops": cells * (6 + (10 + held) * train)}
+    return {"bytes": cells * es * 2, "flops": cells * 5}
+
+
+# ------------------------------------------------------------------------------------------------ the definition in 64 bits
+def _exact_held(x, dtype):
+    """Numbers and their blocks' steps by magnitude: x = m * 2^k with 1/2 <= m < 1."""
+    rows, n = x.shape
+    at = torch.arange(n, device=x.device) // BLOCK
+    top = torch.zeros(rows, int(at[-1]) + 1, dtype=torch.float64, device=x.device)
+    top.scatter_reduce_(1, at.expand(rows, n), x.double().abs(), "amax")
+    m, k = torch.frexp(top)
+    e = torch.where(torch.round(m * 128) > 127, k + 1, k) - 7  # the step's exponent
+    e = torch.where(top > 0, e, -133).clamp(-133, LARGEST[dtype] - 133)
+    step = ((e.long() + 1023) << 52).view(torch.float64)[:, at]
+    return torch.round(x.double() / step).clamp(-127, 127) * step
+
+
+def _exact_norm(case, s):
+    total = s["x"] if s["addend"] is None else s["x"] + s["addend"]
+    x, w, b = total.double(), s["weight"].double(), s["bias"].double()
+    out = {}
+    if s["addend"] is not None:
+        out["total"] = x
+    if case["mode"] == "run" or not case["held"]:
+        train = case["mode"] == "train"
+        leaves = [t.requires_grad_(train) for t in (x.clone(), w, b)]
+        with torch.set_grad_enabled(train):
+            var, mean = torch.var_mean(leaves[0], 1, correction=0, keepdim=True)
+            y = (leaves[0] - mean) / (var + EPS).sqrt() * leaves[1] + leaves[2]
+        out["y"] = y.detach()
+        if train:
+            gx, gw, gb = torch.autograd.grad(y, leaves, s["grad"].double())
+            out.update(grad_x=gx if s["grad_total"] is None else gx + s["grad_total"].double(), grad_weight=gw, grad_bias=gb)
+        return out
+    # the formulas at the held values: the gradient of a row is what the projection that takes ones and xh out leaves of dy * w
+    var, mean = torch.var_mean(x, 1, correction=0, keepdim=True)
+    sd = (var + EPS).sqrt()
+    out["y"] = (x - mean) / sd * w + b
+    xh, dy = (_exact_held(total, case["dtype"]) - mean) / sd, s["grad"].double()
+    u = dy * w
+    n = case["features"]
+    gx = (u - u.sum(1, keepdim=True) / n - xh * ((u * xh).sum(1, keepdim=True) / n)) / sd
+    out.update(grad_x=gx if s["grad_total"] is None else gx + s["grad_total"].double(), grad_weight=(dy * xh).sum(0), grad_bias=dy.sum(0))
+    return out
+
+
+def _exact_act(case, s):
+    f = {"relu": lambda v: v.clamp(min=0), "silu": lambda v: v * torch.sigmoid(v), "gelu": lambda v: v * torch.special.ndtr(v)}[case["act"]]
+    gate = None if s["gate"] is None else s["gate"].double()
+    y = f(s["x"].double())
+    out = {"y": y if gate is None else y * gate}
+    if case["mode"] == "run":
+        return out
+    x = (_exact_held(s["x"], case["dtype"]) if case["held"] else s["x"].double()).requires_grad_(True)
+    leaves = [x]
+    with torch.enable_grad():
+        z = f(x)
+        if gate is not None:
+            leaves.append((_exact_held(s["gate"], case["dtype"]) if case["held"] else gate).requires_grad_(True))
+            z = z * leaves[1]
+    return {**out, **dict(zip(("grad_x", "grad_gate"), torch.autograd.grad(z, leaves, s["grad"].double())))}
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "layer_norm":
+        return _exact_norm(case, s)
+    return _exact_act(case, s) if case["op"] == "activate" else {"values": _exact_held(s["x"], case["dtype"])}
