@@ -4,7 +4,7 @@
 normalised, weight and bias per feature.  `activate`: act(x) * gate, or act(x).  `pack8`: tensors held in 8 bits and brought back.
 
 Held in 8 bits: blocks of 32 neighbouring elements of a row share a step, the power of two 2^(E - 133), E the smallest number for which the block's
-largest magnitude rounds to 127 steps at most (no larger than the type's own largest exponent has it); elements are whole numbers of steps, ties
+largest magnitude is under 126.5 steps (no larger than the type's own largest exponent has it); elements are whole numbers of steps, ties
 to even.  With `held`, the backward pass of the first two reads its operands from that form and uses the values as they are.
 
 Mode "run" is a forward pass, mode "train" a forward and a backward pass that returns the results and every gradient.
@@ -137,9 +137,9 @@ def _held(x, dtype):
         x = torch.cat([x, x.new_zeros(rows, short)], 1)
     x = x.view(rows, -1, BLOCK)
     top = x.abs().amax(2, keepdim=True)
-    e = ((top.view(torch.int32) + 0x10000) >> 23).clamp(max=LARGEST[dtype]) - 133
+    e = ((top.view(torch.int32) + 0x30000) >> 23).clamp(max=LARGEST[dtype]) - 133
     half = e // 2  # in two steps: a power of two and its reciprocal are not always both float32 numbers
-    codes = torch.round(x * _power(-half) * _power(half - e)).clamp(-127, 127)
+    codes = torch.round(x * _power(-half) * _power(half - e)).clamp(-126, 126)
     return (codes * _power(half) * _power(e - half)).view(rows, -1)[:, :n]
 
 
@@ -259,10 +259,10 @@ def _exact_held(x, dtype):
     top = torch.zeros(rows, int(at[-1]) + 1, dtype=torch.float64, device=x.device)
     top.scatter_reduce_(1, at.expand(rows, n), x.double().abs(), "amax")
     m, k = torch.frexp(top)
-    e = torch.where(torch.round(m * 128) > 127, k + 1, k) - 7  # the step's exponent
+    e = torch.where(m * 128 >= 126.5, k + 1, k) - 7  # the step's exponent
     e = torch.where(top > 0, e, -133).clamp(-133, LARGEST[dtype] - 133)
     step = ((e.long() + 1023) << 52).view(torch.float64)[:, at]
-    return torch.round(x.double() / step).clamp(-127, 127) * step
+    return torch.round(x.double() / step).clamp(-126, 126) * step
 
 
 def _exact_norm(case, s):
