@@ -608,6 +608,122 @@ BS_API bs_status bs_log_probs_backward(const bs_log_probs_desc *desc, const void
                                        const float *entropy, const float *grad_logp, const float *grad_entropy, void *grad_logits, void *stream);
 
 /*
+ * Activations held in 8 bits: what training keeps for its backward pass in a half or a quarter of its bytes (Section 7 names training as
+ * the next step; the paper's stacks keep nothing between layers, what is between stacks stays in memory).
+ * Rows of `columns` elements; blocks of 32 neighbouring elements of a row (the row's last may be shorter) share one step, a power of two:
+ *   E     one byte a block, min((B + 3 * 2^16) >> 23, L): B the bits, as float32, of the block's largest finite magnitude, L = 254 (float32,
+ *         bfloat16) or 142 (binary16).  The smallest E for which that magnitude is under 126.5 steps (subnormal numbers:
+ *         125), or the type's largest
+ *   step  2^(E - 133)
+ *   code  one signed byte an element: x / step, ties to even, -126 .. 126; -127, 127: infinite; -128: NaN
+ * An element comes back as code * step, off by half a step at most (under 0.8 % of its block's largest magnitude; two steps where that is over
+ * 126.5 / 128 of the next power of two behind the type's largest numbers); infinities and NaN come back as they were, -0 as +0.  Division by a
+ * power of two is exact, so the codes are the same in any arithmetic.  One number much larger than its block's others takes their precision.
+ * codes are rows x columns bytes, exponents rows x ceil(columns / 32) bytes, both dense.
+ */
+#define BS_PACK8_BLOCK 32
+
+typedef struct bs_pack8_desc {
+    int64_t rows, columns; /* rows may be 0: nothing is enqueued                      */
+    int64_t x_stride;      /* elements from a row to the next; 0 = columns            */
+    int32_t dtype;         /* bs_dtype of x                                           */
+    int32_t reserved;
+} bs_pack8_desc;
+
+/*
+ * Enqueue x -> codes, exponents (bs_pack8) or codes, exponents -> x, rounded to its type (bs_unpack8), on `stream`.  Never synchronises,
+ * never allocates.  x is aligned to its element size.  No output shares a byte with an input or another output.
+ * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, columns < 1, stride below columns), BS_ERR_UNSUPPORTED (type; over 2^30 columns, 2^29 blocks of all
+ *         rows, a stride over 2^40), BS_ERR_ALIGN, BS_ERR_ALIAS, BS_ERR_HIP.
+ */
+BS_API bs_status bs_pack8(const bs_pack8_desc *desc, const void *x, int8_t *codes, uint8_t *exponents, void *stream);
+BS_API bs_status bs_unpack8(const bs_pack8_desc *desc, const int8_t *codes, const uint8_t *exponents, void *x, void *stream);
+
+/*
+ * Activation with an optional gate: y = act(x) * gate, or act(x), over rows of `columns` elements, and the gradients
+ *   grad_x = grad_y * gate * act'(x),  grad_gate = grad_y * act(x).
+ * The forward pass can leave x and gate in 8 bits (above) for the backward pass, which then computes at the values they stand for.
+ * Arithmetic is float32, results are rounded once to the storage type.
+ */
+typedef struct bs_activate_desc {
+    int64_t rows, columns; /* rows may be 0: nothing is enqueued                      */
+    int64_t x_stride, gate_stride, y_stride, grad_y_stride, grad_x_stride, grad_gate_stride; /* elements from a row to the next; 0 = columns */
+    int32_t dtype;         /* bs_dtype of every tensor                                */
+    int32_t activation;    /* bs_activation                                           */
+} bs_activate_desc;
+
+/*
+ * Enqueue the forward pass on `stream`.  Never synchronises, never allocates.
+ *   x, gate                     device (gate NULL: none), aligned to their element size, as are all tensors here
+ *   y                           device, written
+ *   x_codes, x_exponents        device, written: x in 8 bits; both NULL: not wanted
+ *   gate_codes, gate_exponents  the same of gate
+ * No output shares a byte with an input or another output.
+ * Errors: BS_ERR_NULL (x, y; codes without exponents or the other way round; a gate's without a gate), BS_ERR_SHAPE, BS_ERR_UNSUPPORTED (type,
+ *         activation; sizes as bs_pack8), BS_ERR_ALIGN, BS_ERR_ALIAS, BS_ERR_HIP.
+ */
+BS_API bs_status bs_activate(const bs_activate_desc *desc, const void *x, const void *gate, void *y, int8_t *x_codes, uint8_t *x_exponents,
+                             int8_t *gate_codes, uint8_t *gate_exponents, void *stream);
+/*
+ * Enqueue the backward pass.  x (and gate) are read as tensors (x_codes NULL) or from their 8 bits (x NULL); with a gate both are given the same
+ * way.  grad_x, grad_gate may be NULL: not wanted.  Errors: those of bs_activate.
+ */
+BS_API bs_status bs_activate_backward(const bs_activate_desc *desc, const void *x, const int8_t *x_codes, const uint8_t *x_exponents,
+                                      const void *gate, const int8_t *gate_codes, const uint8_t *gate_exponents, const void *grad_y,
+                                      void *grad_x, void *grad_gate, void *stream);
+
+/*
+ * Layer normalisation of rows of `features` elements, with an addition in front of it:
+ *   t = x + addend, rounded to the storage type (no addend: t = x);  mean, var over the row, var without Bessel's correction
+ *   y = (t - mean) / sqrt(var + eps) * weight + bias
+ * and the gradients, with u = grad_y * weight and xh = (t - mean) / sqrt(var + eps), means over the row:
+ *   grad_x = (u - mean(u) - xh * mean(u * xh)) / sqrt(var + eps) + grad_total  (of x and of addend alike; grad_total: the gradient of t itself)
+ *   grad_weight = sum grad_y * xh,  grad_bias = sum grad_y  (over the rows)
+ * The forward pass can leave t in 8 bits (above) for the backward pass, which then takes t for the values they stand for; mean and var are the
+ * forward pass's.  Where a row's mean is many deviations from 0, these values are coarse against its deviations: 2^-8 of the mean.
+ * Statistics, sums and arithmetic are float32, results are rounded once to the storage type.
+ */
+typedef struct bs_layer_norm_desc {
+    int64_t rows, features; /* rows may be 0: gradients of weight and bias are zeros, nothing else is written */
+    int64_t x_stride, addend_stride, total_stride, y_stride, grad_y_stride, grad_total_stride, grad_x_stride; /* elements from a row to the next; 0 = features */
+    double eps;             /* finite, >= 0                                            */
+    int32_t dtype;          /* bs_dtype of every tensor of rows                        */
+    int32_t param_dtype;    /* BS_F32 or dtype: weight, bias and their gradients       */
+} bs_layer_norm_desc;
+
+/*
+ * Enqueue the forward pass on `stream`.  Never synchronises, never allocates.
+ *   x, addend         device (addend NULL: none), aligned to their element size, as are all tensors here
+ *   weight, bias      device, `features` elements each; NULL: ones, zeros
+ *   y                 device, written
+ *   total             device, written: t.  NULL: not wanted
+ *   stats             device, 8-byte aligned, written: mean and 1 / sqrt(var + eps) of every row, floats; NULL: not wanted
+ *   codes, exponents  device, written: t in 8 bits; both NULL: not wanted
+ * No output shares a byte with an input or another output.
+ * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, features < 1, stride below features), BS_ERR_PARAM (eps), BS_ERR_UNSUPPORTED (type; sizes as bs_pack8),
+ *         BS_ERR_ALIGN, BS_ERR_ALIAS, BS_ERR_HIP.
+ */
+BS_API bs_status bs_layer_norm(const bs_layer_norm_desc *desc, const void *x, const void *addend, const void *weight, const void *bias, void *y,
+                               void *total, float *stats, int8_t *codes, uint8_t *exponents, void *stream);
+
+/* Device bytes bs_layer_norm_backward needs as workspace where grad_weight or grad_bias is wanted; 0 for an invalid description. */
+BS_API uint64_t bs_layer_norm_workspace_bytes(const bs_layer_norm_desc *desc);
+
+/*
+ * Enqueue the backward pass.
+ *   t                        device: x, or total where there was an addend; NULL: codes and exponents are read instead
+ *   stats                    device, those of the forward pass
+ *   grad_y, grad_total       device (grad_total NULL: zero)
+ *   grad_x, grad_weight, grad_bias  device, written; each may be NULL: not wanted
+ *   workspace                device, 16-byte aligned, >= bs_layer_norm_workspace_bytes(desc); not needed without grad_weight and grad_bias
+ * Sums are float32, in an order that does not depend on timing: equal calls give equal bits.  No output shares a byte with an input, another
+ * output or the workspace.  Errors: those of bs_layer_norm, BS_ERR_WORKSPACE.
+ */
+BS_API bs_status bs_layer_norm_backward(const bs_layer_norm_desc *desc, const void *t, const int8_t *codes, const uint8_t *exponents,
+                                        const float *stats, const void *weight, const void *grad_y, const void *grad_total, void *grad_x,
+                                        void *grad_weight, void *grad_bias, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
  * Compile, without loading them and without touching any device, all run-time builds the
  * current plan (device or host-only) asks for, for GPU architecture `arch` ("gfx950"; NULL =
  * "gfx950").  A way to check on a machine without a GPU that a stack's kernels build.

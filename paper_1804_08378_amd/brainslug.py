@@ -30,6 +30,7 @@ VARIANT_NAMES = {1: "stream", 2: "pool_direct", 3: "lds_tile", 4: "pool_rows", 5
 BS_LAYOUT_NCHW, BS_LAYOUT_NHWC = 0, 1
 BS_ACT_IDENTITY, BS_ACT_RELU, BS_ACT_SILU, BS_ACT_GELU = 0, 1, 2, 3
 BS_MAX_TOP = 32
+BS_PACK8_BLOCK = 32
 BS_GROUP_NORM_EXCHANGE_BYTES = 4 << 20
 STATUS_NAMES = {
     0: "BS_OK", 1: "BS_ERR_NULL", 2: "BS_ERR_SHAPE", 3: "BS_ERR_PARAM", 4: "BS_ERR_UNSUPPORTED",
@@ -99,6 +100,22 @@ class bs_log_probs_desc(C.Structure):
                 ("lse_bytes", C.c_int32)]
 
 
+class bs_pack8_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("columns", C.c_int64), ("x_stride", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class bs_activate_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("columns", C.c_int64), ("x_stride", C.c_int64), ("gate_stride", C.c_int64), ("y_stride", C.c_int64),
+                ("grad_y_stride", C.c_int64), ("grad_x_stride", C.c_int64), ("grad_gate_stride", C.c_int64),
+                ("dtype", C.c_int32), ("activation", C.c_int32)]
+
+
+class bs_layer_norm_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("features", C.c_int64), ("x_stride", C.c_int64), ("addend_stride", C.c_int64), ("total_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("grad_y_stride", C.c_int64), ("grad_total_stride", C.c_int64), ("grad_x_stride", C.c_int64),
+                ("eps", C.c_double), ("dtype", C.c_int32), ("param_dtype", C.c_int32)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -141,6 +158,13 @@ _SIGNATURES = {
     "bs_log_probs_workspace_bytes": (C.c_uint64, [C.POINTER(bs_log_probs_desc)]),
     "bs_log_probs": (C.c_int, [C.POINTER(bs_log_probs_desc)] + [C.c_void_p] * 8 + [C.c_uint64, C.c_void_p]),
     "bs_log_probs_backward": (C.c_int, [C.POINTER(bs_log_probs_desc)] + [C.c_void_p] * 8),
+    "bs_pack8": (C.c_int, [C.POINTER(bs_pack8_desc)] + [C.c_void_p] * 4),
+    "bs_unpack8": (C.c_int, [C.POINTER(bs_pack8_desc)] + [C.c_void_p] * 4),
+    "bs_activate": (C.c_int, [C.POINTER(bs_activate_desc)] + [C.c_void_p] * 8),
+    "bs_activate_backward": (C.c_int, [C.POINTER(bs_activate_desc)] + [C.c_void_p] * 10),
+    "bs_layer_norm": (C.c_int, [C.POINTER(bs_layer_norm_desc)] + [C.c_void_p] * 10),
+    "bs_layer_norm_workspace_bytes": (C.c_uint64, [C.POINTER(bs_layer_norm_desc)]),
+    "bs_layer_norm_backward": (C.c_int, [C.POINTER(bs_layer_norm_desc)] + [C.c_void_p] * 11 + [C.c_uint64, C.c_void_p]),
     "bs_probe_issue_rate": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
     "bs_probe_stream": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]),
     "bs_stack_jit_check": (C.c_int, [C.c_void_p, C.c_char_p, C.POINTER(C.c_int32)]),
@@ -429,6 +453,40 @@ def bs_log_probs(desc: bs_log_probs_desc, logits, targets, logp, entropy, lse, t
 def bs_log_probs_backward(desc: bs_log_probs_desc, logits, targets, lse, entropy, grad_logp, grad_entropy, grad_logits, stream) -> None:
     _check(load().bs_log_probs_backward(C.byref(desc), logits or None, targets or None, lse or None, entropy or None, grad_logp or None,
                                         grad_entropy or None, grad_logits or None, stream or None), "bs_log_probs_backward")
+
+
+def bs_pack8(desc: bs_pack8_desc, x, codes, exponents, stream) -> None:
+    _check(load().bs_pack8(C.byref(desc), x or None, codes or None, exponents or None, stream or None), "bs_pack8")
+
+
+def bs_unpack8(desc: bs_pack8_desc, codes, exponents, x, stream) -> None:
+    _check(load().bs_unpack8(C.byref(desc), codes or None, exponents or None, x or None, stream or None), "bs_unpack8")
+
+
+def bs_activate(desc: bs_activate_desc, x, gate, y, x_codes, x_exponents, gate_codes, gate_exponents, stream) -> None:
+    _check(load().bs_activate(C.byref(desc), x or None, gate or None, y or None, x_codes or None, x_exponents or None, gate_codes or None,
+                              gate_exponents or None, stream or None), "bs_activate")
+
+
+def bs_activate_backward(desc: bs_activate_desc, x, x_codes, x_exponents, gate, gate_codes, gate_exponents, grad_y, grad_x, grad_gate, stream) -> None:
+    _check(load().bs_activate_backward(C.byref(desc), x or None, x_codes or None, x_exponents or None, gate or None, gate_codes or None,
+                                       gate_exponents or None, grad_y or None, grad_x or None, grad_gate or None, stream or None), "bs_activate_backward")
+
+
+def bs_layer_norm(desc: bs_layer_norm_desc, x, addend, weight, bias, y, total, stats, codes, exponents, stream) -> None:
+    _check(load().bs_layer_norm(C.byref(desc), x or None, addend or None, weight or None, bias or None, y or None, total or None, stats or None,
+                                codes or None, exponents or None, stream or None), "bs_layer_norm")
+
+
+def bs_layer_norm_workspace_bytes(desc: bs_layer_norm_desc) -> int:
+    return int(load().bs_layer_norm_workspace_bytes(C.byref(desc)))
+
+
+def bs_layer_norm_backward(desc: bs_layer_norm_desc, t, codes, exponents, stats, weight, grad_y, grad_total, grad_x, grad_weight, grad_bias,
+                           workspace, workspace_bytes, stream) -> None:
+    _check(load().bs_layer_norm_backward(C.byref(desc), t or None, codes or None, exponents or None, stats or None, weight or None, grad_y or None,
+                                         grad_total or None, grad_x or None, grad_weight or None, grad_bias or None, workspace or None,
+                                         int(workspace_bytes), stream or None), "bs_layer_norm_backward")
 
 
 def bs_stack_plan_backward(handle) -> None:

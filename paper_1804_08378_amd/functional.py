@@ -1,9 +1,11 @@
 """What training a network from scratch needs beside its stacks, on torch tensors: group normalisation with a residual operand and an
-activation (channels last), and the log probabilities at a classifier's end, both with their gradients.
+activation (channels last), the log probabilities at a classifier's end, layer normalisation behind an addition, activations with a gate, each
+with its gradients, and what the backward passes need held in 8 bits.
 
-`group_norm` and `log_probs` are differentiable functions; `GroupNormAct` is the normalisation as a module.  The `_forward` / `_backward`
-pairs are the single passes, for programs that keep their own tape.  Everything runs on the current stream of the tensors' device through the
-C ABI (`bs_group_norm`, `bs_log_probs` in include/brainslug.h); there is no fallback: tensors the library cannot take raise.  What overrides
+`group_norm`, `log_probs`, `layer_norm` and `activate` are differentiable functions; `GroupNormAct` and `LayerNorm` are the normalisations as
+modules.  The `_forward` / `_backward` pairs are the single passes, for programs that keep their own tape.  `pack8` / `unpack8` hold a tensor in 8
+bits; `checkpoints_in_8_bits` holds what autograd keeps for any layer so.  Everything runs on the current stream of the tensors' device through the
+C ABI (`bs_group_norm`, `bs_log_probs`, `bs_layer_norm`, `bs_activate`, `bs_pack8` in include/brainslug.h); there is no fallback: tensors the library cannot take raise.  What overrides
 torch's functions overrides these too: `torch.fx` records a call of one of them as one node, so `optimize_graph` and `capture` take models with them.
 """
 from __future__ import annotations
@@ -20,7 +22,8 @@ from torch.overrides import handle_torch_function, has_torch_function_variadic
 from . import brainslug as bs
 
 __all__ = ["group_norm", "group_norm_forward", "group_norm_backward", "GroupNormAct", "log_probs", "log_probs_forward", "log_probs_backward",
-           "LogProbs", "ACTIVATIONS"]
+           "LogProbs", "layer_norm", "layer_norm_forward", "layer_norm_backward", "LayerNormed", "LayerNorm", "activate", "activate_forward",
+           "activate_backward", "Activated", "pack8", "unpack8", "Packed8", "checkpoints_in_8_bits", "ACTIVATIONS"]
 
 ACTIVATIONS = {"identity": bs.BS_ACT_IDENTITY, "relu": bs.BS_ACT_RELU, "silu": bs.BS_ACT_SILU, "gelu": bs.BS_ACT_GELU}
 _DTYPES = {torch.float32: bs.BS_F32, torch.bfloat16: bs.BS_BF16, torch.float16: bs.BS_F16}
@@ -68,7 +71,7 @@ def _on_gpu(t: torch.Tensor, what: str) -> None:
 def _refuse_recorders(what: str, *tensors: Optional[torch.Tensor]) -> None:
     """Results are written through pointers: whoever records or derives operations on tensors would see an empty tensor and nothing else."""
     if torch.jit.is_tracing():
-        raise RuntimeError(f"{what}: torch.jit.trace records calls of group_norm and log_probs, not the single passes, nor calls with out")
+        raise RuntimeError(f"{what}: torch.jit.trace records calls of the differentiable functions, not the single passes, nor calls with out")
     if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
         raise NotImplementedError(f"{what} has no forward-mode derivatives")
 
@@ -402,3 +405,427 @@ def log_probs(logits, targets=None, top: int = 0, ignore_index: int = -100) -> L
     if torch.is_grad_enabled() and logits.requires_grad:
         return LogProbs(*_LogProbs.apply(logits, targets, top, ignore_index))
     return _run_log_probs(logits, targets, top, ignore_index, traced=True)
+
+
+# ------------------------------------------------------------------------------------------------ rows
+def _rows(t: torch.Tensor) -> Optional[Tuple[int, int]]:
+    """Rows (all dimensions but the last) of a tensor whose rows are contiguous and follow each other at one distance, and that distance; else
+    None.  Nothing reads a tensor without elements."""
+    columns = t.shape[-1]
+    if t.numel() == 0:
+        return t.numel() // max(1, columns), columns
+    if columns > 1 and t.stride(-1) != 1:
+        return None
+    rows, step = 1, None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size > 1:
+            if step is not None and stride != rows * step:
+                return None
+            step = stride if step is None else step
+            rows *= size
+    step = columns if step is None else step
+    return (rows, step) if step >= columns else None
+
+
+def _readable_rows_of(t: Optional[torch.Tensor]) -> Tuple[Optional[torch.Tensor], int]:
+    """`t` and the distance of its rows; a copy where it cannot be read in place."""
+    if t is None:
+        return None, 0
+    found = _rows(t)
+    if found is None:
+        t = t.contiguous()
+        found = _rows(t)
+    return t, found[1]
+
+
+def _row_operand(x: torch.Tensor, what: str) -> None:
+    _on_gpu(x, what)
+    if x.dim() < 1:
+        raise ValueError(f"{what} needs rows: a tensor of one dimension at least")
+
+
+def _alike(t: Optional[torch.Tensor], x: torch.Tensor, what: str) -> None:
+    if t is not None and (t.shape != x.shape or t.dtype != x.dtype or t.device != x.device):
+        raise ValueError(f"{what} must have the other operand's shape, type and device (no broadcasting)")
+
+
+class Packed8(NamedTuple):
+    """Rows in 8 bits (bs_pack8 in include/brainslug.h): `codes`, int8, of the rows' shape, `exponents`, uint8, one for every 32 neighbouring
+    elements of a row."""
+    codes: torch.Tensor
+    exponents: torch.Tensor
+
+
+def _empty_packed(x: torch.Tensor) -> Packed8:
+    columns = x.shape[-1]
+    return Packed8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+                   torch.empty((*x.shape[:-1], -(-columns // bs.BS_PACK8_BLOCK)), dtype=torch.uint8, device=x.device))
+
+
+def _packed_operand(p, what: str) -> Packed8:
+    codes, exponents = p
+    _row_operand(codes, what)
+    if codes.dtype != torch.int8 or exponents.dtype != torch.uint8 or codes.device != exponents.device or \
+            tuple(exponents.shape) != (*codes.shape[:-1], -(-codes.shape[-1] // bs.BS_PACK8_BLOCK)):
+        raise ValueError(f"{what}: int8 codes and uint8 exponents, one for every 32 of a row, on one device, as pack8 gives them")
+    return Packed8(codes.contiguous(), exponents.contiguous())
+
+
+def _parts(t) -> tuple:
+    """The tensors of an operand that is one tensor or a Packed8 (or None)."""
+    return tuple(t) if isinstance(t, tuple) else (t,)
+
+
+def _stream(t: torch.Tensor) -> int:
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+# ------------------------------------------------------------------------------------------------ 8 bits
+def _pack8_desc(x: torch.Tensor, dtype: int, step: int):
+    d = bs.bs_pack8_desc()
+    d.rows, d.columns = x.numel() // max(1, x.shape[-1]), x.shape[-1]
+    d.x_stride, d.dtype = step, dtype
+    return d
+
+
+def pack8(x) -> Packed8:
+    """`x` in 8 bits, 33 bytes for 32 elements of a row (its last dimension): whole numbers of a step, the power of two by which the largest of the
+    32 has 63 to 126 steps.  Elements are off by half a step at most, under 0.8 % of that largest one; infinities and NaN stay."""
+    if has_torch_function_variadic(x):
+        return handle_torch_function(pack8, (x,), x)
+    _refuse_recorders("pack8", x)
+    with torch.no_grad():
+        _row_operand(x, "pack8")
+        dtype = _dtype(x, "pack8")
+        x, step = _readable_rows_of(x)
+        out = _empty_packed(x)
+        with torch.cuda.device(x.device):
+            bs.bs_pack8(_pack8_desc(x, dtype, step), x.data_ptr(), out.codes.data_ptr(), out.exponents.data_ptr(), _stream(x))
+        return out
+
+
+def unpack8(packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """The values that `packed` (a Packed8) stands for, rounded to `dtype`; types that `pack8` takes hold those of their own tensors exactly."""
+    if has_torch_function_variadic(*packed):
+        return handle_torch_function(unpack8, tuple(packed), packed, dtype)
+    _refuse_recorders("unpack8")
+    with torch.no_grad():
+        codes, exponents = _packed_operand(packed, "unpack8")
+        if dtype not in _DTYPES:
+            raise TypeError(f"unpack8: float32, bfloat16 and float16 tensors, not {dtype}")
+        out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+        with torch.cuda.device(codes.device):
+            bs.bs_unpack8(_pack8_desc(out, _DTYPES[dtype], out.shape[-1]), codes.data_ptr(), exponents.data_ptr(), out.data_ptr(), _stream(codes))
+        return out
+
+
+def _dense_order(t: torch.Tensor) -> Optional[Tuple[int, ...]]:
+    """The order of dimensions in which a tensor is one block of memory without gaps, else None."""
+    order = tuple(sorted(range(t.dim()), key=lambda i: (t.stride(i), t.shape[i]), reverse=True))
+    step = 1
+    for i in reversed(order):
+        if t.shape[i] > 1:
+            if t.stride(i) != step:
+                return None
+            step *= t.shape[i]
+    return order
+
+
+class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
+    """`with checkpoints_in_8_bits(model): y = model(x)`: what autograd keeps for the backward pass in the block -- convolutions' and linear layers'
+    inputs, the operands of stacks and of the functions here -- is held by `pack8` and brought back when the backward pass asks for it, so that the
+    gradients are those at the values in 8 bits.
+
+    Held so are tensors on the GPU of `pack8`'s types and sizes with at least `least` elements and dense in memory (any order of dimensions); the others
+    stay as they are, and so do the parameters and buffers of `model` (a module, or an iterable of tensors), which are in use anyway.  A tensor that several
+    nodes keep is held once for each.  Not for values of very different size side by side, such as masks of the type's lowest value: 32 neighbours in
+    memory share a step.  Under autocast, whose copies of the weights could not be told from activations, it refuses."""
+
+    def __init__(self, model, least: int = 1 << 14):
+        tensors = [*model.parameters(), *model.buffers()] if isinstance(model, nn.Module) else list(model)
+        least = _integer(least, "checkpoints_in_8_bits: least", 64)
+        memory = {t.untyped_storage().data_ptr() for t in tensors}
+
+        def pack(t):
+            if torch.is_autocast_enabled("cuda"):
+                raise RuntimeError("checkpoints_in_8_bits: not under autocast")
+            # (`tensors` are alive as long as this is: no other memory has their addresses)
+            if not t.is_cuda or t.dtype not in _DTYPES or t.numel() < max(1, least) or type(t) not in (torch.Tensor, nn.Parameter) or \
+                    t.untyped_storage().data_ptr() in memory or torch.jit.is_tracing():
+                return t
+            order = _dense_order(t)
+            if order is None:
+                return t
+            t = t.detach()
+            shape = [t.shape[i] for i in order]
+            columns, inner = 1, len(shape)  # rows of as many dimensions as a call takes
+            while inner and columns * shape[inner - 1] <= 1 << 30:
+                inner -= 1
+                columns *= shape[inner]
+            if t.numel() // columns * -(-columns // bs.BS_PACK8_BLOCK) > 1 << 29:
+                return t
+            return pack8(t.permute(order).reshape(-1, columns)), t.dtype, order, shape
+
+        def unpack(kept):
+            if isinstance(kept, torch.Tensor):
+                return kept
+            packed, dtype, order, shape = kept
+            back = sorted(range(len(order)), key=order.__getitem__)
+            return unpack8(packed, dtype).view(shape).permute(back)
+
+        self._alive = tensors
+        super().__init__(pack, unpack)
+
+
+# ------------------------------------------------------------------------------------------------ layer normalisation
+class LayerNormed(NamedTuple):
+    """`y`; the sum `total` that was normalised (None without an addend); per row mean and reciprocal deviation, float32; what was normalised in 8
+    bits (None: not asked for)."""
+    y: torch.Tensor
+    total: Optional[torch.Tensor]
+    stats: Optional[torch.Tensor]
+    kept: Optional[Packed8]
+
+
+def _row_params(params, like: torch.Tensor, dtype: int) -> int:
+    code = bs.BS_F32
+    given = [p for p in params if p is not None]
+    for p in given:
+        if tuple(p.shape) != (like.shape[-1],) or not p.is_contiguous() or p.device != like.device:
+            raise ValueError("layer_norm: weight and bias hold one element a feature, contiguous, on the rows' device")
+        code = _dtype(p, "layer_norm")
+        if code not in (bs.BS_F32, dtype) or p.dtype != given[0].dtype:
+            raise TypeError("layer_norm: weight and bias are both float32 or both of the rows' type")
+    return code
+
+
+def _layer_norm_desc(like: torch.Tensor, dtype: int, weight, bias, eps: float):
+    d = bs.bs_layer_norm_desc()
+    d.rows, d.features = like.numel() // max(1, like.shape[-1]), like.shape[-1]
+    d.dtype, d.param_dtype, d.eps = dtype, _row_params((weight, bias), like, dtype), float(eps)
+    return d
+
+
+def _run_layer_norm(x, weight, bias, addend, eps, checkpoint, keep_stats, recorded=False) -> LayerNormed:
+    """`recorded`: called by the node that a recorder sees."""
+    if not recorded:
+        if has_torch_function_variadic(x, weight, bias, addend):  # (layer_norm has looked already)
+            return handle_torch_function(layer_norm_forward, (x, weight, bias, addend), x, weight, bias, addend, eps, checkpoint)
+        if torch.jit.is_tracing() and not keep_stats:
+            r = _LayerNorm.apply(x, weight, bias, addend, eps, checkpoint)
+            return LayerNormed(*(r if addend is not None else (r, None)), None, None)
+        _refuse_recorders("layer_norm", x, weight, bias, addend)
+    with torch.no_grad():
+        _row_operand(x, "layer_norm")
+        _alike(addend, x, "layer_norm: addend")
+        d = _layer_norm_desc(x, _dtype(x, "layer_norm"), weight, bias, eps)
+        x, d.x_stride = _readable_rows_of(x)
+        addend, d.addend_stride = _readable_rows_of(addend)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        total = torch.empty(x.shape, dtype=x.dtype, device=x.device) if addend is not None else None
+        stats = torch.empty((*x.shape[:-1], 2), dtype=torch.float32, device=x.device) if keep_stats else None
+        kept = _empty_packed(x) if checkpoint else None
+        with torch.cuda.device(x.device):
+            bs.bs_layer_norm(d, x.data_ptr(), _ptr(addend), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(total), _ptr(stats),
+                             *((0, 0) if kept is None else (kept.codes.data_ptr(), kept.exponents.data_ptr())), _stream(x))
+        return LayerNormed(y, total, stats, kept)
+
+
+def layer_norm_forward(x, weight=None, bias=None, addend=None, eps: float = 1e-5, checkpoint: bool = False) -> LayerNormed:
+    """Rows (the last dimension of `x`) plus those of `addend`, the sum `total` rounded to x's type, normalised: (total - mean) / sqrt(var + eps) *
+    weight + bias, and what `layer_norm_backward` needs; `checkpoint`: that too in 8 bits, `kept`.  Rows may lie further apart than they are long
+    (other memory orders are copied first)."""
+    return _run_layer_norm(x, weight, bias, addend, eps, checkpoint, True)
+
+
+def layer_norm_backward(x, stats, grad, weight=None, bias=None, grad_total=None, need=(True, True, True)):
+    """`(grad_x, grad_weight, grad_bias)`: from what was normalised -- `x`, or `total` where there was an addend, or `kept` -- its `stats`, the gradient
+    `grad` of y and `grad_total` of total (None: zero).  grad_x is the gradient of x and of the addend alike; `need` says which are wanted (those of
+    absent parameters are None)."""
+    tensors = (*_parts(x), stats, grad, weight, bias, grad_total)
+    if has_torch_function_variadic(*tensors):
+        return handle_torch_function(layer_norm_backward, tensors, x, stats, grad, weight, bias, grad_total, need)
+    _refuse_recorders("layer_norm_backward", *tensors)
+    with torch.no_grad():
+        _row_operand(grad, "layer_norm_backward")
+        held = _packed_operand(x, "layer_norm_backward") if isinstance(x, tuple) else None
+        if held is None:
+            _alike(x, grad, "layer_norm_backward: x")
+        elif held.codes.shape != grad.shape or held.codes.device != grad.device:
+            raise ValueError("layer_norm_backward: the codes must have the gradient's shape and device")
+        _alike(grad_total, grad, "layer_norm_backward: grad_total")
+        if tuple(stats.shape) != (*grad.shape[:-1], 2) or stats.dtype != torch.float32 or stats.device != grad.device:
+            raise ValueError("layer_norm_backward: stats must be those of layer_norm_forward")
+        stats = stats.contiguous()
+        d = _layer_norm_desc(grad, _dtype(grad, "layer_norm_backward"), weight, bias, 0.0)
+        if held is None:
+            x, d.x_stride = _readable_rows_of(x)
+        grad, d.grad_y_stride = _readable_rows_of(grad)
+        grad_total, d.grad_total_stride = _readable_rows_of(grad_total)
+        gx = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device) if need[0] else None
+        gw, gb = (torch.empty(p.shape, dtype=p.dtype, device=p.device) if wanted and p is not None else None for wanted, p in zip(need[1:], (weight, bias)))
+        n = bs.bs_layer_norm_workspace_bytes(d) if gw is not None or gb is not None else 0
+        ws = _workspace(n, grad)
+        with torch.cuda.device(grad.device):
+            bs.bs_layer_norm_backward(d, _ptr(x) if held is None else 0, *((0, 0) if held is None else (held.codes.data_ptr(), held.exponents.data_ptr())),
+                                      stats.data_ptr(), _ptr(weight), grad.data_ptr(), _ptr(grad_total), _ptr(gx), _ptr(gw), _ptr(gb), _ptr(ws), n,
+                                      _stream(grad))
+        return gx, gw, gb
+
+
+class _LayerNorm(torch.autograd.Function):
+    """Keeps what was normalised, as it is or in 8 bits, the statistics and the parameters."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, addend, eps, checkpoint):
+        r = _run_layer_norm(x, weight, bias, addend, eps, checkpoint, True, recorded=True)
+        kept = r.kept if checkpoint else (x if addend is None else r.total, None)
+        ctx.save_for_backward(*kept, r.stats, weight, bias)
+        ctx.set_materialize_grads(False)
+        return r.y if addend is None else (r.y, r.total)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad, grad_total=None):
+        kept, exponents, stats, weight, bias = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        if grad is None:
+            return grad_total, None, None, grad_total if need[3] else None, None, None
+        gx, gw, gb = layer_norm_backward(kept if exponents is None else Packed8(kept, exponents), stats, grad, weight, bias, grad_total,
+                                         (need[0] or need[3], need[1], need[2]))
+        return gx if need[0] else None, gw, gb, gx if need[3] else None, None, None
+
+
+def layer_norm(x, weight=None, bias=None, addend=None, eps: float = 1e-5, checkpoint: bool = False):
+    """The rows of `x` normalised, weight and bias per feature; with an `addend` `(y, total)`: the rows of total = x + addend normalised, and total,
+    which a residual network adds to next.  Differentiable in every tensor.  `checkpoint`: autograd keeps the normalised rows in 8 bits instead of
+    in their own type, and the gradients are those at the values these stand for.  See `layer_norm_forward`."""
+    if has_torch_function_variadic(x, weight, bias, addend):
+        return handle_torch_function(layer_norm, (x, weight, bias, addend), x, weight, bias, addend, eps, checkpoint)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, addend)):
+        return _LayerNorm.apply(x, weight, bias, addend, eps, checkpoint)
+    r = _run_layer_norm(x, weight, bias, addend, eps, False, False)
+    return r.y if addend is None else (r.y, r.total)
+
+
+class LayerNorm(nn.LayerNorm):
+    """`nn.LayerNorm` over the last dimension (same parameters, same state dict) with an optional addition in front: `m(x)`, or
+    `y, total = m(x, addend)`.  `checkpoint`: what its backward pass needs is kept in 8 bits."""
+
+    def __init__(self, features: int, eps: float = 1e-5, elementwise_affine: bool = True, bias: bool = True, checkpoint: bool = False, device=None, dtype=None):
+        super().__init__(_integer(features, "LayerNorm: features", 64), eps, elementwise_affine, bias, device=device, dtype=dtype)
+        self.checkpoint = checkpoint
+
+    def forward(self, x: torch.Tensor, addend: Optional[torch.Tensor] = None):
+        if x.shape[-1] != self.normalized_shape[0]:
+            raise ValueError(f"LayerNorm: rows of {x.shape[-1]} features, not {self.normalized_shape[0]}")
+        return layer_norm(x, self.weight, self.bias, addend, self.eps, self.checkpoint)
+
+    def extra_repr(self) -> str:
+        return super().extra_repr() + f", checkpoint={self.checkpoint}"
+
+
+# ------------------------------------------------------------------------------------------------ activations
+class Activated(NamedTuple):
+    """`y`; x and gate in 8 bits (None: not asked for, no gate)."""
+    y: torch.Tensor
+    x: Optional[Packed8]
+    gate: Optional[Packed8]
+
+
+def _activate_desc(like: torch.Tensor, dtype: int, activation: str):
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activate: activation {activation!r}, not one of {', '.join(ACTIVATIONS)}")
+    d = bs.bs_activate_desc()
+    d.rows, d.columns = like.numel() // max(1, like.shape[-1]), like.shape[-1]
+    d.dtype, d.activation = dtype, ACTIVATIONS[activation]
+    return d
+
+
+def _run_activate(x, activation, gate, checkpoint, recorded=False, traced=False) -> Activated:
+    """`recorded`: called by the node that a recorder sees; `traced`: make that node where torch.jit.trace records."""
+    if not recorded:
+        if has_torch_function_variadic(x, gate):  # (activate has looked already)
+            return handle_torch_function(activate_forward, (x, gate), x, activation, gate, checkpoint)
+        if traced and torch.jit.is_tracing():
+            return Activated(_Activate.apply(x, gate, activation, checkpoint), None, None)
+        _refuse_recorders("activate", x, gate)
+    with torch.no_grad():
+        _row_operand(x, "activate")
+        _alike(gate, x, "activate: gate")
+        d = _activate_desc(x, _dtype(x, "activate"), activation)
+        x, d.x_stride = _readable_rows_of(x)
+        gate, d.gate_stride = _readable_rows_of(gate)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        held = tuple(_empty_packed(x) if checkpoint and t is not None else None for t in (x, gate))
+        with torch.cuda.device(x.device):
+            bs.bs_activate(d, x.data_ptr(), _ptr(gate), y.data_ptr(), *(_ptr(t) for h in held for t in (h or (None, None))), _stream(x))
+        return Activated(y, *held)
+
+
+def activate_forward(x, activation: str = "silu", gate=None, checkpoint: bool = False) -> Activated:
+    """act(x) * gate, or act(x); `checkpoint`: x and gate too in 8 bits.  Rows (the last dimension) of either operand may lie further apart than they
+    are long, as in the halves of one product's result (other memory orders are copied first)."""
+    return _run_activate(x, activation, gate, checkpoint)
+
+
+def activate_backward(x, grad, activation: str = "silu", gate=None, need=(True, True)):
+    """`(grad_x, grad_gate)` from the gradient `grad` of `activate_forward`'s result; x and gate both as they were or both in 8 bits (Packed8).
+    `need` says which are wanted (that of an absent gate is None)."""
+    tensors = (*_parts(x), grad, *_parts(gate))
+    if has_torch_function_variadic(*tensors):
+        return handle_torch_function(activate_backward, tensors, x, grad, activation, gate, need)
+    _refuse_recorders("activate_backward", *tensors)
+    with torch.no_grad():
+        _row_operand(grad, "activate_backward")
+        d = _activate_desc(grad, _dtype(grad, "activate_backward"), activation)
+        held = isinstance(x, tuple)
+        if gate is not None and isinstance(gate, tuple) != held:
+            raise ValueError("activate_backward: x and gate both as tensors or both in 8 bits")
+        if held:
+            x, gate = (_packed_operand(t, "activate_backward") if t is not None else None for t in (x, gate))
+            if any(t is not None and (t.codes.shape != grad.shape or t.codes.device != grad.device) for t in (x, gate)):
+                raise ValueError("activate_backward: the codes must have the gradient's shape and device")
+            pointers = [0, *(_ptr(t) for t in x), 0, *(_ptr(t) for t in gate or (None, None))]
+        else:
+            _alike(x, grad, "activate_backward: x")
+            _alike(gate, grad, "activate_backward: gate")
+            x, d.x_stride = _readable_rows_of(x)
+            gate, d.gate_stride = _readable_rows_of(gate)
+            pointers = [x.data_ptr(), 0, 0, _ptr(gate), 0, 0]
+        grad, d.grad_y_stride = _readable_rows_of(grad)
+        gx = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device) if need[0] else None
+        gg = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device) if need[1] and gate is not None else None
+        with torch.cuda.device(grad.device):
+            bs.bs_activate_backward(d, *pointers, grad.data_ptr(), _ptr(gx), _ptr(gg), _stream(grad))
+        return gx, gg
+
+
+class _Activate(torch.autograd.Function):
+    """Keeps x and gate, as they are or in 8 bits."""
+
+    @staticmethod
+    def forward(ctx, x, gate, activation, checkpoint):
+        r = _run_activate(x, activation, gate, checkpoint, recorded=True)
+        kept = (*r.x, *(r.gate or (None, None))) if checkpoint else (x, None, gate, None)
+        ctx.save_for_backward(*kept)
+        ctx.activation = activation
+        return r.y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, x_exponents, gate, gate_exponents = ctx.saved_tensors
+        if x_exponents is not None:
+            x, gate = Packed8(x, x_exponents), None if gate is None else Packed8(gate, gate_exponents)
+        return (*activate_backward(x, grad, ctx.activation, gate, ctx.needs_input_grad[:2]), None, None)
+
+
+def activate(x, activation: str = "silu", gate=None, checkpoint: bool = False):
+    """act(x) * gate, or act(x) without a gate; differentiable in both.  `checkpoint`: autograd keeps x and gate in 8 bits instead of in their own
+    type, and the gradients are those at the values these stand for.  See `activate_forward`."""
+    if has_torch_function_variadic(x, gate):
+        return handle_torch_function(activate, (x, gate), x, activation, gate, checkpoint)
+    if torch.is_grad_enabled() and (x.requires_grad or (gate is not None and gate.requires_grad)):
+        return _Activate.apply(x, gate, activation, checkpoint)
+    return _run_activate(x, activation, gate, False, traced=True).y

@@ -1,0 +1,217 @@
+"""What layer normalisation, activations and the 8-bit form refuse, and which tensors are read in place, without a GPU: nothing is launched, no pointer
+is followed."""
+import ctypes as C
+import itertools
+
+import pytest
+import torch
+
+from paper_1804_08378_amd import brainslug as bs
+from paper_1804_08378_amd import functional as F
+
+NULL, SHAPE, PARAM, UNSUPPORTED, ALIGN, WORKSPACE, ALIAS = 1, 2, 3, 4, 7, 8, 12
+
+
+def norm_desc(rows=6, features=100, dtype=bs.BS_F32, param_dtype=bs.BS_F32, eps=1e-5, **strides):
+    d = bs.bs_layer_norm_desc()
+    d.rows, d.features, d.dtype, d.param_dtype, d.eps = rows, features, dtype, param_dtype, eps
+    for k, v in strides.items():
+        setattr(d, k, v)
+    return d
+
+
+def act_desc(rows=6, columns=100, dtype=bs.BS_F32, activation=bs.BS_ACT_SILU, **strides):
+    d = bs.bs_activate_desc()
+    d.rows, d.columns, d.dtype, d.activation = rows, columns, dtype, activation
+    for k, v in strides.items():
+        setattr(d, k, v)
+    return d
+
+
+def pack_desc(rows=6, columns=100, dtype=bs.BS_F32, x_stride=0):
+    d = bs.bs_pack8_desc()
+    d.rows, d.columns, d.dtype, d.x_stride = rows, columns, dtype, x_stride
+    return d
+
+
+def status(fn, *args):
+    with pytest.raises(bs.BrainSlugError) as e:
+        fn(*args)
+    return e.value.status
+
+
+# addresses that stand for buffers: 1 MiB apart, never followed
+X, A, W, B, Y, T, S, Q, E, GQ, GE, DY, DT, DX, DW, DB, WS = (0x10000000 + i * 0x100000 for i in range(17))
+BIG = 1 << 20
+
+
+def forward(d, x=X, a=A, w=W, b=B, y=Y, t=T, s=S, q=Q, e=E):
+    return status(bs.bs_layer_norm, d, x, a, w, b, y, t, s, q, e, 0)
+
+
+def backward(d, t=T, q=0, e=0, s=S, w=W, dy=DY, dt=DT, dx=DX, dw=DW, db=DB, ws=WS, n=BIG):
+    return status(bs.bs_layer_norm_backward, d, t, q, e, s, w, dy, dt, dx, dw, db, ws, n, 0)
+
+
+def test_layer_norm_refusals():
+    for call in (forward, backward):
+        assert call(norm_desc(rows=-1)) == SHAPE and call(norm_desc(features=0)) == SHAPE
+        assert call(norm_desc(dtype=3)) == UNSUPPORTED and call(norm_desc(param_dtype=bs.BS_F16)) == UNSUPPORTED and call(norm_desc(param_dtype=7)) == UNSUPPORTED
+        assert call(norm_desc(features=(1 << 30) + 1)) == UNSUPPORTED and call(norm_desc(rows=(1 << 29) + 1, features=1)) == UNSUPPORTED
+        assert call(norm_desc(rows=1 << 28, features=65)) == UNSUPPORTED and call(norm_desc(rows=1 << 62, features=1 << 62)) in (SHAPE, UNSUPPORTED)
+        for eps in (-1.0, float("nan"), float("inf")):
+            assert call(norm_desc(eps=eps)) == PARAM
+        for name in ("x_stride", "addend_stride", "total_stride", "y_stride", "grad_y_stride", "grad_total_stride", "grad_x_stride"):
+            assert call(norm_desc(**{name: 99})) == SHAPE and call(norm_desc(**{name: -1})) == SHAPE and call(norm_desc(**{name: 1 << 50})) == UNSUPPORTED
+    d = norm_desc()
+    assert forward(d, x=0) == NULL and forward(d, y=0) == NULL and forward(d, q=0) == NULL and forward(d, e=0) == NULL
+    assert backward(d, t=0) == NULL and backward(d, q=Q, e=E) == NULL and backward(d, t=0, q=Q) == NULL and backward(d, s=0) == NULL and backward(d, dy=0) == NULL
+    assert backward(d, e=E) == NULL
+    assert forward(d, x=X + 2) == ALIGN and forward(d, a=A + 1) == ALIGN and forward(d, w=W + 2) == ALIGN and forward(d, s=S + 4) == ALIGN
+    assert backward(d, t=T + 2) == ALIGN and backward(d, dt=DT + 2) == ALIGN and backward(d, dw=DW + 2) == ALIGN and backward(d, ws=WS + 8) == ALIGN
+    assert backward(d, n=0) == WORKSPACE and backward(d, ws=0) == WORKSPACE
+    need = bs.bs_layer_norm_workspace_bytes(d)
+    assert 0 < need < BIG and backward(d, n=need - 1) == WORKSPACE
+    for out in ("y", "t", "s", "q", "e"):
+        for other in (X, A, W, B):
+            assert forward(d, **{out: other}) == ALIAS
+    assert forward(d, t=Y) == ALIAS and forward(d, q=S) == ALIAS and forward(d, e=Q + 599) == ALIAS and forward(d, x=Y + 2396) == ALIAS
+    for out in ("dx", "dw", "db", "ws"):
+        for other in (T, S, W, DY, DT):
+            assert backward(d, **{out: other}) == ALIAS
+    assert backward(d, dx=DW) == ALIAS and backward(d, dw=DB) == ALIAS and backward(d, t=0, q=DX, e=E) == ALIAS
+    assert forward(norm_desc(y_stride=200, total_stride=200), t=Y + 99 * 4) == ALIAS  # column slices of one buffer that share a column
+    lib = bs.load()
+    assert lib.bs_layer_norm(None, *[None] * 10) == NULL and lib.bs_layer_norm_backward(None, *[None] * 11, 0, None) == NULL
+    assert lib.bs_layer_norm_workspace_bytes(None) == 0 and bs.bs_layer_norm_workspace_bytes(norm_desc(features=0)) == 0
+    assert lib.bs_layer_norm(C.byref(norm_desc(rows=0)), *[None] * 10) == 0  # no rows: nothing to do
+    assert lib.bs_layer_norm_backward(C.byref(norm_desc(rows=0)), *[None] * 11, 0, None) == 0
+    assert backward(norm_desc(rows=0), ws=0) == WORKSPACE
+
+
+@pytest.mark.parametrize("rows,features", [(1, 1), (1, 4096), (8192, 4096), (200704, 256), (1 << 28, 32), (5, 1 << 20), (100000, 20000), (17, 300)])
+def test_layer_norm_workspaces_stay_small(rows, features):
+    """Partial sums: at most a quarter of the tensor, or 8 MiB."""
+    for dtype in (bs.BS_F32, bs.BS_F16):
+        n = bs.bs_layer_norm_workspace_bytes(norm_desc(rows, features, dtype))
+        assert 0 < n <= max(8 << 20, rows * features * 2 // 4 + 16 * features), n
+
+
+def act(d, x=X, g=A, y=Y, q=Q, e=E, gq=GQ, ge=GE):
+    return status(bs.bs_activate, d, x, g, y, q, e, gq, ge, 0)
+
+
+def act_backward(d, x=X, q=0, e=0, g=A, gq=0, ge=0, dy=DY, dx=DX, dg=DW):
+    return status(bs.bs_activate_backward, d, x, q, e, g, gq, ge, dy, dx, dg, 0)
+
+
+def test_activate_refusals():
+    for call in (act, act_backward):
+        assert call(act_desc(rows=-1)) == SHAPE and call(act_desc(columns=0)) == SHAPE
+        assert call(act_desc(dtype=3)) == UNSUPPORTED and call(act_desc(activation=4)) == UNSUPPORTED and call(act_desc(activation=-1)) == UNSUPPORTED
+        assert call(act_desc(columns=(1 << 30) + 1)) == UNSUPPORTED and call(act_desc(rows=1 << 29, columns=33)) == UNSUPPORTED
+        for name in ("x_stride", "gate_stride", "y_stride", "grad_y_stride", "grad_x_stride", "grad_gate_stride"):
+            assert call(act_desc(**{name: 99})) == SHAPE and call(act_desc(**{name: 1 << 50})) == UNSUPPORTED
+        assert call(act_desc(), x=0) == NULL and call(act_desc(), x=X + 2) == ALIGN and call(act_desc(), g=A + 1) == ALIGN
+    d = act_desc()
+    assert act(d, y=0) == NULL and act(d, e=0) == NULL and act(d, q=0) == NULL and act(d, gq=0) == NULL and act(d, ge=0) == NULL
+    assert act(d, q=0, e=0) == NULL and act(d, gq=0, ge=0) == NULL and act(d, g=0) == NULL  # both operands in 8 bits or none; none without a gate
+    for out in ("y", "q", "e", "gq", "ge"):
+        assert act(d, **{out: X}) == ALIAS and act(d, **{out: A}) == ALIAS
+    assert act(d, gq=Q + 599) == ALIAS and act(d, ge=E + 23) == ALIAS and act(d, y=Q - 2396) == ALIAS and act(d, y=Y + 2) == ALIGN
+    assert act_backward(d, dy=0) == NULL and act_backward(d, x=0, q=Q, e=E) == NULL and act_backward(d, q=Q, e=E) == NULL and act_backward(d, e=E) == NULL
+    assert act_backward(d, gq=GQ, ge=GE) == NULL and act_backward(d, g=0) == NULL and act_backward(d, x=0, q=Q, e=E, g=0, gq=GQ) == NULL
+    assert act_backward(d, dx=X) == ALIAS and act_backward(d, dg=A) == ALIAS and act_backward(d, dx=DY) == ALIAS and act_backward(d, dg=DX + 4) == ALIAS
+    assert act_backward(d, x=0, q=DX, e=E, g=0, gq=GQ, ge=GE) == ALIAS
+    lib = bs.load()
+    assert lib.bs_activate(None, *[None] * 8) == NULL and lib.bs_activate_backward(None, *[None] * 10) == NULL
+    assert lib.bs_activate(C.byref(act_desc(rows=0)), *[None] * 8) == 0 and lib.bs_activate_backward(C.byref(act_desc(rows=0)), *[None] * 10) == 0
+
+
+def test_pack8_refusals():
+    pack = lambda d, x=X, q=Q, e=E: status(bs.bs_pack8, d, x, q, e, 0)
+    unpack = lambda d, x=X, q=Q, e=E: status(bs.bs_unpack8, d, q, e, x, 0)
+    for call in (pack, unpack):
+        assert call(pack_desc(rows=-1)) == SHAPE and call(pack_desc(columns=0)) == SHAPE and call(pack_desc(x_stride=99)) == SHAPE
+        assert call(pack_desc(dtype=3)) == UNSUPPORTED and call(pack_desc(columns=(1 << 30) + 1)) == UNSUPPORTED and call(pack_desc(rows=1 << 29, columns=33)) == UNSUPPORTED
+        assert call(pack_desc(), x=0) == NULL and call(pack_desc(), q=0) == NULL and call(pack_desc(), e=0) == NULL
+        assert call(pack_desc(), x=X + 2) == ALIGN and call(pack_desc(), q=X + 2399) == ALIAS and call(pack_desc(), e=X) == ALIAS
+    assert pack(pack_desc(), e=Q + 599) == ALIAS
+    lib = bs.load()
+    assert lib.bs_pack8(None, None, None, None, None) == NULL and lib.bs_unpack8(None, None, None, None, None) == NULL
+    assert lib.bs_pack8(C.byref(pack_desc(rows=0)), None, None, None, None) == 0
+
+
+def test_which_rows_are_read_in_place():
+    """Every element of such a tensor stands where its row and column say."""
+    base = torch.arange(200)
+    taken = 0
+    for size in itertools.product((1, 2, 3), repeat=3):
+        for stride in itertools.product((0, 1, 2, 3, 4, 6, 9, 12), repeat=3):
+            t = torch.as_strided(base, size, stride)
+            found = F._rows(t)
+            if found is not None:
+                rows, step = found
+                assert step >= size[-1] and rows == size[0] * size[1]
+                assert torch.equal(torch.as_strided(base, (rows, size[-1]), (step, 1)), t.reshape(rows, -1)), (size, stride)
+                taken += 1
+            elif t.is_contiguous() or (size[-1] == 1 or stride[-1] == 1) and size[0] == 1 and stride[1] >= size[-1]:
+                pytest.fail(f"a copy of {size} {stride}")
+    assert taken > 1000
+    assert F._rows(torch.zeros(3, 0, 7)) == (0, 7) and F._rows(torch.zeros(7)) == (1, 7) and F._rows(torch.zeros(4, 0)) is not None
+
+
+def test_dense_orders():
+    base = torch.arange(24)
+    for t in (base.view(2, 3, 4), base.view(2, 3, 4).permute(2, 0, 1), base.view(4, 6).t(), base.view(2, 1, 3, 4).permute(0, 3, 1, 2), base, base.view(1, 24, 1)):
+        order = F._dense_order(t)
+        assert torch.equal(t.permute(order).reshape(-1), base)
+    for t in (base.view(4, 6)[:, :5], base[::2], base[:6].expand(4, 6), base.view(4, 6)[::2]):
+        assert F._dense_order(t) is None
+
+
+def test_functions_refuse_what_they_cannot_take():
+    x = torch.zeros(4, 8)
+    for call in (lambda: F.layer_norm(x), lambda: F.layer_norm_forward(x), lambda: F.activate(x), lambda: F.activate_forward(x, "relu", x), lambda: F.pack8(x),
+                 lambda: F.layer_norm_backward(x, torch.zeros(4, 2), x), lambda: F.activate_backward(x, x),
+                 lambda: F.unpack8(F.Packed8(torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8)))):
+        with pytest.raises(RuntimeError, match="GPU"):
+            call()
+    with pytest.raises((TypeError, ValueError)):
+        F.LayerNorm(8.0)
+    with pytest.raises((TypeError, ValueError)):
+        F.checkpoints_in_8_bits(nn_model(), least=1.5)
+
+
+def nn_model():
+    return torch.nn.Linear(2, 2)
+
+
+@pytest.fixture
+def host_tensors(monkeypatch):
+    """Tensors in host memory stand for device tensors; a call that reaches the library fails the test."""
+    monkeypatch.setattr(F, "_native", False)
+    monkeypatch.setattr(F, "_on_gpu", lambda t, what: None)
+    for name in ("bs_layer_norm", "bs_layer_norm_backward", "bs_activate", "bs_activate_backward", "bs_pack8", "bs_unpack8"):
+        monkeypatch.setattr(F.bs, name, lambda *a: pytest.fail("called"))
+
+
+def test_operands_that_do_not_fit(host_tensors):
+    x, w, stats = torch.zeros(4, 8), torch.ones(8), torch.zeros(4, 2)
+    codes, exponents = torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8)
+    packed = F.Packed8(codes, exponents)
+    for error, call in [
+            (ValueError, lambda: F.layer_norm(torch.tensor(1.0))), (TypeError, lambda: F.layer_norm(x.double())), (TypeError, lambda: F.layer_norm(x.int())),
+            (ValueError, lambda: F.layer_norm(x, w[:7])), (ValueError, lambda: F.layer_norm(x, None, torch.ones(16)[::2])), (TypeError, lambda: F.layer_norm(x, w.half())),
+            (TypeError, lambda: F.layer_norm(x.half(), w, w.half())), (ValueError, lambda: F.layer_norm(x, w, w, x[:1])), (ValueError, lambda: F.layer_norm(x, w, w, x.half())),
+            (ValueError, lambda: F.layer_norm_backward(x, stats[:3], x)), (ValueError, lambda: F.layer_norm_backward(x, stats.double(), x)),
+            (ValueError, lambda: F.layer_norm_backward(x[:3], stats, x)), (ValueError, lambda: F.layer_norm_backward(x, stats, x, w, w, x[:, :4])),
+            (ValueError, lambda: F.layer_norm_backward(packed, stats[:2], x[:2])), (ValueError, lambda: F.layer_norm_backward(F.Packed8(codes, exponents[:3]), stats, x)),
+            (ValueError, lambda: F.layer_norm_backward(F.Packed8(codes.to(torch.uint8), exponents), stats, x)),
+            (ValueError, lambda: F.activate(x, "tanh")), (ValueError, lambda: F.activate(x, "silu", x[0])), (TypeError, lambda: F.activate(x.double())),
+            (ValueError, lambda: F.activate_backward(x, x, "silu", packed)), (ValueError, lambda: F.activate_backward(packed, x, "silu", x)),
+            (ValueError, lambda: F.activate_backward(packed, x[:, :4], "silu")), (ValueError, lambda: F.activate_backward(x, x.half(), "silu")),
+            (TypeError, lambda: F.pack8(x.double())), (ValueError, lambda: F.pack8(torch.tensor(1.0))), (TypeError, lambda: F.unpack8(packed, torch.int32)),
+            (ValueError, lambda: F.unpack8(F.Packed8(codes, exponents.int()))), (ValueError, lambda: F.unpack8(F.Packed8(codes, torch.zeros(4, 2, dtype=torch.uint8))))]:
+        with pytest.raises(error):
+            call()
