@@ -13,7 +13,7 @@ TORCH_EXT = os.path.join(HERE, "_bs_torch.so")  # the binding's native calls (cs
 SOURCES = ["bs_stack.cpp", "bs_plan.cpp", "bs_run.cpp", "bs_jit.cpp", "bs_trace.cpp", "bs_kernels.hip", "bs_lds.hip", "bs_rows.hip",
            "bs_rows2.hip", "bs_xrows.hip", "bs_chain.hip", "bs_chain_window.hip", "bs_chain_nhwc.hip", "bs_chain_window_nhwc.hip", "bs_nhwc.hip", "bs_nhwc_tile.hip", "bs_nhwc_rows.hip", "bs_strip.hip", "bs_pool_band.hip", "bs_backward.cpp", "bs_backward.hip", "bs_backward_strip.hip", "bs_probe.hip",
            "bs_norm.cpp", "bs_norm.hip", "bs_norm_resident.hip", "bs_norm_resident_grad.hip", "bs_log_probs.cpp", "bs_log_probs.hip",
-           "bs_layer_norm.cpp", "bs_layer_norm.hip", "bs_activate.cpp", "bs_activate.hip"]
+           "bs_layer_norm.cpp", "bs_layer_norm.hip", "bs_layer_norm_team.hip", "bs_layer_norm_team_grad.hip", "bs_activate.cpp", "bs_activate.hip"]
 # device headers whose text is embedded in the library for run-time (hipRTC) kernel builds
 JIT_HEADERS = ["bs_kargs.h", "bs_device.h", "bs_lds_device.h", "bs_rows_device.h", "bs_xrows_device.h", "bs_chain_device.h", "bs_chain_window_device.h"]
 
@@ -62,7 +62,7 @@ def up_to_date() -> bool:
             os.path.join(CSRC, "bs_torch.cpp"), os.path.join(ROOT, "include", "brainslug.h")))):
         return False
     t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, h) for h in JIT_HEADERS + ["bs_internal.h", "bs_rows_tables.h", "bs_nhwc_device.h", "bs_bwd_device.h", "bs_strip_device.h", "bs_backward_keys.h", "bs_norm.h", "bs_exp_device.h", "bs_norm_device.h", "bs_norm_resident.h", "bs_log_probs.h", "bs_rows_args.h", "bs_rows8_device.h", "bs_layer_norm.h", "bs_activate.h"]]
+    deps = sources() + [os.path.join(CSRC, h) for h in JIT_HEADERS + ["bs_internal.h", "bs_rows_tables.h", "bs_nhwc_device.h", "bs_bwd_device.h", "bs_strip_device.h", "bs_backward_keys.h", "bs_norm.h", "bs_exp_device.h", "bs_norm_device.h", "bs_norm_resident.h", "bs_log_probs.h", "bs_rows_args.h", "bs_rows8_device.h", "bs_layer_norm.h", "bs_layer_norm_team.h", "bs_activate.h"]]
     deps.append(os.path.join(ROOT, "include", "brainslug.h"))
     return all(os.path.getmtime(d) <= t for d in deps)
 

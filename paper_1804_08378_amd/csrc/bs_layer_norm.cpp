@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdint>
 
 using namespace bs;
 
@@ -26,11 +27,32 @@ void fill(const bs_layer_norm_desc &d, LayerNormK &k)
     k.C = (uint32_t)d.features;
     k.f32_params = d.param_dtype == BS_F32;
     k.eps = (float)d.eps;
-    // parts of the rows whose sums are joined by a second launch
-    const uint64_t columns = ceil_div(k.C, 64 * (d.dtype == BS_F32 ? 4 : 8));
-    const uint64_t wanted = std::min<uint64_t>({ceil_div(1024, columns), ceil_div(k.rows, 16), 256});
-    k.per_part = ceil_div(k.rows, std::max<uint64_t>(1, wanted));
-    k.parts = (uint32_t)(k.rows ? ceil_div(k.rows, k.per_part) : 0);
+}
+
+// Lanes that a row takes and their vectors; a row of 16384 elements (forward, 16 bits: 32768) is the longest that registers hold.
+LayerNormTeam team_of(const LayerNormK &k, int32_t dtype, bool backward)
+{
+    const uint64_t vectors = ceil_div(k.C, dtype == BS_F32 ? 4 : 8);
+    LayerNormTeam t{8, 1, 0};
+    while (t.team < 1024 && (uint64_t)t.team < vectors) t.team *= 2;
+    while ((uint64_t)t.team * t.vectors < vectors) t.vectors *= 2;
+    if (t.vectors > (backward && dtype != BS_F32 ? 2 : 4)) return LayerNormTeam{0, 0, 0};
+    const uint64_t threads = backward ? (uint64_t)K_LAYER_NORM_GRAD_THREADS : (uint64_t)(t.team <= 64 ? 256 : t.team), teams = threads / (uint64_t)t.team;
+    t.groups = (uint32_t)std::min<uint64_t>(ceil_div(k.rows, teams), backward ? K_LAYER_NORM_GRAD_GROUPS : 256 * 2048 / threads);
+    return t;
+}
+
+// Parts of the rows, whose sums a second launch joins: what the backward pass's work-groups leave, or of long rows 1024 tiles.
+void parts(LayerNormK &k, const LayerNormTeam &t, int32_t dtype)
+{
+    if (!k.rows) return;
+    if (t.team) {
+        k.parts = t.groups;
+        return;
+    }
+    const uint64_t tiles = ceil_div(k.C, 64 * (dtype == BS_F32 ? 4 : 8));
+    k.per_part = ceil_div(k.rows, std::max<uint64_t>(1, std::min(ceil_div(1024, tiles), ceil_div(k.rows, 16))));
+    k.parts = (uint32_t)ceil_div(k.rows, k.per_part);
 }
 
 uint64_t space(const LayerNormK &k) { return std::max<uint64_t>(16, (uint64_t)k.parts * k.C * 8); }
@@ -64,7 +86,8 @@ bs_status bs_layer_norm(const bs_layer_norm_desc *desc, const void *x, const voi
                                           {bytes_of(k.y, k.rows, C, es), bytes_of(k.total, k.rows, C, es), bytes_of(stats, k.rows * 8),
                                            bytes_of(codes, cells), bytes_of(exponents, k.rows * blocks_of(C))});
     if (alias != BS_OK) return alias;
-    return launch_layer_norm(LAYER_NORM, k, desc->dtype, stream);
+    const LayerNormTeam team = team_of(k, desc->dtype, false);
+    return team.team ? launch_layer_norm_team(k, team, desc->dtype, stream) : launch_layer_norm(LAYER_NORM, k, desc->dtype, stream);
 }
 
 uint64_t bs_layer_norm_workspace_bytes(const bs_layer_norm_desc *desc)
@@ -72,6 +95,7 @@ uint64_t bs_layer_norm_workspace_bytes(const bs_layer_norm_desc *desc)
     if (check_desc(desc) != BS_OK) return 0;
     LayerNormK k{};
     fill(*desc, k);
+    parts(k, team_of(k, desc->dtype, true), desc->dtype);
     return space(k);
 }
 
@@ -95,7 +119,9 @@ bs_status bs_layer_norm_backward(const bs_layer_norm_desc *desc, const void *t, 
     k.dweight = grad_weight;
     k.dbias = grad_bias;
     k.stats = const_cast<float *>(stats);
-    k.part = static_cast<float *>(workspace);
+    k.part = params ? static_cast<float *>(workspace) : nullptr;
+    const LayerNormTeam team = team_of(k, desc->dtype, true);
+    parts(k, team, desc->dtype);
     const uint64_t es = dtype_size(desc->dtype), ps = dtype_size(desc->param_dtype), C = k.C, cells = k.rows * C;
     if (params && (!workspace || workspace_bytes < space(k))) return BS_ERR_WORKSPACE;
     for (const void *p : {t, grad_y, grad_total, (const void *)grad_x})
@@ -109,10 +135,14 @@ bs_status bs_layer_norm_backward(const bs_layer_norm_desc *desc, const void *t, 
                                            bytes_of(params ? workspace : nullptr, space(k))});
     if (alias != BS_OK) return alias;
     bs_status st = BS_OK;
-    if (grad_x && k.rows) st = launch_layer_norm(LAYER_NORM_GRAD, k, desc->dtype, stream);
-    if (st == BS_OK && params && k.rows) st = launch_layer_norm(LAYER_NORM_GRAD_PARTS, k, desc->dtype, stream);
-    if (st == BS_OK && params) st = launch_layer_norm(LAYER_NORM_GRAD_JOIN, k, desc->dtype, stream);
-    return st;
+    if (k.rows && team.team) {
+        if (grad_x || params) st = launch_layer_norm_team_grad(k, team, desc->dtype, stream);
+        if (st != BS_OK || !params || k.parts == 1) return st;  // (one work-group writes the parameters' gradients itself)
+    } else if (k.rows) {
+        if (grad_x) st = launch_layer_norm(LAYER_NORM_GRAD, k, desc->dtype, stream);
+        if (st == BS_OK && params) st = launch_layer_norm(LAYER_NORM_GRAD_PARTS, k, desc->dtype, stream);
+    }
+    return st == BS_OK && params ? launch_layer_norm(LAYER_NORM_GRAD_JOIN, k, desc->dtype, stream) : st;
 }
 
 }  // extern "C"

@@ -1,12 +1,14 @@
-// Argument block and launches of the layer-normalisation kernels (bs_layer_norm.hip), shared with the host code that fills them (bs_layer_norm.cpp).
+// Argument block and launches of the layer-normalisation kernels (bs_layer_norm*.hip), shared with the host code that fills them (bs_layer_norm.cpp).
 #pragma once
 
 #include "bs_rows_args.h"
 
 namespace bs {
 
-constexpr int K_LAYER_NORM_THREADS = 256;
-constexpr uint32_t K_LAYER_NORM_ROW_GROUPS = 16384;  // work-groups that walk over the rows, at most
+constexpr uint32_t K_LAYER_NORM_ROW_GROUPS = 512;  // work-groups that walk over long rows, at most: two of each compute unit
+
+constexpr int K_LAYER_NORM_GRAD_THREADS = 1024;           // of a work-group of the backward pass with the rows in registers
+constexpr uint32_t K_LAYER_NORM_GRAD_GROUPS = 256;        // of them at most: one of each compute unit
 
 struct LayerNormK {
     RowTensor x, addend, y, total;  // backward: x is t; addend, total: p may be nullptr
@@ -26,5 +28,13 @@ struct LayerNormK {
 
 enum LayerNormPass { LAYER_NORM, LAYER_NORM_GRAD, LAYER_NORM_GRAD_PARTS, LAYER_NORM_GRAD_JOIN };
 bs_status launch_layer_norm(LayerNormPass pass, const LayerNormK &k, int32_t dtype, void *stream);
+
+// Rows in the registers of teams of lanes: lanes of a team, vectors of a lane, work-groups.  team == 0: rows too long for that.
+struct LayerNormTeam {
+    int team, vectors;
+    uint32_t groups;
+};
+bs_status launch_layer_norm_team(const LayerNormK &k, const LayerNormTeam &t, int32_t dtype, void *stream);
+bs_status launch_layer_norm_team_grad(const LayerNormK &k, const LayerNormTeam &t, int32_t dtype, void *stream);
 
 }  // namespace bs

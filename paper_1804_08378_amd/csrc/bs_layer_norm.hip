@@ -4,20 +4,18 @@
 //   u = dy * weight;  dx = rstd * (u - S1 / C - xh * S2 / C) + dt,  S1 = sum u, S2 = sum u * xh over the row
 //   dweight = sum dy * xh,  dbias = sum dy  over the rows
 //
-// Rows of any length: a work-group walks over its row in 128-bit vectors, as often as the formulas need it.  Statistics are float32: a lane takes
-// mean and squared deviations of each vector from the vector's own mean and merges them (Chan's update), so that a mean far from zero cancels nothing.
+// Here: rows too long for registers (bs_layer_norm_team.h has the others), and the join of the parameters' gradients.  A work-group walks over its row
+// in 128-bit vectors, as often as the formulas need it.  Statistics are float32: a lane takes mean and squared deviations of each vector from the
+// vector's own mean and merges them (Chan's update), so that a mean far from zero cancels nothing.
 #include <hip/hip_runtime.h>
 
-#include "bs_layer_norm.h"
-#include "bs_rows8_device.h"
+#include "bs_layer_norm_team.h"
 
 namespace bs {
 namespace {
 
-constexpr int T = K_LAYER_NORM_THREADS;
-
-template <int DT>
-BS_DEV const char *row_of(const RowTensor &t, uint64_t row) { return static_cast<const char *>(t.p) + row * t.stride * K_ES<DT>; }
+constexpr int T = 1024;  // lanes of a work-group that walks over a row
+constexpr int PT = 256;  // of one that sums over rows
 
 // t of a lane's columns.
 template <int DT>
@@ -123,11 +121,11 @@ __global__ __launch_bounds__(T) void layer_norm_grad_kernel(LayerNormK k)
     }
 }
 
-// Sums of dy and dy * xh over a part of the rows: a wave's worth of columns by a work-group, a wave every T / 64-th row.
+// Sums of dy and dy * xh over a part of the rows: a wave's worth of columns by a work-group, a wave every fourth row.
 template <int DT>
-__global__ __launch_bounds__(T) void layer_norm_grad_parts_kernel(LayerNormK k)
+__global__ __launch_bounds__(PT) void layer_norm_grad_parts_kernel(LayerNormK k)
 {
-    constexpr int VEC = K_VEC<DT>, W = T / 64;
+    constexpr int VEC = K_VEC<DT>, W = PT / 64;
     __shared__ float lds[W][64 * VEC];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, tiles = (k.C + 64 * VEC - 1) / (64 * VEC);
     const uint32_t part = blockIdx.x / tiles, c0 = (blockIdx.x - part * tiles) * 64 * VEC, c = c0 + lane * VEC;
@@ -149,7 +147,7 @@ __global__ __launch_bounds__(T) void layer_norm_grad_parts_kernel(LayerNormK k)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) lds[wave][lane * VEC + i] = s[m][i];
         __syncthreads();
-        for (uint32_t j = threadIdx.x; j < 64 * VEC && c0 + j < k.C; j += T) {
+        for (uint32_t j = threadIdx.x; j < 64 * VEC && c0 + j < k.C; j += PT) {
             float sum = 0.0f;
 #pragma unroll
             for (int w = 0; w < W; ++w) sum += lds[w][j];
@@ -158,34 +156,32 @@ __global__ __launch_bounds__(T) void layer_norm_grad_parts_kernel(LayerNormK k)
     }
 }
 
-// Joins the parts: 64 columns by a work-group, a wave every T / 64-th part.
+// Joins the parts: eight columns by a work-group, 128 lanes for each of them, in a fixed order.
+constexpr int JT = 1024, JC = 8;
 template <int DT>
-__global__ __launch_bounds__(T) void layer_norm_grad_join_kernel(LayerNormK k)
+__global__ __launch_bounds__(JT) void layer_norm_grad_join_kernel(LayerNormK k)
 {
-    constexpr int W = T / 64;
-    __shared__ float lds[2][W][64];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    __shared__ float db[JT], dw[JT];
+    const uint32_t c = blockIdx.x * JC + threadIdx.x % JC;
     float s0 = 0.0f, s1 = 0.0f;
-    if (c < k.C)
-        for (uint32_t p = wave; p < k.parts; p += W) {
+    if (c < k.C) {
+#pragma unroll 4
+        for (uint32_t p = threadIdx.x / JC; p < k.parts; p += JT / JC) {
             const float2 in = *reinterpret_cast<const float2 *>(k.part + 2 * ((uint64_t)p * k.C + c));
             s0 += in.x;
             s1 += in.y;
         }
-    lds[0][wave][lane] = s0;
-    lds[1][wave][lane] = s1;
-    __syncthreads();
-    if (wave || c >= k.C) return;
-    auto put = [&](void *p, const float (&v)[W][64]) {
-        if (!p) return;
-        float s = 0.0f;
-#pragma unroll
-        for (int w = 0; w < W; ++w) s += v[w][lane];
-        if (DT == DT_F32 || k.f32_params) static_cast<float *>(p)[c] = s;
-        else static_cast<uint16_t *>(p)[c] = half_bits<DT>(s);
-    };
-    put(k.dbias, lds[0]);
-    put(k.dweight, lds[1]);
+    }
+    db[threadIdx.x] = s0;
+    dw[threadIdx.x] = s1;
+    for (uint32_t half = JT / 2; half >= JC; half /= 2) {
+        __syncthreads();
+        if (threadIdx.x < half) {
+            db[threadIdx.x] += db[threadIdx.x + half];
+            dw[threadIdx.x] += dw[threadIdx.x + half];
+        }
+    }
+    if (threadIdx.x < JC && c < k.C) put_params<DT>(k, c, db[threadIdx.x], dw[threadIdx.x]);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -205,8 +201,8 @@ void launch(LayerNormPass pass, const LayerNormK &k, hipStream_t st)
     switch (pass) {
     case LAYER_NORM: layer_norm_kernel<DT><<<rows, block, 0, st>>>(k); break;
     case LAYER_NORM_GRAD: layer_norm_grad_kernel<DT><<<rows, block, 0, st>>>(k); break;
-    case LAYER_NORM_GRAD_PARTS: layer_norm_grad_parts_kernel<DT><<<dim3(tiles * k.parts), block, 0, st>>>(k); break;
-    case LAYER_NORM_GRAD_JOIN: layer_norm_grad_join_kernel<DT><<<dim3((k.C + 63) / 64), block, 0, st>>>(k); break;
+    case LAYER_NORM_GRAD_PARTS: layer_norm_grad_parts_kernel<DT><<<dim3(tiles * k.parts), dim3(PT), 0, st>>>(k); break;
+    case LAYER_NORM_GRAD_JOIN: layer_norm_grad_join_kernel<DT><<<dim3((k.C + JC - 1) / JC), dim3(JT), 0, st>>>(k); break;
     }
 }
 

@@ -1,0 +1,164 @@
+// Layer normalisation, forward, with the rows in registers (bs_layer_norm_team.h); formulas: bs_layer_norm.hip.
+#include <hip/hip_runtime.h>
+
+#include "bs_layer_norm_team.h"
+
+namespace bs {
+namespace {
+
+// Lanes of a work-group: a team of several waves, or as many teams as four waves hold.
+template <int TEAM>
+constexpr int K_THREADS = TEAM <= 64 ? 256 : TEAM;
+
+template <int DT, int TEAM, int NV, bool ADD>
+__global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerNormK k)
+{
+    constexpr int VEC = K_VEC<DT>, T = K_THREADS<TEAM>, W = TEAM / 64;  // W: waves of a team, 0: several teams in a wave
+    constexpr bool HOLD = NV * VEC <= 16, AHEAD = TEAM * NV < 4096;  // weight and bias stay in registers; the next row is loaded ahead
+    constexpr uint32_t TEAMS = T / TEAM;
+    __shared__ float lds[2][W > 1 ? W : 1][2];
+    const uint32_t lane = threadIdx.x % TEAM, team = team_of<TEAM, T>();
+    const bool whole = k.C % VEC == 0;
+    float w[HOLD ? NV : 1][VEC], b[HOLD ? NV : 1][VEC];
+    if constexpr (HOLD)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t c = (j * TEAM + lane) * VEC;
+            load_row_params<DT>(k.weight, k.f32_params, c, k.C, 1.0f, w[j]);
+            load_row_params<DT>(k.bias, k.f32_params, c, k.C, 0.0f, b[j]);
+        }
+    // columns of a wave of the team
+    auto columns_of = [&](uint32_t wave) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t c = (j * TEAM + wave * 64) * VEC;
+            n += c < k.C ? min(k.C - c, (uint32_t)(64 * VEC)) : 0;
+        }
+        return (float)n;
+    };
+    const float columns = (float)k.C;
+    Raw<DT, VEC> x[NV], a[NV];
+    auto load = [&](uint64_t row) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t c = row < k.rows ? (j * TEAM + lane) * VEC : k.C;
+            x[j] = load_vector<DT>(row_of<DT>(k.x, row), c, k.C);
+            if constexpr (ADD) a[j] = load_vector<DT>(row_of<DT>(k.addend, row), c, k.C);
+        }
+    };
+    uint64_t first = (uint64_t)blockIdx.x * TEAMS;  // the same for all lanes of a work-group
+    if constexpr (AHEAD) load(first + team);
+    for (uint32_t turn = 0; first < k.rows; first += (uint64_t)gridDim.x * TEAMS, turn ^= 1) {
+        const uint64_t row = first + team;
+        if constexpr (!AHEAD) load(row);
+        Raw<DT, VEC> t[NV];
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            t[j] = x[j];
+            float v[VEC];
+            if constexpr (ADD) {
+                float add[VEC];
+                unpack<DT, VEC>(x[j], v);
+                unpack<DT, VEC>(a[j], add);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] += add[i];
+                t[j] = to_words<DT>(v);
+            }
+            unpack<DT, VEC>(t[j], v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s += v[i];
+        }
+        if constexpr (AHEAD) load(first + (uint64_t)gridDim.x * TEAMS + team);
+        s = lanes_sum<TEAM < 64 ? TEAM : 64>(s);
+        const float n = W > 1 ? columns_of(threadIdx.x / 64) : columns;
+        float mean = n > 0.0f ? s / n : 0.0f, m2 = 0.0f;  // of a wave's columns
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t c = (j * TEAM + lane) * VEC;
+            forget(t[j].q);
+            if (c < k.C) {
+                float v[VEC];
+                unpack<DT, VEC>(t[j], v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float d = whole || c + i < k.C ? v[i] - mean : 0.0f;
+                    m2 = __builtin_fmaf(d, d, m2);
+                }
+            }
+        }
+        m2 = lanes_sum<TEAM < 64 ? TEAM : 64>(m2);
+        if constexpr (W > 1) {
+            if (threadIdx.x % 64 == 0) {
+                lds[turn][threadIdx.x / 64][0] = mean;
+                lds[turn][threadIdx.x / 64][1] = m2;
+            }
+            __syncthreads();  // (the other turn's values are read before the next barrier)
+            const float nw = columns_of(threadIdx.x % W), mw = lds[turn][threadIdx.x % W][0], qw = lds[turn][threadIdx.x % W][1];
+            mean = lanes_sum<W>(nw * mw) / columns;
+            m2 = lanes_sum<W>(__builtin_fmaf(nw * (mw - mean), mw - mean, qw));
+        }
+        const float rstd = 1.0f / sqrtf(m2 / columns + k.eps);
+        if (row >= k.rows) continue;  // (teams of one wave)
+        if (k.stats && lane == 0) *reinterpret_cast<float2 *>(k.stats + 2 * row) = make_float2(mean, rstd);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t c = (j * TEAM + lane) * VEC;
+            forget(t[j].q);
+            if (ADD && k.total.p) store_vector<DT>(const_cast<char *>(row_of<DT>(k.total, row)), c, k.C, t[j]);
+            float v[VEC], wj[VEC], bj[VEC];
+            unpack<DT, VEC>(t[j], v);
+            if (k.held.codes) store_held<DT>(k.held, row, c, k.C, v);
+            if constexpr (!HOLD) {
+                load_row_params<DT>(k.weight, k.f32_params, afresh(c), k.C, 1.0f, wj);
+                load_row_params<DT>(k.bias, k.f32_params, afresh(c), k.C, 0.0f, bj);
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = __builtin_fmaf((v[i] - mean) * rstd, HOLD ? w[HOLD ? j : 0][i] : wj[i], HOLD ? b[HOLD ? j : 0][i] : bj[i]);
+            store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, row)), c, k.C, v);
+            if constexpr (!HOLD) __builtin_amdgcn_sched_barrier(0);  // (one vector's numbers at a time in registers)
+        }
+    }
+}
+
+template <int DT, int TEAM, int NV>
+void launch(const LayerNormK &k, uint32_t groups, hipStream_t st)
+{
+    const dim3 grid(groups), block(K_THREADS<TEAM>);
+    if (k.addend.p) layer_norm_team_kernel<DT, TEAM, NV, true><<<grid, block, 0, st>>>(k);
+    else layer_norm_team_kernel<DT, TEAM, NV, false><<<grid, block, 0, st>>>(k);
+}
+
+template <int DT>
+void launch_type(const LayerNormK &k, const LayerNormTeam &t, hipStream_t st)
+{
+    switch (t.team * 16 + t.vectors) {
+    case 8 * 16 + 1: launch<DT, 8, 1>(k, t.groups, st); break;
+    case 16 * 16 + 1: launch<DT, 16, 1>(k, t.groups, st); break;
+    case 32 * 16 + 1: launch<DT, 32, 1>(k, t.groups, st); break;
+    case 64 * 16 + 1: launch<DT, 64, 1>(k, t.groups, st); break;
+    case 128 * 16 + 1: launch<DT, 128, 1>(k, t.groups, st); break;
+    case 256 * 16 + 1: launch<DT, 256, 1>(k, t.groups, st); break;
+    case 512 * 16 + 1: launch<DT, 512, 1>(k, t.groups, st); break;
+    case 1024 * 16 + 1: launch<DT, 1024, 1>(k, t.groups, st); break;
+    case 1024 * 16 + 2: launch<DT, 1024, 2>(k, t.groups, st); break;
+    case 1024 * 16 + 4: launch<DT, 1024, 4>(k, t.groups, st); break;
+    }
+}
+
+}  // namespace
+
+bs_status launch_layer_norm_team(const LayerNormK &k, const LayerNormTeam &t, int32_t dtype, void *stream)
+{
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dtype == BS_F32) launch_type<DT_F32>(k, t, st);
+    else if (dtype == BS_BF16) launch_type<DT_BF16>(k, t, st);
+    else launch_type<DT_F16>(k, t, st);
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return BS_OK;
+    set_hip_error((int32_t)e);
+    return BS_ERR_HIP;
+}
+
+}  // namespace bs

@@ -15,65 +15,184 @@ template <int DT>
 constexpr int K_ES = DT == DT_F32 ? 4 : 2;
 
 // ------------------------------------------------------------------------------------------------ access
-// VEC elements of a row from column c on; columns from `columns` on are 0 and are not read.  Rows may begin at any element: 128-bit accesses need no
-// more than the element's alignment.
+// Rows may begin at any element: accesses of up to 128 bits need no more than the element's alignment.
+template <int N, int A>
+BS_DEV void load_words(const char *p, uint32_t (&w)[N])
+{
+    using V = typename WordsOf<N>::type;
+    const V t = *reinterpret_cast<const typename AtMultiplesOf<V, A>::type *>(p);
+    if constexpr (N == 1) {
+        w[0] = t;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = t[i];
+    }
+}
+
+// The first `n` of the elements of E bytes that N words hold (not all of them), the others 0: a load for every bit of n, largest first.  (Words are
+// chosen by masks: of conditions between elements of an array the compiler makes indexes, and puts the array into memory for them.)
+BS_DEV uint32_t mask_if(bool b) { return 0u - (uint32_t)b; }
+template <int N, int E>
+BS_DEV void load_first(const char *p, uint32_t n, uint32_t (&w)[N])
+{
+    const uint32_t bytes = n * E;
+    uint32_t at = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = 0;
+    if constexpr (N > 4)
+        if (bytes & 16) {
+            uint32_t t[4];
+            load_words<4, E>(p, t);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = t[i];
+            at = 16;
+        }
+    if constexpr (N > 2)
+        if (bytes & 8) {
+            uint32_t t[2];
+            load_words<2, E>(p + at, t);
+#pragma unroll
+            for (int i = 0; i < N; i += 4)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) w[i + m] |= t[m] & mask_if(at == 4 * (uint32_t)i);
+            at += 8;
+        }
+    if constexpr (N > 1)
+        if (bytes & 4) {
+            uint32_t t[1];
+            load_words<1, E>(p + at, t);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) w[i] |= t[0] & mask_if(at == 4 * (uint32_t)i);
+            at += 4;
+        }
+    if constexpr (E <= 2)
+        if (bytes & 2) {
+            uint32_t t;
+            if constexpr (E == 2) t = *reinterpret_cast<const uint16_t *>(p + at);
+            else t = (uint32_t)(uint8_t)p[at] | (uint32_t)(uint8_t)p[at + 1] << 8;
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] |= t & mask_if(at == 4 * (uint32_t)i);
+            at += 2;
+        }
+    if constexpr (E == 1)
+        if (bytes & 1) {
+            const uint32_t t = (uint32_t)(uint8_t)p[at] << (8 * (at & 2));
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] |= t & mask_if(at / 4 == (uint32_t)i);
+        }
+}
+
+template <int N>
+BS_DEV uint32_t word_at(const uint32_t (&w)[N], uint32_t at)
+{
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) t |= w[i] & mask_if(at / 4 == (uint32_t)i);
+    return t;
+}
+// The other way: nothing behind the n-th element is written.
+template <int N, int E>
+BS_DEV void store_first(char *p, uint32_t n, const uint32_t (&w)[N])
+{
+    const uint32_t bytes = n * E;
+    uint32_t at = 0;
+    if constexpr (N > 2)
+        if (bytes & 8) {
+            const uint32_t t[2] = {w[0], w[1]};
+            store_words<2, E, false>(p, t);
+            at = 8;
+        }
+    if constexpr (N > 1)
+        if (bytes & 4) {
+            const uint32_t t[1] = {word_at(w, at)};
+            store_words<1, E, false>(p + at, t);
+            at += 4;
+        }
+    if constexpr (E <= 2)
+        if (bytes & 2) {
+            const uint32_t t = word_at(w, at);
+            if constexpr (E == 2) {
+                *reinterpret_cast<uint16_t *>(p + at) = (uint16_t)t;
+            } else {
+                p[at] = (char)t;
+                p[at + 1] = (char)(t >> 8);
+            }
+            at += 2;
+        }
+    if constexpr (E == 1)
+        if (bytes & 1) p[at] = (char)(word_at(w, at) >> (8 * (at & 2)));
+}
+
+// A lane's vector of a row as it stands in memory; columns from `columns` on are 0 and are not read.
+template <int DT>
+BS_DEV Raw<DT, K_VEC<DT>> load_vector(const char *row, uint32_t c, uint32_t columns)
+{
+    const char *p = row + (uint64_t)c * K_ES<DT>;
+    uint32_t w[4] = {};
+    if (c + K_VEC<DT> <= columns) load_words<4, K_ES<DT>>(p, w);
+    else if (c < columns) load_first<4, K_ES<DT>>(p, columns - c, w);
+    Raw<DT, K_VEC<DT>> r;
+    r.q = make_uint4(w[0], w[1], w[2], w[3]);
+    return r;
+}
+template <int DT>
+BS_DEV void store_vector(char *row, uint32_t c, uint32_t columns, const Raw<DT, K_VEC<DT>> &r)
+{
+    char *p = row + (uint64_t)c * K_ES<DT>;
+    const uint32_t w[4] = {r.q.x, r.q.y, r.q.z, r.q.w};
+    if (c + K_VEC<DT> <= columns) store_words<4, K_ES<DT>, true>(p, w);
+    else if (c < columns) store_first<4, K_ES<DT>>(p, columns - c, w);
+}
+
+// Numbers rounded to their type.
+template <int DT>
+BS_DEV Raw<DT, K_VEC<DT>> to_words(const float (&v)[K_VEC<DT>])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == DT_F32) w[i] = __float_as_uint(v[i]);
+        else w[i] = pack2<DT>(v[2 * i], v[2 * i + 1]);
+    }
+    Raw<DT, K_VEC<DT>> r;
+    r.q = make_uint4(w[0], w[1], w[2], w[3]);
+    return r;
+}
+
 template <int DT>
 BS_DEV void load_cols(const char *row, uint32_t c, uint32_t columns, float (&v)[K_VEC<DT>])
 {
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    const char *p = row + (uint64_t)c * K_ES<DT>;
-    Raw<DT, K_VEC<DT>> r;
-    r.q = make_uint4(0, 0, 0, 0);
-    if (c + K_VEC<DT> <= columns) {
-        const u4 t = *reinterpret_cast<const typename AtMultiplesOf<u4, K_ES<DT>>::type *>(p);
-        r.q = make_uint4(t.x, t.y, t.z, t.w);
-        unpack<DT, K_VEC<DT>>(r, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i) {
-            v[i] = 0.0f;
-            if (c + i < columns) {
-                if constexpr (DT == DT_F32) v[i] = reinterpret_cast<const float *>(p)[i];
-                else v[i] = half_up<DT>(reinterpret_cast<const uint16_t *>(p)[i]);
-            }
-        }
-    }
+    unpack<DT, K_VEC<DT>>(load_vector<DT>(row, c, columns), v);
 }
-
 template <int DT>
 BS_DEV void store_cols(char *row, uint32_t c, uint32_t columns, const float (&v)[K_VEC<DT>])
 {
-    char *p = row + (uint64_t)c * K_ES<DT>;
-    if (c + K_VEC<DT> <= columns) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (DT == DT_F32) w[i] = __float_as_uint(v[i]);
-            else w[i] = pack2<DT>(v[2 * i], v[2 * i + 1]);
-        }
-        store_words<4, K_ES<DT>, true>(p, w);
-    } else {
-#pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i)
-            if (c + i < columns) {
-                if constexpr (DT == DT_F32) reinterpret_cast<float *>(p)[i] = v[i];
-                else reinterpret_cast<uint16_t *>(p)[i] = half_bits<DT>(v[i]);
-            }
-    }
+    store_vector<DT>(row, c, columns, to_words<DT>(v));
 }
 
-// Parameters of a lane's columns, `none` where there are none and 0 behind the last column.
+// Parameters of a lane's columns, `none` where there are none; behind the last column: any number.
 template <int DT>
 BS_DEV void load_row_params(const void *p, bool f32, uint32_t c, uint32_t columns, float none, float (&v)[K_VEC<DT>])
 {
+    constexpr int VEC = K_VEC<DT>;
+    if (!p) {
 #pragma unroll
-    for (int i = 0; i < K_VEC<DT>; ++i) {
-        v[i] = 0.0f;
-        if (c + i < columns) {
-            if (!p) v[i] = none;
-            else if (DT == DT_F32 || f32) v[i] = static_cast<const float *>(p)[c + i];
-            else v[i] = half_up<DT>(static_cast<const uint16_t *>(p)[c + i]);
+        for (int i = 0; i < VEC; ++i) v[i] = none;
+    } else if (DT == DT_F32 || f32) {
+        struct __attribute__((packed, aligned(4))) Floats { float f[VEC]; };
+        const float *q = static_cast<const float *>(p) + c;
+        if (c + VEC <= columns) {
+            const Floats t = *reinterpret_cast<const Floats *>(q);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = t.f[i];
+        } else {
+            uint32_t w[VEC] = {};
+            if (c < columns) load_first<VEC, 4>(reinterpret_cast<const char *>(q), columns - c, w);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = __uint_as_float(w[i]);
         }
+    } else {
+        load_cols<DT>(static_cast<const char *>(p), c, columns, v);
     }
 }
 
@@ -128,17 +247,19 @@ template <int DT>
 BS_DEV void from_8_bits(const uint32_t (&codes)[K_VEC<DT> / 4], uint32_t e, float (&v)[K_VEC<DT>])
 {
     const float step = __builtin_amdgcn_ldexpf(1.0f, (int)e - 133);
-    float n[K_VEC<DT>], most = 0.0f;
+    float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < K_VEC<DT>; ++i) {
-        n[i] = (float)(int)(int8_t)(codes[i / 4] >> (8 * (i % 4)));
-        most = __builtin_fmaxf(most, __builtin_fabsf(n[i]));
-        v[i] = n[i] * step;
+        const float n = (float)(int)(int8_t)(codes[i / 4] >> (8 * (i % 4)));
+        most = __builtin_fmaxf(most, __builtin_fabsf(n));
+        v[i] = n * step;
     }
     if (most >= 127.0f) {
 #pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i)
-            if (__builtin_fabsf(n[i]) >= 127.0f) v[i] = __uint_as_float(n[i] == 127.0f ? K_INF : n[i] == -127.0f ? K_INF | 0x80000000u : 0x7fc00000u);
+        for (int i = 0; i < K_VEC<DT>; ++i) {
+            const int n = (int)(int8_t)(codes[i / 4] >> (8 * (i % 4)));
+            if (n >= 127 || n <= -127) v[i] = __uint_as_float(n == 127 ? K_INF : n == -127 ? K_INF | 0x80000000u : 0x7fc00000u);
+        }
     }
 }
 
@@ -146,36 +267,18 @@ template <int DT>
 BS_DEV void store_codes(int8_t *row, uint32_t c, uint32_t columns, const uint32_t (&codes)[K_VEC<DT> / 4])
 {
     char *p = reinterpret_cast<char *>(row) + c;
-    if (c + K_VEC<DT> <= columns) {
-        store_words<K_VEC<DT> / 4, 1, true>(p, codes);
-    } else {
-#pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i)
-            if (c + i < columns) p[i] = (char)(codes[i / 4] >> (8 * (i % 4)));
-    }
+    if (c + K_VEC<DT> <= columns) store_words<K_VEC<DT> / 4, 1, true>(p, codes);
+    else if (c < columns) store_first<K_VEC<DT> / 4, 1>(p, columns - c, codes);
 }
 
 template <int DT>
 BS_DEV void load_codes(const int8_t *row, uint32_t c, uint32_t columns, uint32_t (&codes)[K_VEC<DT> / 4])
 {
-    constexpr int N = K_VEC<DT> / 4;
     const char *p = reinterpret_cast<const char *>(row) + c;
-    if (c + K_VEC<DT> <= columns) {
-        using V = typename WordsOf<N>::type;
-        const V t = *reinterpret_cast<const typename AtMultiplesOf<V, 1>::type *>(p);
-        if constexpr (N == 1) {
-            codes[0] = t;
-        } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) codes[i] = t[i];
-        }
-    } else {
-#pragma unroll
-        for (int w = 0; w < N; ++w) codes[w] = 0;
-#pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i)
-            if (c + i < columns) codes[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
-    }
+    for (int i = 0; i < K_VEC<DT> / 4; ++i) codes[i] = 0;
+    if (c + K_VEC<DT> <= columns) load_words<K_VEC<DT> / 4, 1>(p, codes);
+    else if (c < columns) load_first<K_VEC<DT> / 4, 1>(p, columns - c, codes);
 }
 
 // A lane's vector of a row held in 8 bits, as numbers (0 behind the last column).
