@@ -509,17 +509,28 @@ struct Operators {
     decltype(&bs_log_probs_workspace_bytes) head_bytes;
     decltype(&bs_log_probs) head;
     decltype(&bs_log_probs_backward) head_backward;
+    decltype(&bs_layer_norm) rows_norm;
+    decltype(&bs_layer_norm_workspace_bytes) rows_norm_bytes;
+    decltype(&bs_layer_norm_backward) rows_norm_backward;
+    decltype(&bs_activate) activate;
+    decltype(&bs_activate_backward) activate_backward;
+    decltype(&bs_pack8) pack8;
+    decltype(&bs_unpack8) unpack8;
 };
 Operators g_operators{};
 
-// set_operators((addresses of the six functions, in this order))
+// set_operators((addresses of the thirteen functions, in this order))
 PyObject *set_operators(PyObject *, PyObject *args)
 {
-    unsigned long long a[6];
-    if (!PyArg_ParseTuple(args, "(KKKKKK)", a, a + 1, a + 2, a + 3, a + 4, a + 5)) return nullptr;
+    unsigned long long a[13];
+    if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKKK)", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8, a + 9, a + 10, a + 11, a + 12)) return nullptr;
     g_operators = {reinterpret_cast<decltype(Operators::norm_bytes)>(a[0]), reinterpret_cast<decltype(Operators::norm)>(a[1]),
                    reinterpret_cast<decltype(Operators::norm_backward)>(a[2]), reinterpret_cast<decltype(Operators::head_bytes)>(a[3]),
-                   reinterpret_cast<decltype(Operators::head)>(a[4]), reinterpret_cast<decltype(Operators::head_backward)>(a[5])};
+                   reinterpret_cast<decltype(Operators::head)>(a[4]), reinterpret_cast<decltype(Operators::head_backward)>(a[5]),
+                   reinterpret_cast<decltype(Operators::rows_norm)>(a[6]), reinterpret_cast<decltype(Operators::rows_norm_bytes)>(a[7]),
+                   reinterpret_cast<decltype(Operators::rows_norm_backward)>(a[8]), reinterpret_cast<decltype(Operators::activate)>(a[9]),
+                   reinterpret_cast<decltype(Operators::activate_backward)>(a[10]), reinterpret_cast<decltype(Operators::pack8)>(a[11]),
+                   reinterpret_cast<decltype(Operators::unpack8)>(a[12])};
     Py_RETURN_NONE;
 }
 
@@ -814,6 +825,279 @@ PyObject *log_probs_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------------------------------- operators over rows
+// Layer normalisation, activations, 8-bit checkpoints.  Rows: all dimensions but the last.
+
+// Elements from a row to the next where rows are contiguous and follow each other at one distance; 0: they do not.
+int64_t rows_step(const at::Tensor &t)
+{
+    const int64_t dims = t.dim(), columns = t.size(dims - 1);
+    if (columns > 1 && t.stride(dims - 1) != 1) return 0;
+    int64_t rows = 1, step = -1;
+    for (int64_t i = dims - 2; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (step >= 0 && t.stride(i) != rows * step) return 0;
+        if (step < 0) step = t.stride(i);
+        rows *= t.size(i);
+    }
+    if (step < 0) return columns;
+    return step >= columns ? step : 0;
+}
+
+// What the calls over rows have in common: `like` gives shape, type and device.
+struct RowsCall {
+    at::Tensor like;
+    int64_t rows = 0, columns = 0;
+    int32_t dtype = -1;
+
+    // false: not the plain case
+    bool read(PyObject *o)
+    {
+        const at::Tensor *t = tensor_of(o);
+        if (!g_operators.rows_norm || !t || recorders_active() || !t->defined() || dual(*t) || !t->is_cuda() || !t->has_storage() || t->dim() < 1 || t->numel() < 1) return false;
+        like = *t;
+        columns = t->size(t->dim() - 1);
+        rows = t->numel() / columns;
+        dtype = dtype_code(t->scalar_type());
+        return !t->is_neg();
+    }
+    // An operand of like's shape, type and device that is read in place (or none).
+    bool beside(const at::Tensor &t, int64_t &stride) const
+    {
+        return !t.defined() || (on_gpu(t, like.device()) && t.sizes() == like.sizes() && t.scalar_type() == like.scalar_type() && !t.is_neg() && (stride = rows_step(t)) != 0);
+    }
+    bool parameter(const at::Tensor &t, int32_t &type, bool first) const
+    {
+        if (!t.defined()) return true;
+        if (!on_gpu(t, like.device()) || t.dim() != 1 || t.size(0) != columns || !t.is_contiguous()) return false;
+        const int32_t code = dtype_code(t.scalar_type());
+        if ((code != BS_F32 && code != dtype) || (!first && code != type)) return false;
+        type = code;
+        return true;
+    }
+    int64_t blocks() const { return (columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK; }
+    // codes and exponents of like's shape
+    bool held(const at::Tensor &codes, const at::Tensor &exponents) const
+    {
+        if (!codes.defined() || !exponents.defined() || !on_gpu(codes, like.device()) || !on_gpu(exponents, like.device())) return false;
+        if (codes.scalar_type() != at::kChar || exponents.scalar_type() != at::kByte || codes.sizes() != like.sizes() || exponents.dim() != like.dim()) return false;
+        for (int64_t i = 0; i + 1 < like.dim(); ++i)
+            if (exponents.size(i) != like.size(i)) return false;
+        return exponents.size(like.dim() - 1) == blocks() && codes.is_contiguous() && exponents.is_contiguous();
+    }
+    at::Tensor empty() const { return at::empty(like.sizes(), like.options().memory_format(at::MemoryFormat::Contiguous)); }
+    at::Tensor empty_last(int64_t last, at::ScalarType type) const
+    {
+        c10::SmallVector<int64_t, 6> sizes(like.sizes().begin(), like.sizes().end());
+        sizes.back() = last;
+        return at::empty(sizes, like.options().dtype(type).memory_format(at::MemoryFormat::Contiguous));
+    }
+    void empty_held(at::Tensor &codes, at::Tensor &exponents) const
+    {
+        codes = empty_last(columns, at::kChar);
+        exponents = empty_last(blocks(), at::kByte);
+    }
+    void *stream() const { return c10::hip::getCurrentHIPStream(like.device().index()).stream(); }
+};
+
+void *ptr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+int8_t *codes_of(const at::Tensor &t) { return static_cast<int8_t *>(ptr(t)); }
+uint8_t *exponents_of(const at::Tensor &t) { return static_cast<uint8_t *>(ptr(t)); }
+
+// layer_norm(x, weight, bias, addend, eps, checkpoint, keep statistics?) -> (y, total, stats, codes, exponents) or None
+PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    RowsCall c;
+    bs_layer_norm_desc d{};
+    at::Tensor weight, bias, addend, y, total, stats, codes, exponents;
+    d.param_dtype = BS_F32;
+    if (n != 7 || !c.read(args[0]) || !optional_tensor(args[1], weight) || !optional_tensor(args[2], bias) || !optional_tensor(args[3], addend) ||
+        !read_float(args[4], d.eps) || c.dtype < 0 || (d.x_stride = rows_step(c.like)) == 0 || !c.beside(addend, d.addend_stride) ||
+        !c.parameter(weight, d.param_dtype, true) || !c.parameter(bias, d.param_dtype, !weight.defined()))
+        Py_RETURN_NONE;
+    const bool checkpoint = args[5] == Py_True, keep = args[6] == Py_True;
+    if (!checkpoint && args[5] != Py_False) Py_RETURN_NONE;
+    d.rows = c.rows;
+    d.features = c.columns;
+    d.dtype = c.dtype;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.like.device());
+        y = c.empty();
+        if (addend.defined()) total = c.empty();
+        if (keep) stats = c.empty_last(2, at::kFloat);
+        if (checkpoint) c.empty_held(codes, exponents);
+        const int rc = g_operators.rows_norm(&d, c.like.data_ptr(), ptr(addend), ptr(weight), ptr(bias), y.data_ptr(), ptr(total), static_cast<float *>(ptr(stats)),
+                                             codes_of(codes), exponents_of(exponents), c.stream());
+        if (rc != 0) throw CallFailed(rc, "bs_layer_norm");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({y, total, stats, codes, exponents});
+    END_HANDLE_TH_ERRORS
+}
+
+// layer_norm_backward(x or codes, exponents or None, stats, grad, weight, bias, grad_total, wanted: bits 1 x, 2 weight, 4 bias)
+// -> (grad_x, grad_weight, grad_bias) or None
+PyObject *layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    RowsCall c;
+    bs_layer_norm_desc d{};
+    at::Tensor x, exponents, stats, weight, bias, grad_total, gx, gw, gb;
+    int64_t wanted;
+    d.param_dtype = BS_F32;
+    if (n != 8 || !c.read(args[3]) || !optional_tensor(args[0], x) || !optional_tensor(args[1], exponents) || !optional_tensor(args[2], stats) ||
+        !optional_tensor(args[4], weight) || !optional_tensor(args[5], bias) || !optional_tensor(args[6], grad_total) || !read_int(args[7], wanted) ||
+        !x.defined() || !stats.defined() || c.dtype < 0)
+        Py_RETURN_NONE;
+    const bool held = exponents.defined();
+    if (held ? !c.held(x, exponents) : !c.beside(x, d.x_stride)) Py_RETURN_NONE;
+    if ((d.grad_y_stride = rows_step(c.like)) == 0 || !c.beside(grad_total, d.grad_total_stride) || !c.parameter(weight, d.param_dtype, true) ||
+        !c.parameter(bias, d.param_dtype, !weight.defined()))
+        Py_RETURN_NONE;
+    if (!on_gpu(stats, c.like.device()) || stats.scalar_type() != at::kFloat || !stats.is_contiguous() || stats.dim() != c.like.dim() || stats.size(stats.dim() - 1) != 2) Py_RETURN_NONE;
+    for (int64_t i = 0; i + 1 < stats.dim(); ++i)
+        if (stats.size(i) != c.like.size(i)) Py_RETURN_NONE;
+    d.rows = c.rows;
+    d.features = c.columns;
+    d.dtype = c.dtype;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.like.device());
+        if (wanted & 1) gx = c.empty();
+        if ((wanted & 2) && weight.defined()) gw = at::empty({c.columns}, weight.options());
+        if ((wanted & 4) && bias.defined()) gb = at::empty({c.columns}, bias.options());
+        const uint64_t bytes = gw.defined() || gb.defined() ? g_operators.rows_norm_bytes(&d) : 0;
+        const at::Tensor ws = workspace_of(bytes, c.like.options().memory_format(at::MemoryFormat::Contiguous));
+        const int rc = g_operators.rows_norm_backward(&d, held ? nullptr : x.data_ptr(), held ? codes_of(x) : nullptr, exponents_of(exponents),
+                                                      static_cast<const float *>(stats.data_ptr()), ptr(weight), c.like.data_ptr(), ptr(grad_total), ptr(gx), ptr(gw),
+                                                      ptr(gb), ptr(ws), bytes, c.stream());
+        if (rc != 0) throw CallFailed(rc, "bs_layer_norm_backward");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({gx, gw, gb});
+    END_HANDLE_TH_ERRORS
+}
+
+// activate(x, activation, gate, checkpoint) -> (y, x codes, x exponents, gate codes, gate exponents) or None
+PyObject *activate(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    RowsCall c;
+    bs_activate_desc d{};
+    at::Tensor gate, y, xc, xe, gc, ge;
+    int64_t act;
+    if (n != 4 || !c.read(args[0]) || !read_int(args[1], act) || !optional_tensor(args[2], gate) || c.dtype < 0 || (d.x_stride = rows_step(c.like)) == 0 ||
+        !c.beside(gate, d.gate_stride))
+        Py_RETURN_NONE;
+    const bool checkpoint = args[3] == Py_True;
+    if (!checkpoint && args[3] != Py_False) Py_RETURN_NONE;
+    d.rows = c.rows;
+    d.columns = c.columns;
+    d.dtype = c.dtype;
+    d.activation = (int32_t)act;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.like.device());
+        y = c.empty();
+        if (checkpoint) c.empty_held(xc, xe);
+        if (checkpoint && gate.defined()) c.empty_held(gc, ge);
+        const int rc = g_operators.activate(&d, c.like.data_ptr(), ptr(gate), y.data_ptr(), codes_of(xc), exponents_of(xe), codes_of(gc), exponents_of(ge), c.stream());
+        if (rc != 0) throw CallFailed(rc, "bs_activate");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({y, xc, xe, gc, ge});
+    END_HANDLE_TH_ERRORS
+}
+
+// activate_backward(x or codes, exponents or None, grad, activation, gate or codes or None, exponents or None, wanted: bits 1 x, 2 gate)
+// -> (grad_x, grad_gate) or None
+PyObject *activate_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    RowsCall c;
+    bs_activate_desc d{};
+    at::Tensor x, xe, gate, ge, gx, gg;
+    int64_t act, wanted;
+    if (n != 7 || !c.read(args[2]) || !optional_tensor(args[0], x) || !optional_tensor(args[1], xe) || !read_int(args[3], act) || !optional_tensor(args[4], gate) ||
+        !optional_tensor(args[5], ge) || !read_int(args[6], wanted) || !x.defined() || c.dtype < 0 || (d.grad_y_stride = rows_step(c.like)) == 0)
+        Py_RETURN_NONE;
+    const bool held = xe.defined();
+    if (gate.defined() ? held != ge.defined() : ge.defined()) Py_RETURN_NONE;
+    if (held ? !c.held(x, xe) || (gate.defined() && !c.held(gate, ge)) : !c.beside(x, d.x_stride) || !c.beside(gate, d.gate_stride)) Py_RETURN_NONE;
+    d.rows = c.rows;
+    d.columns = c.columns;
+    d.dtype = c.dtype;
+    d.activation = (int32_t)act;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.like.device());
+        if (wanted & 1) gx = c.empty();
+        if ((wanted & 2) && gate.defined()) gg = c.empty();
+        const int rc = g_operators.activate_backward(&d, held ? nullptr : x.data_ptr(), held ? codes_of(x) : nullptr, exponents_of(xe), held ? nullptr : ptr(gate),
+                                                     held ? codes_of(gate) : nullptr, exponents_of(ge), c.like.data_ptr(), ptr(gx), ptr(gg), c.stream());
+        if (rc != 0) throw CallFailed(rc, "bs_activate_backward");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({gx, gg});
+    END_HANDLE_TH_ERRORS
+}
+
+// pack8(x) -> (codes, exponents) or None
+PyObject *pack8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    RowsCall c;
+    bs_pack8_desc d{};
+    at::Tensor codes, exponents;
+    if (n != 1 || !c.read(args[0]) || c.dtype < 0 || (d.x_stride = rows_step(c.like)) == 0) Py_RETURN_NONE;
+    d.rows = c.rows;
+    d.columns = c.columns;
+    d.dtype = c.dtype;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.like.device());
+        c.empty_held(codes, exponents);
+        const int rc = g_operators.pack8(&d, c.like.data_ptr(), codes_of(codes), exponents_of(exponents), c.stream());
+        if (rc != 0) throw CallFailed(rc, "bs_pack8");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return tuple_of({codes, exponents});
+    END_HANDLE_TH_ERRORS
+}
+
+// unpack8(codes, exponents, bs_dtype) -> values or None
+PyObject *unpack8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    RowsCall c;
+    bs_pack8_desc d{};
+    at::Tensor exponents, out;
+    int64_t dtype;
+    if (n != 3 || !c.read(args[0]) || !optional_tensor(args[1], exponents) || !read_int(args[2], dtype) || !c.held(c.like, exponents)) Py_RETURN_NONE;
+    const at::ScalarType type = dtype == BS_F32 ? at::kFloat : dtype == BS_BF16 ? at::kBFloat16 : at::kHalf;
+    d.rows = c.rows;
+    d.columns = c.columns;
+    d.dtype = (int32_t)dtype;
+    try {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(c.like.device());
+        out = c.empty_last(c.columns, type);
+        const int rc = g_operators.unpack8(&d, codes_of(c.like), exponents_of(exponents), out.data_ptr(), c.stream());
+        if (rc != 0) throw CallFailed(rc, "bs_unpack8");
+    } catch (const CallFailed &e) {
+        return failed(e);
+    }
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 constexpr PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 
@@ -842,6 +1126,14 @@ PyMethodDef module_methods[] = {{"set_error", set_error, METH_O, "(class): raise
                                 {"log_probs", fast(log_probs), METH_FASTCALL, "(logits, targets, top, ignore_index) -> results or None"},
                                 {"log_probs_backward", fast(log_probs_backward), METH_FASTCALL,
                                  "(logits, targets, lse, entropy, grad_logp, grad_entropy, ignore_index) -> gradient or None"},
+                                {"layer_norm", fast(layer_norm), METH_FASTCALL, "(x, weight, bias, addend, eps, checkpoint, keep) -> results or None"},
+                                {"layer_norm_backward", fast(layer_norm_backward), METH_FASTCALL,
+                                 "(x or codes, exponents, stats, grad, weight, bias, grad_total, wanted) -> gradients or None"},
+                                {"activate", fast(activate), METH_FASTCALL, "(x, activation, gate, checkpoint) -> results or None"},
+                                {"activate_backward", fast(activate_backward), METH_FASTCALL,
+                                 "(x or codes, exponents, grad, activation, gate or codes, exponents, wanted) -> gradients or None"},
+                                {"pack8", fast(pack8), METH_FASTCALL, "(x) -> (codes, exponents) or None"},
+                                {"unpack8", fast(unpack8), METH_FASTCALL, "(codes, exponents, dtype) -> values or None"},
                                 {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_bs_torch", nullptr, -1, module_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -42,7 +42,8 @@ def _native_calls():
                 module, lib = bs._torch_calls(), bs.load()
                 if module is not None:
                     names = ("bs_group_norm_workspace_bytes", "bs_group_norm", "bs_group_norm_backward", "bs_log_probs_workspace_bytes", "bs_log_probs",
-                             "bs_log_probs_backward")
+                             "bs_log_probs_backward", "bs_layer_norm", "bs_layer_norm_workspace_bytes", "bs_layer_norm_backward", "bs_activate",
+                             "bs_activate_backward", "bs_pack8", "bs_unpack8")
                     module.set_operators(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in names))
                 _native = module or False
     return _native
@@ -431,6 +432,7 @@ def _readable_rows_of(t: Optional[torch.Tensor]) -> Tuple[Optional[torch.Tensor]
     """`t` and the distance of its rows; a copy where it cannot be read in place."""
     if t is None:
         return None, 0
+    t = t.resolve_neg()
     found = _rows(t)
     if found is None:
         t = t.contiguous()
@@ -491,6 +493,11 @@ def _pack8_desc(x: torch.Tensor, dtype: int, step: int):
 def pack8(x) -> Packed8:
     """`x` in 8 bits, 33 bytes for 32 elements of a row (its last dimension): whole numbers of a step, the power of two by which the largest of the
     32 has 63 to 126 steps.  Elements are off by half a step at most, under 0.8 % of that largest one; infinities and NaN stay."""
+    native = _native_calls()
+    if native:
+        done = native.pack8(x)
+        if done is not None:
+            return Packed8(*done)
     if has_torch_function_variadic(x):
         return handle_torch_function(pack8, (x,), x)
     _refuse_recorders("pack8", x)
@@ -506,16 +513,21 @@ def pack8(x) -> Packed8:
 
 def unpack8(packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values that `packed` (a Packed8) stands for, rounded to `dtype`; types that `pack8` takes hold those of their own tensors exactly."""
-    if has_torch_function_variadic(*packed):
-        return handle_torch_function(unpack8, tuple(packed), packed, dtype)
+    native, code = _native_calls(), _DTYPES.get(dtype)
+    if native and code is not None and isinstance(packed, tuple):
+        done = native.unpack8(*packed, code)
+        if done is not None:
+            return done
+    if has_torch_function_variadic(*_parts(packed)):
+        return handle_torch_function(unpack8, _parts(packed), packed, dtype)
     _refuse_recorders("unpack8")
     with torch.no_grad():
         codes, exponents = _packed_operand(packed, "unpack8")
-        if dtype not in _DTYPES:
+        if code is None:
             raise TypeError(f"unpack8: float32, bfloat16 and float16 tensors, not {dtype}")
         out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
         with torch.cuda.device(codes.device):
-            bs.bs_unpack8(_pack8_desc(out, _DTYPES[dtype], out.shape[-1]), codes.data_ptr(), exponents.data_ptr(), out.data_ptr(), _stream(codes))
+            bs.bs_unpack8(_pack8_desc(out, code, out.shape[-1]), codes.data_ptr(), exponents.data_ptr(), out.data_ptr(), _stream(codes))
         return out
 
 
@@ -608,6 +620,11 @@ def _layer_norm_desc(like: torch.Tensor, dtype: int, weight, bias, eps: float):
 
 def _run_layer_norm(x, weight, bias, addend, eps, checkpoint, keep_stats, recorded=False) -> LayerNormed:
     """`recorded`: called by the node that a recorder sees."""
+    native = _native_calls()
+    if native:
+        done = native.layer_norm(x, weight, bias, addend, eps, checkpoint, keep_stats)
+        if done is not None:
+            return LayerNormed(*done[:3], Packed8(*done[3:]) if checkpoint else None)
     if not recorded:
         if has_torch_function_variadic(x, weight, bias, addend):  # (layer_norm has looked already)
             return handle_torch_function(layer_norm_forward, (x, weight, bias, addend), x, weight, bias, addend, eps, checkpoint)
@@ -642,6 +659,11 @@ def layer_norm_backward(x, stats, grad, weight=None, bias=None, grad_total=None,
     """`(grad_x, grad_weight, grad_bias)`: from what was normalised -- `x`, or `total` where there was an addend, or `kept` -- its `stats`, the gradient
     `grad` of y and `grad_total` of total (None: zero).  grad_x is the gradient of x and of the addend alike; `need` says which are wanted (those of
     absent parameters are None)."""
+    native = _native_calls()
+    if native:
+        done = native.layer_norm_backward(*(x if isinstance(x, tuple) else (x, None)), stats, grad, weight, bias, grad_total, need[0] | need[1] << 1 | need[2] << 2)
+        if done is not None:
+            return done
     tensors = (*_parts(x), stats, grad, weight, bias, grad_total)
     if has_torch_function_variadic(*tensors):
         return handle_torch_function(layer_norm_backward, tensors, x, stats, grad, weight, bias, grad_total, need)
@@ -744,6 +766,11 @@ def _activate_desc(like: torch.Tensor, dtype: int, activation: str):
 
 def _run_activate(x, activation, gate, checkpoint, recorded=False, traced=False) -> Activated:
     """`recorded`: called by the node that a recorder sees; `traced`: make that node where torch.jit.trace records."""
+    native, act = _native_calls(), ACTIVATIONS.get(activation)
+    if native and act is not None:
+        done = native.activate(x, act, gate, checkpoint)
+        if done is not None:
+            return Activated(done[0], Packed8(*done[1:3]) if checkpoint else None, Packed8(*done[3:]) if checkpoint and gate is not None else None)
     if not recorded:
         if has_torch_function_variadic(x, gate):  # (activate has looked already)
             return handle_torch_function(activate_forward, (x, gate), x, activation, gate, checkpoint)
@@ -772,6 +799,12 @@ def activate_forward(x, activation: str = "silu", gate=None, checkpoint: bool = 
 def activate_backward(x, grad, activation: str = "silu", gate=None, need=(True, True)):
     """`(grad_x, grad_gate)` from the gradient `grad` of `activate_forward`'s result; x and gate both as they were or both in 8 bits (Packed8).
     `need` says which are wanted (that of an absent gate is None)."""
+    native, act = _native_calls(), ACTIVATIONS.get(activation)
+    if native and act is not None:
+        done = native.activate_backward(*(x if isinstance(x, tuple) else (x, None)), grad, act, *(gate if isinstance(gate, tuple) else (gate, None)),
+                                        need[0] | need[1] << 1)
+        if done is not None:
+            return done
     tensors = (*_parts(x), grad, *_parts(gate))
     if has_torch_function_variadic(*tensors):
         return handle_torch_function(activate_backward, tensors, x, grad, activation, gate, need)
