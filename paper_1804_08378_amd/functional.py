@@ -543,15 +543,26 @@ def _dense_order(t: torch.Tensor) -> Optional[Tuple[int, ...]]:
     return order
 
 
+def _autocasts() -> int:
+    """How many autocast blocks the thread is in."""
+    n = torch.autocast_increment_nesting() - 1
+    torch.autocast_decrement_nesting()
+    return n
+
+
 class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """`with checkpoints_in_8_bits(model): y = model(x)`: what autograd keeps for the backward pass in the block -- convolutions' and linear layers'
     inputs, the operands of stacks and of the functions here -- is held by `pack8` and brought back when the backward pass asks for it, so that the
     gradients are those at the values in 8 bits.
 
-    Held so are tensors on the GPU of `pack8`'s types and sizes with at least `least` elements and dense in memory (any order of dimensions); the others
-    stay as they are, and so do the parameters and buffers of `model` (a module, or an iterable of tensors), which are in use anyway.  A tensor that several
-    nodes keep is held once for each.  Not for values of very different size side by side, such as masks of the type's lowest value: 32 neighbours in
-    memory share a step.  Under autocast, whose copies of the weights could not be told from activations, it refuses."""
+    Held so are tensors on the GPU of `pack8`'s types and sizes with at least `least` elements and two dimensions, more than two of them in the last
+    (statistics of rows have no more), dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers of
+    `model` (a module, or an iterable of tensors), which are in use anyway.  A tensor that several nodes keep is held once for each.  Under autocast,
+    whose copies of the weights could not be told from activations, and where an autocast begins inside the block, it refuses.
+
+    What is exact in 16 bits is not so in 8: an element is off by 0.8 % of the largest of 32 neighbours in memory at most.  A ReLU's gradient then takes
+    the other side for elements that close to 0, the largest of a pooling window is another one where two are that close; logits lose it from their
+    probabilities (keep the loss outside of the block), and numbers next to masks of the type's lowest value all they are."""
 
     def __init__(self, model, least: int = 1 << 14):
         tensors = [*model.parameters(), *model.buffers()] if isinstance(model, nn.Module) else list(model)
@@ -559,10 +570,10 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         memory = {t.untyped_storage().data_ptr() for t in tensors}
 
         def pack(t):
-            if torch.is_autocast_enabled("cuda"):
-                raise RuntimeError("checkpoints_in_8_bits: not under autocast")
+            if _autocasts() > self._autocasts:  # (inside an operation autocast itself reads as switched off)
+                raise RuntimeError("checkpoints_in_8_bits: no autocast inside the block")
             # (`tensors` are alive as long as this is: no other memory has their addresses)
-            if not t.is_cuda or t.dtype not in _DTYPES or t.numel() < max(1, least) or type(t) not in (torch.Tensor, nn.Parameter) or \
+            if not t.is_cuda or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or type(t) not in (torch.Tensor, nn.Parameter) or \
                     t.untyped_storage().data_ptr() in memory or torch.jit.is_tracing():
                 return t
             order = _dense_order(t)
@@ -585,8 +596,14 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             back = sorted(range(len(order)), key=order.__getitem__)
             return unpack8(packed, dtype).view(shape).permute(back)
 
-        self._alive = tensors
+        self._alive, self._autocasts = tensors, 0
         super().__init__(pack, unpack)
+
+    def __enter__(self):
+        if torch.is_autocast_enabled("cuda"):
+            raise RuntimeError("checkpoints_in_8_bits: not under autocast")
+        self._autocasts = _autocasts()
+        return super().__enter__()
 
 
 # ------------------------------------------------------------------------------------------------ layer normalisation
@@ -739,7 +756,7 @@ class LayerNorm(nn.LayerNorm):
         self.checkpoint = checkpoint
 
     def forward(self, x: torch.Tensor, addend: Optional[torch.Tensor] = None):
-        if x.shape[-1] != self.normalized_shape[0]:
+        if isinstance(x, torch.Tensor) and x.shape[-1] != self.normalized_shape[0]:  # (not what stands for one where a recorder looks)
             raise ValueError(f"LayerNorm: rows of {x.shape[-1]} features, not {self.normalized_shape[0]}")
         return layer_norm(x, self.weight, self.bias, addend, self.eps, self.checkpoint)
 

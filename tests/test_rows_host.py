@@ -1,5 +1,6 @@
 """What layer normalisation, activations and the 8-bit form refuse, and which tensors are read in place, without a GPU: nothing is launched, no pointer
 is followed."""
+import contextlib
 import ctypes as C
 import itertools
 
@@ -215,3 +216,51 @@ def test_operands_that_do_not_fit(host_tensors):
             (ValueError, lambda: F.unpack8(F.Packed8(codes, exponents.int()))), (ValueError, lambda: F.unpack8(F.Packed8(codes, torch.zeros(4, 2, dtype=torch.uint8))))]:
         with pytest.raises(error):
             call()
+
+
+def test_the_tensors_device_is_current_while_the_library_is_called(monkeypatch):
+    """The Python calls, without a GPU: tensors in host memory stand for device tensors and nothing is launched."""
+    inside, seen = [], []
+
+    @contextlib.contextmanager
+    def device(dev):
+        inside.append(dev)
+        yield
+        inside.pop()
+
+    class Stream:
+        cuda_stream = 0
+
+    monkeypatch.setattr(F, "_native", False)
+    monkeypatch.setattr(F, "_on_gpu", lambda t, what: None)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: Stream)
+    names = ("bs_layer_norm", "bs_layer_norm_backward", "bs_activate", "bs_activate_backward", "bs_pack8", "bs_unpack8")
+    for name in names:
+        monkeypatch.setattr(F.bs, name, lambda *a, name=name: seen.append((name, list(inside))))
+    x, w = torch.zeros(4, 8), torch.ones(8)
+    r = F.layer_norm_forward(x, w, w, x, checkpoint=True)
+    F.layer_norm_backward(r.kept, r.stats, x, w, w)
+    s = F.activate_forward(x, "silu", x, True)
+    F.activate_backward(s.x, x, "silu", s.gate)
+    F.unpack8(F.pack8(x))
+    assert seen == [(name, [torch.device("cpu")]) for name in names]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+def test_tensors_of_another_device(native, monkeypatch):
+    if torch.cuda.device_count() < 2:
+        pytest.skip("needs two GPUs")
+    if not native:
+        monkeypatch.setattr(F, "_native", False)
+
+    def everything(device):
+        x, w = torch.linspace(-1, 1, 400).view(4, 100).to(device), torch.ones(100, device=device)
+        r = F.layer_norm_forward(x, w, w, x, checkpoint=True)
+        s = F.activate_forward(x, "silu", x, True)
+        return [r.y, *r.kept, *F.layer_norm_backward(r.kept, r.stats, x, w, w), s.y, *F.activate_backward(s.x, x, "silu", s.gate), F.unpack8(F.pack8(x))]
+
+    want, got = everything("cuda:0"), everything("cuda:1")
+    assert torch.cuda.current_device() == 0
+    assert all(torch.equal(a, b.to("cuda:0")) for a, b in zip(want, got))
