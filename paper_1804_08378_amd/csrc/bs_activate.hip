@@ -70,8 +70,11 @@ __global__ __launch_bounds__(T) void activate_kernel(ActivateK k)
         if (l >= left) return;  // (whole blocks of lanes at a time)
         const At a = place.at<DT>(k, l);
         float x[K_VEC<DT>], g[K_VEC<DT>], y[K_VEC<DT>];
-        load_cols<DT>(row_of<DT>(k.x, a.row), a.c, k.columns, x);
-        if constexpr (GATE) load_cols<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns, g);
+        Raw<DT, K_VEC<DT>> xw, gw;
+        xw = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
+        if constexpr (GATE) gw = load_vector<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns);
+        unpack<DT, K_VEC<DT>>(xw, x);
+        if constexpr (GATE) unpack<DT, K_VEC<DT>>(gw, g);
 #pragma unroll
         for (int i = 0; i < K_VEC<DT>; ++i) {
             y[i] = act<DT, ACT>(x[i]);
@@ -79,8 +82,8 @@ __global__ __launch_bounds__(T) void activate_kernel(ActivateK k)
         }
         store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, a.row)), a.c, k.columns, y);
         if constexpr (HELD) {
-            store_held<DT>(k.hx, a.row, a.c, k.columns, x);
-            if constexpr (GATE) store_held<DT>(k.hg, a.row, a.c, k.columns, g);
+            store_held<DT>(k.hx, a.row, a.c, k.columns, xw, x);
+            if constexpr (GATE) store_held<DT>(k.hg, a.row, a.c, k.columns, gw, g);
         }
     }
 }
@@ -129,8 +132,9 @@ __global__ __launch_bounds__(T) void pack8_kernel(ActivateK k)
             load_held<DT>(k.hx, a.row, a.c, k.columns, x);
             store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, a.row)), a.c, k.columns, x);
         } else {
-            load_cols<DT>(row_of<DT>(k.x, a.row), a.c, k.columns, x);
-            store_held<DT>(k.hx, a.row, a.c, k.columns, x);
+            const Raw<DT, K_VEC<DT>> w = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
+            unpack<DT, K_VEC<DT>>(w, x);
+            store_held<DT>(k.hx, a.row, a.c, k.columns, w, x);
         }
     }
 }

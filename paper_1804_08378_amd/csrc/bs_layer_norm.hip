@@ -42,7 +42,7 @@ __global__ __launch_bounds__(T) void layer_norm_kernel(LayerNormK k)
             float v[VEC], s = 0.0f, q = 0.0f;
             load_total<DT>(k, row, c, v);
             if (k.total.p) store_cols<DT>(const_cast<char *>(row_of<DT>(k.total, row)), c, k.C, v);
-            if (k.held.codes) store_held<DT>(k.held, row, c, k.C, v);
+            if (k.held.codes) store_held<DT>(k.held, row, c, k.C, to_words<DT>(v), v);
             if (c >= k.C) break;  // (the lane's last vector)
             const float n = (float)min(k.C - c, (uint32_t)VEC);
 #pragma unroll
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(T) void layer_norm_kernel(LayerNormK k)
         const float all = group_sum<T>(mean * count, lds[0]) / (float)k.C;
         const float d = mean - all;
         const float var = group_sum<T>(__builtin_fmaf(d * d, count, m2), lds[1]) / (float)k.C;
-        const float rstd = 1.0f / sqrtf(var + k.eps);
+        const float rstd = reciprocal_root(var + k.eps);
         if (k.stats && threadIdx.x == 0) {
             k.stats[2 * row] = all;
             k.stats[2 * row + 1] = rstd;

@@ -37,7 +37,9 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
         }
         return (float)n;
     };
-    const float columns = (float)k.C;
+    const float share = 1.0f / (float)k.C, own = W > 1 ? columns_of(threadIdx.x / 64) : 0.0f;
+    const float wave_share = W > 1 ? (own > 0.0f ? 1.0f / own : 0.0f) : share;
+    const float other = W > 1 ? columns_of(threadIdx.x % (W > 1 ? W : 1)) : 0.0f;  // columns of the wave whose sums the lane joins
     Raw<DT, VEC> x[NV], a[NV];
     auto load = [&](uint64_t row) {
 #pragma unroll
@@ -72,8 +74,7 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
         }
         if constexpr (AHEAD) load(first + (uint64_t)gridDim.x * TEAMS + team);
         s = lanes_sum<TEAM < 64 ? TEAM : 64>(s);
-        const float n = W > 1 ? columns_of(threadIdx.x / 64) : columns;
-        float mean = n > 0.0f ? s / n : 0.0f, m2 = 0.0f;  // of a wave's columns
+        float mean = s * wave_share, m2 = 0.0f;  // of a wave's columns
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const uint32_t c = (j * TEAM + lane) * VEC;
@@ -81,10 +82,15 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
             if (c < k.C) {
                 float v[VEC];
                 unpack<DT, VEC>(t[j], v);
+                if (whole) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float d = whole || c + i < k.C ? v[i] - mean : 0.0f;
-                    m2 = __builtin_fmaf(d, d, m2);
+                    for (int i = 0; i < VEC; ++i) m2 = __builtin_fmaf(v[i] - mean, v[i] - mean, m2);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        const float d = c + i < k.C ? v[i] - mean : 0.0f;
+                        m2 = __builtin_fmaf(d, d, m2);
+                    }
                 }
             }
         }
@@ -95,11 +101,11 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
                 lds[turn][threadIdx.x / 64][1] = m2;
             }
             __syncthreads();  // (the other turn's values are read before the next barrier)
-            const float nw = columns_of(threadIdx.x % W), mw = lds[turn][threadIdx.x % W][0], qw = lds[turn][threadIdx.x % W][1];
-            mean = lanes_sum<W>(nw * mw) / columns;
-            m2 = lanes_sum<W>(__builtin_fmaf(nw * (mw - mean), mw - mean, qw));
+            const float mw = lds[turn][threadIdx.x % W][0], qw = lds[turn][threadIdx.x % W][1];
+            mean = lanes_sum<W>(other * mw) * share;
+            m2 = lanes_sum<W>(__builtin_fmaf(other * (mw - mean), mw - mean, qw));
         }
-        const float rstd = 1.0f / sqrtf(m2 / columns + k.eps);
+        const float rstd = reciprocal_root(__builtin_fmaf(m2, share, k.eps));
         if (row >= k.rows) continue;  // (teams of one wave)
         if (k.stats && lane == 0) *reinterpret_cast<float2 *>(k.stats + 2 * row) = make_float2(mean, rstd);
 #pragma unroll
@@ -109,7 +115,7 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
             if (ADD && k.total.p) store_vector<DT>(const_cast<char *>(row_of<DT>(k.total, row)), c, k.C, t[j]);
             float v[VEC], wj[VEC], bj[VEC];
             unpack<DT, VEC>(t[j], v);
-            if (k.held.codes) store_held<DT>(k.held, row, c, k.C, v);
+            if (k.held.codes) store_held<DT>(k.held, row, c, k.C, t[j], v);
             if constexpr (!HOLD) {
                 load_row_params<DT>(k.weight, k.f32_params, afresh(c), k.C, 1.0f, wj);
                 load_row_params<DT>(k.bias, k.f32_params, afresh(c), k.C, 0.0f, bj);

@@ -206,39 +206,71 @@ constexpr int K_SWAP1 = 0xb1, K_SWAP2 = 0x4e, K_MIRROR8 = 0x141, K_MIRROR16 = 0x
 
 constexpr uint32_t K_INF = 0x7f800000u;
 
-// A lane's part of a block as codes, and the block's exponent.  All lanes of the block call it, columns behind the row's last hold 0.
+// Over the lanes of a block.
 template <int DT>
-BS_DEV uint32_t to_8_bits(const float (&v)[K_VEC<DT>], uint32_t (&codes)[K_VEC<DT> / 4])
+BS_DEV uint32_t block_max(uint32_t v)
 {
-    uint32_t top = 0, all = 0;
+    v = max(v, swapped<K_SWAP1>(v));
+    v = max(v, swapped<K_SWAP2>(v));
+    return K_BLOCK_LANES<DT> == 8 ? max(v, swapped<K_MIRROR8>(v)) : v;
+}
+
+// The largest magnitude of a lane's numbers as float32's bits, infinities and NaN above all others.
+template <int DT>
+BS_DEV uint32_t largest(const Raw<DT, K_VEC<DT>> &r)
+{
+    const uint32_t w[4] = {r.q.x, r.q.y, r.q.z, r.q.w};
+    if constexpr (DT == DT_F32) {
+        return max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
+    } else {  // two at a time
+        typedef uint16_t h2 __attribute__((ext_vector_type(2)));
+        h2 m = __builtin_bit_cast(h2, w[0] & 0x7fff7fffu);
 #pragma unroll
-    for (int i = 0; i < K_VEC<DT>; ++i) {
-        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
-        top = max(top, b < K_INF ? b : 0u);
-        all = max(all, b);
+        for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(h2, w[i] & 0x7fff7fffu));
+        const uint32_t h = m.x > m.y ? m.x : m.y;
+        return DT == DT_BF16 ? h << 16 : __float_as_uint(half_up<DT>(h));
     }
-    top = max(top, swapped<K_SWAP1>(top));
-    top = max(top, swapped<K_SWAP2>(top));
-    if constexpr (K_BLOCK_LANES<DT> == 8) top = max(top, swapped<K_MIRROR8>(top));
-    const uint32_t e = min((top + 0x30000u) >> 23, DT == DT_F16 ? 142u : 254u);
-    const int shift = 133 - (int)e;
+}
+
+// Are there numbers in the wave that the short way does not serve?  (A branch that the compiler must not turn into choices of every lane.)
+BS_DEV bool any_lane(bool b) { return __builtin_expect(__builtin_amdgcn_ballot_w64(b) != 0, 0); }
+
+// A lane's part of a block as codes, and the block's exponent.  `r` and `v`: the same numbers.  All lanes of the block call it, columns behind the row's
+// last hold 0.
+template <int DT>
+BS_DEV uint32_t to_8_bits(const Raw<DT, K_VEC<DT>> &r, const float (&v)[K_VEC<DT>], uint32_t (&codes)[K_VEC<DT> / 4])
+{
+    constexpr int VEC = K_VEC<DT>;
+    constexpr uint32_t L = DT == DT_F16 ? 142u : 254u;
+    uint32_t top = block_max<DT>(largest<DT>(r)), e = (top + 0x30000u) >> 23;
+    float n[VEC];  // 1.5 * 2^23 and a number of steps: the sum's last bits are that number rounded, ties to even
+    if (any_lane(e > L || (e < 6 && top != 0))) {
+        asm volatile("");
+        top = 0;
 #pragma unroll
-    for (int w = 0; w < K_VEC<DT> / 4; ++w) {
-        uint32_t b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float q = __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(v[4 * w + i], shift), -126.0f, 126.0f);
-            b[i] = __float_as_uint(q + 12582912.0f) & 0xffu;  // 1.5 * 2^23 in front: the sum's last bits are the number rounded, ties to even
+        for (int i = 0; i < VEC; ++i) {
+            const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
+            top = max(top, m < K_INF ? m : 0u);
         }
-        codes[w] = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+        top = block_max<DT>(top);
+        e = min((top + 0x30000u) >> 23, L);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
+            const float q = __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(v[i], 133 - (int)e), -126.0f, 126.0f);
+            n[i] = 12582912.0f + (m > K_INF ? -128.0f : m < K_INF ? q : __uint_as_float(0x42fe0000u | (__float_as_uint(v[i]) & 0x80000000u)));  // (127)
+        }
+    } else {
+        const float steps = __uint_as_float((260u - e) << 23);  // 2^(133 - e); of a block of zeros any number
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) n[i] = __builtin_fmaf(v[i], steps, 12582912.0f);
     }
-    if (all >= K_INF) {
 #pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i) {
-            const uint32_t b = __float_as_uint(v[i]), m = b & 0x7fffffffu, at = 8 * (i % 4);
-            const uint32_t code = m > K_INF ? 0x80u : b == m ? 0x7fu : 0x81u;
-            if (m >= K_INF) codes[i / 4] = (codes[i / 4] & ~(0xffu << at)) | code << at;
-        }
+    for (int w = 0; w < VEC / 4; ++w) {
+        // the lowest bytes of four numbers
+        const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(n[4 * w + 1]), __float_as_uint(n[4 * w]), 0x0c0c0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(n[4 * w + 3]), __float_as_uint(n[4 * w + 2]), 0x04000c0cu);
+        codes[w] = lo | hi;
     }
     return e;
 }
@@ -254,7 +286,8 @@ BS_DEV void from_8_bits(const uint32_t (&codes)[K_VEC<DT> / 4], uint32_t e, floa
         most = __builtin_fmaxf(most, __builtin_fabsf(n));
         v[i] = n * step;
     }
-    if (most >= 127.0f) {
+    if (any_lane(most >= 127.0f)) {
+        asm volatile("");
 #pragma unroll
         for (int i = 0; i < K_VEC<DT>; ++i) {
             const int n = (int)(int8_t)(codes[i / 4] >> (8 * (i % 4)));
@@ -294,16 +327,22 @@ BS_DEV void load_held(const HeldRows &h, uint64_t row, uint32_t c, uint32_t colu
 
 // The other way: all lanes of a block call it together.
 template <int DT>
-BS_DEV void store_held(const HeldRows &h, uint64_t row, uint32_t c, uint32_t columns, const float (&v)[K_VEC<DT>])
+BS_DEV void store_held(const HeldRows &h, uint64_t row, uint32_t c, uint32_t columns, const Raw<DT, K_VEC<DT>> &r, const float (&v)[K_VEC<DT>])
 {
     uint32_t codes[K_VEC<DT> / 4];
-    const uint32_t e = to_8_bits<DT>(v, codes);
+    const uint32_t e = to_8_bits<DT>(r, v, codes);
     store_codes<DT>(h.codes + row * columns, c, columns, codes);
     const uint32_t blocks = (columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
     if (c < columns && c % BS_PACK8_BLOCK == 0) h.exponents[row * blocks + c / BS_PACK8_BLOCK] = (uint8_t)e;
 }
 
 // ------------------------------------------------------------------------------------------------ sums
+// 1 / sqrt(v) by the instruction (a unit in the last place), which takes subnormal numbers for 0: small ones are scaled.
+BS_DEV float reciprocal_root(float v)
+{
+    const bool small = v < 0x1p-64f;
+    return __builtin_amdgcn_rsqf(small ? v * 0x1p80f : v) * (small ? 0x1p40f : 1.0f);
+}
 BS_DEV float lane_swapped_sum(float v)  // over rows of 16 lanes, the same in each of them
 {
     v += __uint_as_float(swapped<K_SWAP1>(__float_as_uint(v)));
