@@ -73,6 +73,8 @@ __global__ __launch_bounds__(T) void activate_kernel(ActivateK k)
         Raw<DT, K_VEC<DT>> xw, gw;
         xw = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
         if constexpr (GATE) gw = load_vector<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns);
+        xw = settled<DT>(xw, a.c, k.columns);
+        if constexpr (GATE) gw = settled<DT>(gw, a.c, k.columns);
         unpack<DT, K_VEC<DT>>(xw, x);
         if constexpr (GATE) unpack<DT, K_VEC<DT>>(gw, g);
 #pragma unroll
@@ -99,11 +101,18 @@ __global__ __launch_bounds__(T) void activate_grad_kernel(ActivateK k)
         if (l >= left) return;
         const At a = place.at<DT>(k, l);
         float x[K_VEC<DT>], g[K_VEC<DT>], dy[K_VEC<DT>], dg[K_VEC<DT>];
-        if constexpr (HELD) load_held<DT>(k.hx, a.row, a.c, k.columns, x);
-        else load_cols<DT>(row_of<DT>(k.x, a.row), a.c, k.columns, x);
-        if constexpr (GATE && HELD) load_held<DT>(k.hg, a.row, a.c, k.columns, g);
-        if constexpr (GATE && !HELD) load_cols<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns, g);
-        load_cols<DT>(row_of<DT>(k.dy, a.row), a.c, k.columns, dy);
+        HeldVector<DT> hx, hg;
+        Raw<DT, K_VEC<DT>> xw, gw, dw;
+        if constexpr (HELD) hx.load(k.hx, a.row, a.c, k.columns);
+        else xw = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
+        if constexpr (GATE && HELD) hg.load(k.hg, a.row, a.c, k.columns);
+        if constexpr (GATE && !HELD) gw = load_vector<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns);
+        dw = load_vector<DT>(row_of<DT>(k.dy, a.row), a.c, k.columns);
+        if constexpr (HELD) hx.numbers(a.c, k.columns, x);
+        else unpack<DT, K_VEC<DT>>(settled<DT>(xw, a.c, k.columns), x);
+        if constexpr (GATE && HELD) hg.numbers(a.c, k.columns, g);
+        if constexpr (GATE && !HELD) unpack<DT, K_VEC<DT>>(settled<DT>(gw, a.c, k.columns), g);
+        unpack<DT, K_VEC<DT>>(settled<DT>(dw, a.c, k.columns), dy);
 #pragma unroll
         for (int i = 0; i < K_VEC<DT>; ++i) {
             float value, slope;
@@ -129,10 +138,12 @@ __global__ __launch_bounds__(T) void pack8_kernel(ActivateK k)
         const At a = place.at<DT>(k, l);
         float x[K_VEC<DT>];
         if constexpr (BACK) {
-            load_held<DT>(k.hx, a.row, a.c, k.columns, x);
+            HeldVector<DT> h;
+            h.load(k.hx, a.row, a.c, k.columns);
+            h.numbers(a.c, k.columns, x);
             store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, a.row)), a.c, k.columns, x);
         } else {
-            const Raw<DT, K_VEC<DT>> w = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
+            const Raw<DT, K_VEC<DT>> w = settled<DT>(load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns), a.c, k.columns);
             unpack<DT, K_VEC<DT>>(w, x);
             store_held<DT>(k.hx, a.row, a.c, k.columns, w, x);
         }

@@ -80,8 +80,13 @@ __global__ __launch_bounds__(T) void layer_norm_kernel(LayerNormK k)
 template <int DT>
 BS_DEV void load_grad(const LayerNormK &k, uint64_t row, uint32_t c, float mean, float rstd, float (&xh)[K_VEC<DT>], float (&dy)[K_VEC<DT>])
 {
-    if (k.held.codes) load_held<DT>(k.held, row, c, k.C, xh);
-    else load_cols<DT>(row_of<DT>(k.x, row), c, k.C, xh);
+    if (k.held.codes) {
+        HeldVector<DT> h;
+        h.load(k.held, row, c, k.C);
+        h.numbers(c, k.C, xh);
+    } else {
+        load_cols<DT>(row_of<DT>(k.x, row), c, k.C, xh);
+    }
     load_cols<DT>(row_of<DT>(k.dy, row), c, k.C, dy);
 #pragma unroll
     for (int i = 0; i < K_VEC<DT>; ++i) xh[i] = (xh[i] - mean) * rstd;

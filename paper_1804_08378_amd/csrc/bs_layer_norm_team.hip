@@ -58,12 +58,13 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
         float s = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            t[j] = x[j];
+            const uint32_t c = (j * TEAM + lane) * VEC;
+            t[j] = settled<DT>(x[j], c, k.C);
             float v[VEC];
             if constexpr (ADD) {
                 float add[VEC];
-                unpack<DT, VEC>(x[j], v);
-                unpack<DT, VEC>(a[j], add);
+                unpack<DT, VEC>(t[j], v);
+                unpack<DT, VEC>(settled<DT>(a[j], c, k.C), add);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[i] += add[i];
                 t[j] = to_words<DT>(v);
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
             }
 #pragma unroll
             for (int i = 0; i < VEC; ++i) v[i] = __builtin_fmaf((v[i] - mean) * rstd, HOLD ? w[HOLD ? j : 0][i] : wj[i], HOLD ? b[HOLD ? j : 0][i] : bj[i]);
-            store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, row)), c, k.C, v);
+            store_cols<DT, !ADD>(const_cast<char *>(row_of<DT>(k.y, row)), c, k.C, v);  // behind an addition the next layer reads y from the caches
             if constexpr (!HOLD) __builtin_amdgcn_sched_barrier(0);  // (one vector's numbers at a time in registers)
         }
     }

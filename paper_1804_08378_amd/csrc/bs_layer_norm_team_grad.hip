@@ -15,23 +15,20 @@ template <int DT, bool HELD>
 struct Kept {
     Raw<DT, K_VEC<DT>> words;
     BS_DEV void load(const LayerNormK &k, uint64_t row, uint32_t c) { words = load_vector<DT>(row_of<DT>(k.x, row), c, k.C); }
+    BS_DEV void settle(uint32_t c, uint32_t columns) { words = settled<DT>(words, c, columns); }
     BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { unpack<DT, K_VEC<DT>>(words, v); }
     BS_DEV void forget() { bs::forget(words.q); }
 };
 template <int DT>
 struct Kept<DT, true> {
-    uint32_t codes[K_VEC<DT> / 4], exponent;
-    BS_DEV void load(const LayerNormK &k, uint64_t row, uint32_t c)
-    {
-        load_codes<DT>(k.held.codes + row * k.C, c, k.C, codes);
-        const uint32_t blocks = (k.C + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
-        exponent = c < k.C ? k.held.exponents[row * blocks + c / BS_PACK8_BLOCK] : 0u;
-    }
-    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { from_8_bits<DT>(codes, exponent, v); }
+    HeldVector<DT> h;
+    BS_DEV void load(const LayerNormK &k, uint64_t row, uint32_t c) { h.load(k.held, row, c, k.C); }
+    BS_DEV void settle(uint32_t c, uint32_t columns) { settle_codes<DT>(h.codes, c, columns); }
+    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { from_8_bits<DT>(h.codes, h.exponent, v); }
     BS_DEV void forget()
     {
 #pragma unroll
-        for (int i = 0; i < K_VEC<DT> / 4; ++i) asm("" : "+v"(codes[i]));
+        for (int i = 0; i < K_VEC<DT> / 4; ++i) asm("" : "+v"(h.codes[i]));
     }
 };
 
@@ -43,7 +40,7 @@ template <int DT, int TEAM, int NV, bool HELD, Sums SUMS>
 __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
 {
     constexpr int VEC = K_VEC<DT>, W = TEAM / 64;
-    constexpr bool HOLD = NV * VEC <= 16, AHEAD = TEAM < 1024;  // weights stay in registers; the next row is loaded ahead
+    constexpr bool HOLD = NV * VEC <= 8, AHEAD = NV <= 2;  // weights stay in registers; the next row is loaded ahead
     constexpr uint32_t TEAMS = T / TEAM;
     constexpr int COLUMNS = TEAM * NV * VEC;
     constexpr uint32_t SUMMED = TEAM < 64 ? T / 64 : TEAMS;  // parts of a column's sum in a work-group
@@ -59,6 +56,8 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
     if constexpr (SUMS == SUMS_LDS)  // (a lane adds to its own columns only)
         for (int i = 0; i < NV * VEC; ++i) sums[0][i * TEAM + lane] = sums[1][i * TEAM + lane] = 0.0f;
     const float share = 1.0f / (float)k.C;
+    // a lane's first column of its j-th vector; of several ones worked out at every use, where the compiler would keep all that follows from it
+    auto column = [&](int j) { return HOLD ? (j * TEAM + lane) * VEC : afresh((j * TEAM + lane) * VEC); };
     Kept<DT, HELD> x[NV], nx[NV];
     Raw<DT, VEC> dy[NV], dt[NV], ndy[NV], ndt[NV];
     float2 stats;
@@ -67,7 +66,7 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
         stats = on ? *reinterpret_cast<const float2 *>(k.stats + 2 * row) : make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const uint32_t c = on ? (j * TEAM + lane) * VEC : k.C;
+            const uint32_t c = on ? column(j) : k.C;
             nx[j].load(k, row, c);
             ndy[j] = load_vector<DT>(row_of<DT>(k.dy, row), c, k.C);
             if (AHEAD && k.dt.p) ndt[j] = load_vector<DT>(row_of<DT>(k.dt, row), c, k.C);
@@ -78,14 +77,14 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
         float wj[VEC];
         x[j].numbers(xh);
         unpack<DT, VEC>(dy[j], g);
-        if constexpr (!HOLD) load_row_params<DT>(k.weight, k.f32_params, afresh((j * TEAM + lane) * VEC), k.C, 1.0f, wj);
+        if constexpr (!HOLD) load_row_params<DT>(k.weight, k.f32_params, column(j), k.C, 1.0f, wj);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             xh[i] = (xh[i] - mean) * rstd;
             u[i] = g[i] * (HOLD ? w[HOLD ? j : 0][i] : wj[i]);
         }
     };
-    uint64_t first = (uint64_t)blockIdx.x * TEAMS;
+    uint64_t first = (uint64_t)blockIdx.x * TEAMS;  // the same for all lanes of a work-group
     if constexpr (AHEAD) load(first + team);
     for (uint32_t turn = 0; first < k.rows; first += (uint64_t)gridDim.x * TEAMS, turn ^= 1) {
         const uint64_t row = first + team;
@@ -96,12 +95,14 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
         for (int j = 0; j < NV; ++j) {
             x[j] = nx[j];
             dy[j] = ndy[j];
-            dt[j] = ndt[j];
+            if constexpr (AHEAD) dt[j] = ndt[j];
         }
         if constexpr (AHEAD) load(first + (uint64_t)gridDim.x * TEAMS + team);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float xh[VEC], g[VEC], u[VEC];
+            x[j].settle(column(j), k.C);
+            dy[j] = settled<DT>(dy[j], column(j), k.C);
             numbers(j, mean, rstd, xh, g, u);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
@@ -140,11 +141,11 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
                 forget(dy[j].q);
                 numbers(j, mean, rstd, xh, g, u);
                 if constexpr (!AHEAD)
-                    if (k.dt.p) dt[j] = load_vector<DT>(row_of<DT>(k.dt, row), (j * TEAM + lane) * VEC, k.C);
-                if (k.dt.p) unpack<DT, VEC>(dt[j], add);
+                    if (k.dt.p) dt[j] = load_vector<DT>(row_of<DT>(k.dt, row), column(j), k.C);
+                if (k.dt.p) unpack<DT, VEC>(settled<DT>(dt[j], column(j), k.C), add);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) u[i] = __builtin_fmaf(rstd, (u[i] - s1) - xh[i] * s2, add[i]);
-                store_cols<DT>(const_cast<char *>(row_of<DT>(k.dx, row)), (j * TEAM + lane) * VEC, k.C, u);
+                store_cols<DT>(const_cast<char *>(row_of<DT>(k.dx, row)), column(j), k.C, u);
                 if constexpr (!HOLD) __builtin_amdgcn_sched_barrier(0);  // (one vector's numbers at a time in registers)
             }
     }

@@ -123,24 +123,48 @@ BS_DEV void store_first(char *p, uint32_t n, const uint32_t (&w)[N])
         if (bytes & 1) p[at] = (char)(word_at(w, at) >> (8 * (at & 2)));
 }
 
-// A lane's vector of a row as it stands in memory; columns from `columns` on are 0 and are not read.
+// A lane's vector of a row as it stands in memory.  The row's last vector, where it is not whole, is the whole one that ends with the row, so that it is
+// one load whose result nothing waits for here; `settled` moves its columns to their places, with 0 behind the last.  (Rows shorter than a vector
+// are read in pieces; lanes behind the last column read nothing and hold 0.)
 template <int DT>
 BS_DEV Raw<DT, K_VEC<DT>> load_vector(const char *row, uint32_t c, uint32_t columns)
 {
-    const char *p = row + (uint64_t)c * K_ES<DT>;
     uint32_t w[4] = {};
-    if (c + K_VEC<DT> <= columns) load_words<4, K_ES<DT>>(p, w);
-    else if (c < columns) load_first<4, K_ES<DT>>(p, columns - c, w);
+    if (columns >= K_VEC<DT>) {
+        if (c < columns) load_words<4, K_ES<DT>>(row + (uint64_t)min(c, columns - K_VEC<DT>) * K_ES<DT>, w);
+    } else if (c < columns) {
+        load_first<4, K_ES<DT>>(row + (uint64_t)c * K_ES<DT>, columns - c, w);
+    }
     Raw<DT, K_VEC<DT>> r;
     r.q = make_uint4(w[0], w[1], w[2], w[3]);
     return r;
 }
+// Elements by which a lane's vector began early: fewer than a vector's.
+template <int VEC>
+BS_DEV uint32_t early_by(uint32_t c, uint32_t columns)
+{
+    return columns >= VEC && c < columns && c + VEC > columns ? c + VEC - columns : 0;
+}
 template <int DT>
+BS_DEV Raw<DT, K_VEC<DT>> settled(const Raw<DT, K_VEC<DT>> &r, uint32_t c, uint32_t columns)
+{
+    if (columns % K_VEC<DT> == 0) return r;  // (the same for all lanes)
+    const uint32_t by = early_by<K_VEC<DT>>(c, columns) * K_ES<DT> * 8;  // bits
+    uint64_t lo = (uint64_t)r.q.y << 32 | r.q.x, hi = (uint64_t)r.q.w << 32 | r.q.z;
+    lo = by & 64 ? hi : lo;
+    hi = by & 64 ? 0 : hi;
+    lo = lo >> (by & 63) | (hi << 1) << (63 - (by & 63));
+    hi >>= by & 63;
+    Raw<DT, K_VEC<DT>> s;
+    s.q = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+    return s;
+}
+template <int DT, bool NT = true>
 BS_DEV void store_vector(char *row, uint32_t c, uint32_t columns, const Raw<DT, K_VEC<DT>> &r)
 {
     char *p = row + (uint64_t)c * K_ES<DT>;
     const uint32_t w[4] = {r.q.x, r.q.y, r.q.z, r.q.w};
-    if (c + K_VEC<DT> <= columns) store_words<4, K_ES<DT>, true>(p, w);
+    if (c + K_VEC<DT> <= columns) store_words<4, K_ES<DT>, NT>(p, w);
     else if (c < columns) store_first<4, K_ES<DT>>(p, columns - c, w);
 }
 
@@ -162,12 +186,12 @@ BS_DEV Raw<DT, K_VEC<DT>> to_words(const float (&v)[K_VEC<DT>])
 template <int DT>
 BS_DEV void load_cols(const char *row, uint32_t c, uint32_t columns, float (&v)[K_VEC<DT>])
 {
-    unpack<DT, K_VEC<DT>>(load_vector<DT>(row, c, columns), v);
+    unpack<DT, K_VEC<DT>>(settled<DT>(load_vector<DT>(row, c, columns), c, columns), v);
 }
-template <int DT>
+template <int DT, bool NT = true>
 BS_DEV void store_cols(char *row, uint32_t c, uint32_t columns, const float (&v)[K_VEC<DT>])
 {
-    store_vector<DT>(row, c, columns, to_words<DT>(v));
+    store_vector<DT, NT>(row, c, columns, to_words<DT>(v));
 }
 
 // Parameters of a lane's columns, `none` where there are none; behind the last column: any number.
@@ -300,30 +324,53 @@ template <int DT>
 BS_DEV void store_codes(int8_t *row, uint32_t c, uint32_t columns, const uint32_t (&codes)[K_VEC<DT> / 4])
 {
     char *p = reinterpret_cast<char *>(row) + c;
-    if (c + K_VEC<DT> <= columns) store_words<K_VEC<DT> / 4, 1, true>(p, codes);
+    if (c + K_VEC<DT> <= columns) store_words<K_VEC<DT> / 4, 1, false>(p, codes);
     else if (c < columns) store_first<K_VEC<DT> / 4, 1>(p, columns - c, codes);
 }
 
+// As load_vector and settled.
 template <int DT>
 BS_DEV void load_codes(const int8_t *row, uint32_t c, uint32_t columns, uint32_t (&codes)[K_VEC<DT> / 4])
 {
-    const char *p = reinterpret_cast<const char *>(row) + c;
+    const char *p = reinterpret_cast<const char *>(row);
 #pragma unroll
     for (int i = 0; i < K_VEC<DT> / 4; ++i) codes[i] = 0;
-    if (c + K_VEC<DT> <= columns) load_words<K_VEC<DT> / 4, 1>(p, codes);
-    else if (c < columns) load_first<K_VEC<DT> / 4, 1>(p, columns - c, codes);
+    if (columns >= K_VEC<DT>) {
+        if (c < columns) load_words<K_VEC<DT> / 4, 1>(p + min(c, columns - K_VEC<DT>), codes);
+    } else if (c < columns) {
+        load_first<K_VEC<DT> / 4, 1>(p + c, columns - c, codes);
+    }
+}
+template <int DT>
+BS_DEV void settle_codes(uint32_t (&codes)[K_VEC<DT> / 4], uint32_t c, uint32_t columns)
+{
+    if (columns % K_VEC<DT> == 0) return;
+    const uint32_t by = early_by<K_VEC<DT>>(c, columns) * 8;
+    if constexpr (K_VEC<DT> == 4) {
+        codes[0] >>= by;
+    } else {
+        const uint64_t t = ((uint64_t)codes[1] << 32 | codes[0]) >> by;
+        codes[0] = (uint32_t)t;
+        codes[1] = (uint32_t)(t >> 32);
+    }
 }
 
-// A lane's vector of a row held in 8 bits, as numbers (0 behind the last column).
+// A lane's vector of a row held in 8 bits; `numbers`: 0 behind the last column.
 template <int DT>
-BS_DEV void load_held(const HeldRows &h, uint64_t row, uint32_t c, uint32_t columns, float (&v)[K_VEC<DT>])
-{
-    uint32_t codes[K_VEC<DT> / 4];
-    load_codes<DT>(h.codes + row * columns, c, columns, codes);
-    const uint32_t blocks = (columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
-    const uint32_t e = c < columns ? h.exponents[row * blocks + c / BS_PACK8_BLOCK] : 0u;
-    from_8_bits<DT>(codes, e, v);
-}
+struct HeldVector {
+    uint32_t codes[K_VEC<DT> / 4], exponent;
+    BS_DEV void load(const HeldRows &h, uint64_t row, uint32_t c, uint32_t columns)
+    {
+        load_codes<DT>(h.codes + row * columns, c, columns, codes);
+        const uint32_t blocks = (columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
+        exponent = c < columns ? h.exponents[row * blocks + c / BS_PACK8_BLOCK] : 0u;
+    }
+    BS_DEV void numbers(uint32_t c, uint32_t columns, float (&v)[K_VEC<DT>])
+    {
+        settle_codes<DT>(codes, c, columns);
+        from_8_bits<DT>(codes, exponent, v);
+    }
+};
 
 // The other way: all lanes of a block call it together.
 template <int DT>
