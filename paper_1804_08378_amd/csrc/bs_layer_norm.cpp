@@ -32,7 +32,8 @@ void fill(const bs_layer_norm_desc &d, LayerNormK &k)
 // Lanes that a row takes and their vectors; a row of 16384 elements (forward, 16 bits: 32768) is the longest that registers hold.
 LayerNormTeam team_of(const LayerNormK &k, int32_t dtype, bool backward)
 {
-    const uint64_t vectors = ceil_div(k.C, dtype == BS_F32 ? 4 : 8);
+    const uint64_t vec = dtype == BS_F32 ? 4 : 8, vectors = ceil_div(k.C, vec);
+    if (k.C < vec) return LayerNormTeam{0, 0, 0};  // (every lane reads a whole vector of the row)
     LayerNormTeam t{8, 1, 0};
     while (t.team < 1024 && (uint64_t)t.team < vectors) t.team *= 2;
     while ((uint64_t)t.team * t.vectors < vectors) t.vectors *= 2;

@@ -40,13 +40,15 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
     const float share = 1.0f / (float)k.C, own = W > 1 ? columns_of(threadIdx.x / 64) : 0.0f;
     const float wave_share = W > 1 ? (own > 0.0f ? 1.0f / own : 0.0f) : share;
     const float other = W > 1 ? columns_of(threadIdx.x % (W > 1 ? W : 1)) : 0.0f;  // columns of the wave whose sums the lane joins
+    const bool full = k.C == (uint32_t)(TEAM * NV * VEC);
     Raw<DT, VEC> x[NV], a[NV];
     auto load = [&](uint64_t row) {
+        row = min(row, k.rows - 1);  // (rows behind the last are not written)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const uint32_t c = row < k.rows ? (j * TEAM + lane) * VEC : k.C;
-            x[j] = load_vector<DT>(row_of<DT>(k.x, row), c, k.C);
-            if constexpr (ADD) a[j] = load_vector<DT>(row_of<DT>(k.addend, row), c, k.C);
+            const uint32_t at = read_column<DT>((j * TEAM + lane) * VEC, k.C);
+            x[j] = read_vector<DT>(k.x, row, at);
+            if constexpr (ADD) a[j] = read_vector<DT>(k.addend, row, at);
         }
     };
     uint64_t first = (uint64_t)blockIdx.x * TEAMS;  // the same for all lanes of a work-group
@@ -58,17 +60,17 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
         float s = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const uint32_t c = (j * TEAM + lane) * VEC;
-            t[j] = settled<DT>(x[j], c, k.C);
+            t[j] = x[j];
             float v[VEC];
             if constexpr (ADD) {
                 float add[VEC];
                 unpack<DT, VEC>(t[j], v);
-                unpack<DT, VEC>(settled<DT>(a[j], c, k.C), add);
+                unpack<DT, VEC>(a[j], add);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[i] += add[i];
                 t[j] = to_words<DT>(v);
             }
+            if (!full) t[j] = moved<DT>(t[j], early_by<VEC>((j * TEAM + lane) * VEC, k.C));
             unpack<DT, VEC>(t[j], v);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s += v[i];

@@ -14,21 +14,26 @@ namespace {
 template <int DT, bool HELD>
 struct Kept {
     Raw<DT, K_VEC<DT>> words;
-    BS_DEV void load(const LayerNormK &k, uint64_t row, uint32_t c) { words = load_vector<DT>(row_of<DT>(k.x, row), c, k.C); }
-    BS_DEV void settle(uint32_t c, uint32_t columns) { words = settled<DT>(words, c, columns); }
+    BS_DEV void read(const LayerNormK &k, uint64_t row, uint32_t c, uint32_t at) { words = read_vector<DT>(k.x, row, at); }
+    BS_DEV void move(uint32_t early) { words = moved<DT>(words, early); }
     BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { unpack<DT, K_VEC<DT>>(words, v); }
     BS_DEV void forget() { bs::forget(words.q); }
 };
 template <int DT>
 struct Kept<DT, true> {
-    HeldVector<DT> h;
-    BS_DEV void load(const LayerNormK &k, uint64_t row, uint32_t c) { h.load(k.held, row, c, k.C); }
-    BS_DEV void settle(uint32_t c, uint32_t columns) { settle_codes<DT>(h.codes, c, columns); }
-    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { from_8_bits<DT>(h.codes, h.exponent, v); }
+    uint32_t codes[K_VEC<DT> / 4], exponent;
+    BS_DEV void read(const LayerNormK &k, uint64_t row, uint32_t c, uint32_t at)
+    {
+        load_words<K_VEC<DT> / 4, 1>(reinterpret_cast<const char *>(k.held.codes) + row * k.C + at, codes);
+        const uint32_t blocks = (k.C + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
+        exponent = k.held.exponents[row * blocks + min(c, k.C - 1) / BS_PACK8_BLOCK];
+    }
+    BS_DEV void move(uint32_t early) { move_codes<DT>(codes, early); }
+    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { from_8_bits<DT>(codes, exponent, v); }
     BS_DEV void forget()
     {
 #pragma unroll
-        for (int i = 0; i < K_VEC<DT> / 4; ++i) asm("" : "+v"(h.codes[i]));
+        for (int i = 0; i < K_VEC<DT> / 4; ++i) asm("" : "+v"(codes[i]));
     }
 };
 
@@ -36,7 +41,7 @@ constexpr int T = K_LAYER_NORM_GRAD_THREADS;
 
 enum Sums { SUMS_REGISTERS, SUMS_LDS };  // of a lane's columns: where they are kept
 
-template <int DT, int TEAM, int NV, bool HELD, Sums SUMS>
+template <int DT, int TEAM, int NV, bool HELD, bool TOTAL, Sums SUMS>
 __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
 {
     constexpr int VEC = K_VEC<DT>, W = TEAM / 64;
@@ -61,15 +66,16 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
     Kept<DT, HELD> x[NV], nx[NV];
     Raw<DT, VEC> dy[NV], dt[NV], ndy[NV], ndt[NV];
     float2 stats;
+    const bool full = k.C == (uint32_t)COLUMNS;
     auto load = [&](uint64_t row) {
-        const bool on = row < k.rows;
-        stats = on ? *reinterpret_cast<const float2 *>(k.stats + 2 * row) : make_float2(0.0f, 0.0f);
+        row = min(row, k.rows - 1);  // (rows behind the last are emptied at their first use)
+        stats = *reinterpret_cast<const float2 *>(k.stats + 2 * row);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const uint32_t c = on ? column(j) : k.C;
-            nx[j].load(k, row, c);
-            ndy[j] = load_vector<DT>(row_of<DT>(k.dy, row), c, k.C);
-            if (AHEAD && k.dt.p) ndt[j] = load_vector<DT>(row_of<DT>(k.dt, row), c, k.C);
+            const uint32_t c = column(j), at = read_column<DT>(c, k.C);
+            nx[j].read(k, row, c, at);
+            ndy[j] = read_vector<DT>(k.dy, row, at);
+            if constexpr (AHEAD && TOTAL) ndt[j] = read_vector<DT>(k.dt, row, at);
         }
     };
     // xh and u of a vector, made of its words
@@ -89,20 +95,24 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
     for (uint32_t turn = 0; first < k.rows; first += (uint64_t)gridDim.x * TEAMS, turn ^= 1) {
         const uint64_t row = first + team;
         if constexpr (!AHEAD) load(row);
-        const float mean = stats.x, rstd = stats.y;
+        const bool on = row < k.rows;
+        const float mean = on ? stats.x : 0.0f, rstd = on ? stats.y : 0.0f;
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             x[j] = nx[j];
             dy[j] = ndy[j];
-            if constexpr (AHEAD) dt[j] = ndt[j];
+            if constexpr (AHEAD && TOTAL) dt[j] = ndt[j];
         }
         if constexpr (AHEAD) load(first + (uint64_t)gridDim.x * TEAMS + team);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float xh[VEC], g[VEC], u[VEC];
-            x[j].settle(column(j), k.C);
-            dy[j] = settled<DT>(dy[j], column(j), k.C);
+            if (!full || !on) {
+                const uint32_t early = on ? early_by<VEC>(column(j), k.C) : VEC;
+                x[j].move(early);
+                dy[j] = moved<DT>(dy[j], early);
+            }
             numbers(j, mean, rstd, xh, g, u);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
@@ -133,16 +143,17 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
         }
         s1 *= share;
         s2 *= share;
-        if (k.dx.p && row < k.rows)
+        if (k.dx.p && on)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 float xh[VEC], g[VEC], u[VEC], add[VEC] = {};
                 x[j].forget();
                 forget(dy[j].q);
                 numbers(j, mean, rstd, xh, g, u);
-                if constexpr (!AHEAD)
-                    if (k.dt.p) dt[j] = load_vector<DT>(row_of<DT>(k.dt, row), column(j), k.C);
-                if (k.dt.p) unpack<DT, VEC>(settled<DT>(dt[j], column(j), k.C), add);
+                if constexpr (TOTAL) {
+                    if constexpr (!AHEAD) dt[j] = read_vector<DT>(k.dt, row, read_column<DT>(column(j), k.C));
+                    unpack<DT, VEC>(full ? dt[j] : moved<DT>(dt[j], early_by<VEC>(column(j), k.C)), add);
+                }
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) u[i] = __builtin_fmaf(rstd, (u[i] - s1) - xh[i] * s2, add[i]);
                 store_cols<DT>(const_cast<char *>(row_of<DT>(k.dx, row)), column(j), k.C, u);
@@ -198,8 +209,10 @@ template <int DT, int TEAM, int NV, Sums SUMS>
 void launch(const LayerNormK &k, uint32_t groups, hipStream_t st)
 {
     const dim3 grid(groups), block(T);
-    if (k.held.codes) layer_norm_team_grad_kernel<DT, TEAM, NV, true, SUMS><<<grid, block, 0, st>>>(k);
-    else layer_norm_team_grad_kernel<DT, TEAM, NV, false, SUMS><<<grid, block, 0, st>>>(k);
+    if (k.held.codes && k.dt.p) layer_norm_team_grad_kernel<DT, TEAM, NV, true, true, SUMS><<<grid, block, 0, st>>>(k);
+    else if (k.held.codes) layer_norm_team_grad_kernel<DT, TEAM, NV, true, false, SUMS><<<grid, block, 0, st>>>(k);
+    else if (k.dt.p) layer_norm_team_grad_kernel<DT, TEAM, NV, false, true, SUMS><<<grid, block, 0, st>>>(k);
+    else layer_norm_team_grad_kernel<DT, TEAM, NV, false, false, SUMS><<<grid, block, 0, st>>>(k);
 }
 
 template <int DT>

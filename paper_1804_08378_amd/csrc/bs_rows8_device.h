@@ -139,25 +139,30 @@ BS_DEV Raw<DT, K_VEC<DT>> load_vector(const char *row, uint32_t c, uint32_t colu
     r.q = make_uint4(w[0], w[1], w[2], w[3]);
     return r;
 }
-// Elements by which a lane's vector began early: fewer than a vector's.
+// Elements by which a lane's vector began early, `VEC` of a lane behind the last column: none of its elements is of the row.
 template <int VEC>
 BS_DEV uint32_t early_by(uint32_t c, uint32_t columns)
 {
-    return columns >= VEC && c < columns && c + VEC > columns ? c + VEC - columns : 0;
+    return columns >= VEC && c + VEC > columns ? min(c + VEC - columns, (uint32_t)VEC) : 0;
 }
 template <int DT>
-BS_DEV Raw<DT, K_VEC<DT>> settled(const Raw<DT, K_VEC<DT>> &r, uint32_t c, uint32_t columns)
+BS_DEV Raw<DT, K_VEC<DT>> moved(const Raw<DT, K_VEC<DT>> &r, uint32_t early)
 {
-    if (columns % K_VEC<DT> == 0) return r;  // (the same for all lanes)
-    const uint32_t by = early_by<K_VEC<DT>>(c, columns) * K_ES<DT> * 8;  // bits
+    const uint32_t by = early * K_ES<DT> * 8;  // bits
     uint64_t lo = (uint64_t)r.q.y << 32 | r.q.x, hi = (uint64_t)r.q.w << 32 | r.q.z;
     lo = by & 64 ? hi : lo;
-    hi = by & 64 ? 0 : hi;
+    hi = by & (64 | 128) ? 0 : hi;
+    lo = by & 128 ? 0 : lo;
     lo = lo >> (by & 63) | (hi << 1) << (63 - (by & 63));
     hi >>= by & 63;
     Raw<DT, K_VEC<DT>> s;
     s.q = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
     return s;
+}
+template <int DT>
+BS_DEV Raw<DT, K_VEC<DT>> settled(const Raw<DT, K_VEC<DT>> &r, uint32_t c, uint32_t columns)
+{
+    return columns % K_VEC<DT> == 0 ? r : moved<DT>(r, early_by<K_VEC<DT>>(c, columns));  // (the same for all lanes)
 }
 template <int DT, bool NT = true>
 BS_DEV void store_vector(char *row, uint32_t c, uint32_t columns, const Raw<DT, K_VEC<DT>> &r)
@@ -342,17 +347,18 @@ BS_DEV void load_codes(const int8_t *row, uint32_t c, uint32_t columns, uint32_t
     }
 }
 template <int DT>
+BS_DEV void move_codes(uint32_t (&codes)[K_VEC<DT> / 4], uint32_t early)
+{
+    uint64_t t = codes[0];
+    if constexpr (K_VEC<DT> == 8) t |= (uint64_t)codes[1] << 32;
+    t = early == K_VEC<DT> ? 0 : t >> (early * 8);
+    codes[0] = (uint32_t)t;
+    if constexpr (K_VEC<DT> == 8) codes[1] = (uint32_t)(t >> 32);
+}
+template <int DT>
 BS_DEV void settle_codes(uint32_t (&codes)[K_VEC<DT> / 4], uint32_t c, uint32_t columns)
 {
-    if (columns % K_VEC<DT> == 0) return;
-    const uint32_t by = early_by<K_VEC<DT>>(c, columns) * 8;
-    if constexpr (K_VEC<DT> == 4) {
-        codes[0] >>= by;
-    } else {
-        const uint64_t t = ((uint64_t)codes[1] << 32 | codes[0]) >> by;
-        codes[0] = (uint32_t)t;
-        codes[1] = (uint32_t)(t >> 32);
-    }
+    if (columns % K_VEC<DT> != 0) move_codes<DT>(codes, early_by<K_VEC<DT>>(c, columns));
 }
 
 // A lane's vector of a row held in 8 bits; `numbers`: 0 behind the last column.
