@@ -29,25 +29,25 @@ void fill(const bs_layer_norm_desc &d, LayerNormK &k)
     k.eps = (float)d.eps;
 }
 
-// Lanes that a row takes and their vectors; a row of 16384 elements (forward, 16 bits: 32768) is the longest that registers hold.
+// Lanes that a row takes and their vectors; a row of 64 KiB is the longest that registers hold, one of 16384 elements the longest whose columns' sums
+// the backward pass holds too.
 LayerNormTeam team_of(const LayerNormK &k, int32_t dtype, bool backward)
 {
     const uint64_t vec = dtype == BS_F32 ? 4 : 8, vectors = ceil_div(k.C, vec);
-    if (k.C < vec) return LayerNormTeam{0, 0, 0};  // (every lane reads a whole vector of the row)
-    LayerNormTeam t{8, 1, 0};
+    LayerNormTeam t{8, 1, 0, k.C <= 16384};
+    if (k.C < vec || vectors > 4096) return LayerNormTeam{0, 0, 0, false};  // (every lane reads a whole vector of the row)
     while (t.team < 1024 && (uint64_t)t.team < vectors) t.team *= 2;
     while ((uint64_t)t.team * t.vectors < vectors) t.vectors *= 2;
-    if (t.vectors > (backward && dtype != BS_F32 ? 2 : 4)) return LayerNormTeam{0, 0, 0};
     const uint64_t threads = backward ? (uint64_t)K_LAYER_NORM_GRAD_THREADS : (uint64_t)(t.team <= 64 ? 256 : t.team), teams = threads / (uint64_t)t.team;
     t.groups = (uint32_t)std::min<uint64_t>(ceil_div(k.rows, teams), backward ? K_LAYER_NORM_GRAD_GROUPS : 256 * 2048 / threads);
     return t;
 }
 
-// Parts of the rows, whose sums a second launch joins: what the backward pass's work-groups leave, or of long rows 1024 tiles.
+// Parts of the rows, whose sums a second launch joins: what the backward pass's work-groups leave, or tiles of columns, 1024 of them in all.
 void parts(LayerNormK &k, const LayerNormTeam &t, int32_t dtype)
 {
     if (!k.rows) return;
-    if (t.team) {
+    if (t.sums) {
         k.parts = t.groups;
         return;
     }
@@ -135,15 +135,14 @@ bs_status bs_layer_norm_backward(const bs_layer_norm_desc *desc, const void *t, 
                                           {bytes_of(k.dx, k.rows, C, es), bytes_of(grad_weight, C * ps), bytes_of(grad_bias, C * ps),
                                            bytes_of(params ? workspace : nullptr, space(k))});
     if (alias != BS_OK) return alias;
+    if (!team.sums) k.part = nullptr;
     bs_status st = BS_OK;
-    if (k.rows && team.team) {
-        if (grad_x || params) st = launch_layer_norm_team_grad(k, team, desc->dtype, stream);
-        if (st != BS_OK || !params || k.parts == 1) return st;  // (one work-group writes the parameters' gradients itself)
-    } else if (k.rows) {
-        if (grad_x) st = launch_layer_norm(LAYER_NORM_GRAD, k, desc->dtype, stream);
-        if (st == BS_OK && params) st = launch_layer_norm(LAYER_NORM_GRAD_PARTS, k, desc->dtype, stream);
-    }
-    return st == BS_OK && params ? launch_layer_norm(LAYER_NORM_GRAD_JOIN, k, desc->dtype, stream) : st;
+    if (k.rows && team.team && (grad_x || (params && team.sums))) st = launch_layer_norm_team_grad(k, team, desc->dtype, stream);
+    else if (k.rows && grad_x) st = launch_layer_norm(LAYER_NORM_GRAD, k, desc->dtype, stream);
+    if (st != BS_OK || !params || (team.sums && k.parts == 1)) return st;  // (one work-group writes the parameters' gradients itself)
+    k.part = static_cast<float *>(workspace);
+    if (k.rows && !team.sums) st = launch_layer_norm(LAYER_NORM_GRAD_PARTS, k, desc->dtype, stream);
+    return st == BS_OK ? launch_layer_norm(LAYER_NORM_GRAD_JOIN, k, desc->dtype, stream) : st;
 }
 
 }  // extern "C"

@@ -29,10 +29,12 @@ struct LayerNormK {
 enum LayerNormPass { LAYER_NORM, LAYER_NORM_GRAD, LAYER_NORM_GRAD_PARTS, LAYER_NORM_GRAD_JOIN };
 bs_status launch_layer_norm(LayerNormPass pass, const LayerNormK &k, int32_t dtype, void *stream);
 
-// Rows in the registers of teams of lanes: lanes of a team, vectors of a lane, work-groups.  team == 0: rows too long for that.
+// Rows in the registers of teams of lanes: lanes of a team, vectors of a lane, work-groups; does the backward pass sum the gradients of weight and
+// bias on its way?  team == 0: rows too long (or short) for that.
 struct LayerNormTeam {
     int team, vectors;
     uint32_t groups;
+    bool sums;
 };
 bs_status launch_layer_norm_team(const LayerNormK &k, const LayerNormTeam &t, int32_t dtype, void *stream);
 bs_status launch_layer_norm_team_grad(const LayerNormK &k, const LayerNormTeam &t, int32_t dtype, void *stream);

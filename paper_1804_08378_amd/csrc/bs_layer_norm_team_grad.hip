@@ -1,6 +1,6 @@
 // Layer normalisation, backward, with the rows in registers (bs_layer_norm_team.h); formulas: bs_layer_norm.hip.
 //
-// A lane keeps the sums of dy and dy * xh of its columns over all rows of its team, in registers or, of long rows, in LDS; a work-group's teams are
+// A lane keeps the sums of dy and dy * xh of its columns over all rows of its team, in registers or, of long rows, in LDS (of rows over 16384 columns nowhere: bs_layer_norm.hip sums them); a work-group's teams are
 // added through LDS at the end, and the work-groups' sums are joined by a second launch, in orders that depend on sizes only: equal calls give equal
 // bits.  A work-group is as large as a compute unit takes, and there is one for each: the fewer there are, the fewer sums cross memory.
 #include <hip/hip_runtime.h>
@@ -39,13 +39,14 @@ struct Kept<DT, true> {
 
 constexpr int T = K_LAYER_NORM_GRAD_THREADS;
 
-enum Sums { SUMS_REGISTERS, SUMS_LDS };  // of a lane's columns: where they are kept
+enum Sums { SUMS_NONE, SUMS_REGISTERS, SUMS_LDS };  // of a lane's columns: where they are kept
 
 template <int DT, int TEAM, int NV, bool HELD, bool TOTAL, Sums SUMS>
 __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
 {
     constexpr int VEC = K_VEC<DT>, W = TEAM / 64;
     constexpr bool HOLD = NV * VEC <= 8, AHEAD = NV <= 2;  // weights stay in registers; the next row is loaded ahead
+    constexpr bool AGAIN = HELD && SUMS == SUMS_NONE;  // codes are read once more from the cache instead of kept in registers
     constexpr uint32_t TEAMS = T / TEAM;
     constexpr int COLUMNS = TEAM * NV * VEC;
     constexpr uint32_t SUMMED = TEAM < 64 ? T / 64 : TEAMS;  // parts of a column's sum in a work-group
@@ -147,7 +148,13 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 float xh[VEC], g[VEC], u[VEC], add[VEC] = {};
-                x[j].forget();
+                if constexpr (AGAIN) {
+                    const uint32_t c = column(j);
+                    x[j].read(k, row, c, read_column<DT>(c, k.C));
+                    if (!full) x[j].move(early_by<VEC>(c, k.C));
+                } else {
+                    x[j].forget();
+                }
                 forget(dy[j].q);
                 numbers(j, mean, rstd, xh, g, u);
                 if constexpr (TOTAL) {
@@ -160,7 +167,7 @@ __global__ __launch_bounds__(T) void layer_norm_team_grad_kernel(LayerNormK k)
                 if constexpr (!HOLD) __builtin_amdgcn_sched_barrier(0);  // (one vector's numbers at a time in registers)
             }
     }
-    if (!k.part) return;
+    if (SUMS == SUMS_NONE || !k.part) return;
     auto put = [&](int j, int i, float b, float g) {
         const uint32_t c = (j * TEAM + lane) * VEC + i;
         if (c >= k.C) return;
@@ -229,7 +236,9 @@ void launch_type(const LayerNormK &k, const LayerNormTeam &t, hipStream_t st)
     case 1024 * 16 + 1: launch<DT, 1024, 1, SUMS_REGISTERS>(k, t.groups, st); break;
     case 1024 * 16 + 2: launch<DT, 1024, 2, SUMS_LDS>(k, t.groups, st); break;
     case 1024 * 16 + 4:
-        if constexpr (DT == DT_F32) launch<DT, 1024, 4, SUMS_LDS>(k, t.groups, st);  // two floats a column: 128 KiB of LDS
+        // two floats a column: 128 KiB of LDS hold those of 16384 columns
+        if constexpr (DT == DT_F32) launch<DT, 1024, 4, SUMS_LDS>(k, t.groups, st);
+        else launch<DT, 1024, 4, SUMS_NONE>(k, t.groups, st);
         break;
     }
 }
