@@ -633,7 +633,7 @@ typedef struct bs_pack8_desc {
 /*
  * Enqueue x -> codes, exponents (bs_pack8) or codes, exponents -> x, rounded to its type (bs_unpack8), on `stream`.  Never synchronises,
  * never allocates.  x is aligned to its element size.  No output shares a byte with an input or another output.
- * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, columns < 1, stride below columns), BS_ERR_UNSUPPORTED (type; over 2^30 columns, 2^29 blocks of all
+ * Errors: BS_ERR_NULL, BS_ERR_SHAPE (rows < 0, columns < 1, stride below columns), BS_ERR_UNSUPPORTED (type; over 2^30 columns, 2^28 blocks of all
  *         rows, a stride over 2^40), BS_ERR_ALIGN, BS_ERR_ALIAS, BS_ERR_HIP.
  */
 BS_API bs_status bs_pack8(const bs_pack8_desc *desc, const void *x, int8_t *codes, uint8_t *exponents, void *stream);

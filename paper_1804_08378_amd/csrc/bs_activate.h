@@ -6,7 +6,6 @@
 namespace bs {
 
 constexpr int K_ACTIVATE_THREADS = 256;
-constexpr int K_ACTIVATE_UNROLL = 1;  // vectors of a lane
 
 struct ActivateK {
     RowTensor x, gate, y;     // y: what is written (pack8: nothing, unpack8: x)

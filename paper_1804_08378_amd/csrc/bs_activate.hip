@@ -10,36 +10,65 @@
 #include "bs_norm_device.h"
 #include "bs_rows8_device.h"
 
+#include <type_traits>
+
 namespace bs {
 namespace {
 
-constexpr int T = K_ACTIVATE_THREADS, U = K_ACTIVATE_UNROLL;
+constexpr int T = K_ACTIVATE_THREADS;
 
 struct At {
     uint64_t row;
     uint32_t c;
 };
 
-// The row and column of vector blockIdx.x * T * U + l.
-struct Place {
-    uint64_t row0;
-    uint32_t rest;
-    BS_DEV explicit Place(const ActivateK &k)
+BS_DEV bool on(const ActivateK &k) { return (uint64_t)blockIdx.x * T + threadIdx.x < k.vectors; }  // (whole blocks of lanes at a time)
+
+// The row and first column of the lane's vector.
+template <int DT>
+BS_DEV At place_of(const ActivateK &k)
+{
+    const uint64_t base = (uint64_t)blockIdx.x * T, row0 = k.vectors < (1u << 31) ? fdiv((uint32_t)base, k.by_row) : base / k.per_row;
+    const uint32_t t = (uint32_t)(base - row0 * k.per_row) + threadIdx.x, r = fdiv(t, k.by_row);
+    return At{row0 + r, (t - r * k.per_row) * K_VEC<DT>};
+}
+
+// A lane's vector of a tensor or of a tensor in 8 bits, behind `get` in flight, behind `place` as numbers' words.  SHORT: rows shorter than a vector, read
+// in pieces.
+template <int DT, bool SHORT>
+struct Words {
+    Raw<DT, K_VEC<DT>> r;
+    BS_DEV void get(const RowTensor &t, const At &a, uint32_t columns)
     {
-        const uint64_t base = (uint64_t)blockIdx.x * (T * U);
-        row0 = k.vectors < (1u << 31) ? fdiv((uint32_t)base, k.by_row) : base / k.per_row;
-        rest = (uint32_t)(base - row0 * k.per_row);
+        if constexpr (SHORT) r = load_vector<DT>(row_of<DT>(t, a.row), a.c, columns);
+        else r = read_vector<DT>(t, a.row, read_column<DT>(a.c, columns));
     }
-    template <int DT>
-    BS_DEV At at(const ActivateK &k, uint32_t l) const
+    BS_DEV void place(const At &a, uint32_t columns)
     {
-        const uint32_t t = rest + l, r = fdiv(t, k.by_row);
-        return At{row0 + r, (t - r * k.per_row) * K_VEC<DT>};
+        if (!SHORT && columns % BS_PACK8_BLOCK != 0) r = moved<DT>(r, early_by<K_VEC<DT>>(a.c, columns));
     }
+    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { unpack<DT, K_VEC<DT>>(r, v); }
+};
+template <int DT, bool SHORT>
+struct Codes {
+    HeldVector<DT> h;
+    BS_DEV void get(const HeldRows &t, const At &a, uint32_t columns)
+    {
+        if constexpr (SHORT) h.load(t, a.row, a.c, columns);
+        else h.read(t, a.row, a.c, columns);
+    }
+    BS_DEV void place(const At &a, uint32_t columns)
+    {
+        if (!SHORT && columns % BS_PACK8_BLOCK != 0) h.move(early_by<K_VEC<DT>>(a.c, columns));
+    }
+    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { h.numbers(v); }
 };
 
 template <int DT>
-BS_DEV const char *row_of(const RowTensor &t, uint64_t row) { return static_cast<const char *>(t.p) + row * t.stride * K_ES<DT>; }
+BS_DEV void store(const RowTensor &t, const At &a, uint32_t columns, const float (&v)[K_VEC<DT>])
+{
+    store_cols<DT>(const_cast<char *>(row_of<DT>(t, a.row)), a.c, columns, v);
+}
 
 template <int DT, int ACT>
 BS_DEV void act_and_slope(float z, float &value, float &slope)
@@ -59,95 +88,106 @@ BS_DEV void act_and_slope(float z, float &value, float &slope)
     }
 }
 
+template <int DT, int ACT, bool GATE, bool HELD, bool SHORT>
+BS_DEV void activate(const ActivateK &k, const At &a)
+{
+    Words<DT, SHORT> xw, gw;
+    xw.get(k.x, a, k.columns);
+    if constexpr (GATE) gw.get(k.gate, a, k.columns);
+    xw.place(a, k.columns);
+    if constexpr (GATE) gw.place(a, k.columns);
+    float x[K_VEC<DT>], g[K_VEC<DT>], y[K_VEC<DT>];
+    xw.numbers(x);
+    if constexpr (GATE) gw.numbers(g);
+#pragma unroll
+    for (int i = 0; i < K_VEC<DT>; ++i) {
+        y[i] = act<DT, ACT>(x[i]);
+        if constexpr (GATE) y[i] *= g[i];
+    }
+    store<DT>(k.y, a, k.columns, y);
+    if constexpr (HELD) {
+        store_held<DT>(k.hx, a.row, a.c, k.columns, xw.r, x);
+        if constexpr (GATE) store_held<DT>(k.hg, a.row, a.c, k.columns, gw.r, g);
+    }
+}
+
+template <int DT, int ACT, bool GATE, bool HELD, bool SHORT>
+BS_DEV void activate_grad(const ActivateK &k, const At &a)
+{
+    using Kept = typename std::conditional<HELD, Codes<DT, SHORT>, Words<DT, SHORT>>::type;
+    Kept xw, gw;
+    Words<DT, SHORT> dw;
+    if constexpr (HELD) {
+        xw.get(k.hx, a, k.columns);
+        if constexpr (GATE) gw.get(k.hg, a, k.columns);
+    } else {
+        xw.get(k.x, a, k.columns);
+        if constexpr (GATE) gw.get(k.gate, a, k.columns);
+    }
+    dw.get(k.dy, a, k.columns);
+    float x[K_VEC<DT>], g[K_VEC<DT>], dy[K_VEC<DT>], dg[K_VEC<DT>];
+    xw.place(a, k.columns);
+    if constexpr (GATE) gw.place(a, k.columns);
+    dw.place(a, k.columns);
+    xw.numbers(x);
+    if constexpr (GATE) gw.numbers(g);
+    dw.numbers(dy);
+#pragma unroll
+    for (int i = 0; i < K_VEC<DT>; ++i) {
+        float value, slope;
+        act_and_slope<DT, ACT>(x[i], value, slope);
+        dg[i] = dy[i] * value;
+        x[i] = dy[i] * slope;
+        if constexpr (GATE) x[i] *= g[i];
+    }
+    if (k.dx.p) store<DT>(k.dx, a, k.columns, x);
+    if (GATE && k.dg.p) store<DT>(k.dg, a, k.columns, dg);
+}
+
+template <int DT, bool BACK, bool SHORT>
+BS_DEV void pack8(const ActivateK &k, const At &a)
+{
+    float x[K_VEC<DT>];
+    if constexpr (BACK) {
+        Codes<DT, SHORT> h;
+        h.get(k.hx, a, k.columns);
+        h.place(a, k.columns);
+        h.numbers(x);
+        store<DT>(k.y, a, k.columns, x);
+    } else {
+        Words<DT, SHORT> w;
+        w.get(k.x, a, k.columns);
+        w.place(a, k.columns);
+        w.numbers(x);
+        store_held<DT>(k.hx, a.row, a.c, k.columns, w.r, x);
+    }
+}
+
 template <int DT, int ACT, bool GATE, bool HELD>
 __global__ __launch_bounds__(T) void activate_kernel(ActivateK k)
 {
-    const Place place(k);
-    const uint64_t left = k.vectors - (uint64_t)blockIdx.x * (T * U);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const uint32_t l = u * T + threadIdx.x;
-        if (l >= left) return;  // (whole blocks of lanes at a time)
-        const At a = place.at<DT>(k, l);
-        float x[K_VEC<DT>], g[K_VEC<DT>], y[K_VEC<DT>];
-        Raw<DT, K_VEC<DT>> xw, gw;
-        xw = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
-        if constexpr (GATE) gw = load_vector<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns);
-        xw = settled<DT>(xw, a.c, k.columns);
-        if constexpr (GATE) gw = settled<DT>(gw, a.c, k.columns);
-        unpack<DT, K_VEC<DT>>(xw, x);
-        if constexpr (GATE) unpack<DT, K_VEC<DT>>(gw, g);
-#pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i) {
-            y[i] = act<DT, ACT>(x[i]);
-            if constexpr (GATE) y[i] *= g[i];
-        }
-        store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, a.row)), a.c, k.columns, y);
-        if constexpr (HELD) {
-            store_held<DT>(k.hx, a.row, a.c, k.columns, xw, x);
-            if constexpr (GATE) store_held<DT>(k.hg, a.row, a.c, k.columns, gw, g);
-        }
-    }
+    if (!on(k)) return;
+    const At a = place_of<DT>(k);
+    if (k.columns < K_VEC<DT>) activate<DT, ACT, GATE, HELD, true>(k, a);
+    else activate<DT, ACT, GATE, HELD, false>(k, a);
 }
 
 template <int DT, int ACT, bool GATE, bool HELD>
 __global__ __launch_bounds__(T) void activate_grad_kernel(ActivateK k)
 {
-    const Place place(k);
-    const uint64_t left = k.vectors - (uint64_t)blockIdx.x * (T * U);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const uint32_t l = u * T + threadIdx.x;
-        if (l >= left) return;
-        const At a = place.at<DT>(k, l);
-        float x[K_VEC<DT>], g[K_VEC<DT>], dy[K_VEC<DT>], dg[K_VEC<DT>];
-        HeldVector<DT> hx, hg;
-        Raw<DT, K_VEC<DT>> xw, gw, dw;
-        if constexpr (HELD) hx.load(k.hx, a.row, a.c, k.columns);
-        else xw = load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns);
-        if constexpr (GATE && HELD) hg.load(k.hg, a.row, a.c, k.columns);
-        if constexpr (GATE && !HELD) gw = load_vector<DT>(row_of<DT>(k.gate, a.row), a.c, k.columns);
-        dw = load_vector<DT>(row_of<DT>(k.dy, a.row), a.c, k.columns);
-        if constexpr (HELD) hx.numbers(a.c, k.columns, x);
-        else unpack<DT, K_VEC<DT>>(settled<DT>(xw, a.c, k.columns), x);
-        if constexpr (GATE && HELD) hg.numbers(a.c, k.columns, g);
-        if constexpr (GATE && !HELD) unpack<DT, K_VEC<DT>>(settled<DT>(gw, a.c, k.columns), g);
-        unpack<DT, K_VEC<DT>>(settled<DT>(dw, a.c, k.columns), dy);
-#pragma unroll
-        for (int i = 0; i < K_VEC<DT>; ++i) {
-            float value, slope;
-            act_and_slope<DT, ACT>(x[i], value, slope);
-            dg[i] = dy[i] * value;
-            x[i] = dy[i] * slope;
-            if constexpr (GATE) x[i] *= g[i];
-        }
-        if (k.dx.p) store_cols<DT>(const_cast<char *>(row_of<DT>(k.dx, a.row)), a.c, k.columns, x);
-        if (GATE && k.dg.p) store_cols<DT>(const_cast<char *>(row_of<DT>(k.dg, a.row)), a.c, k.columns, dg);
-    }
+    if (!on(k)) return;
+    const At a = place_of<DT>(k);
+    if (k.columns < K_VEC<DT>) activate_grad<DT, ACT, GATE, HELD, true>(k, a);
+    else activate_grad<DT, ACT, GATE, HELD, false>(k, a);
 }
 
 template <int DT, bool BACK>
 __global__ __launch_bounds__(T) void pack8_kernel(ActivateK k)
 {
-    const Place place(k);
-    const uint64_t left = k.vectors - (uint64_t)blockIdx.x * (T * U);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const uint32_t l = u * T + threadIdx.x;
-        if (l >= left) return;
-        const At a = place.at<DT>(k, l);
-        float x[K_VEC<DT>];
-        if constexpr (BACK) {
-            HeldVector<DT> h;
-            h.load(k.hx, a.row, a.c, k.columns);
-            h.numbers(a.c, k.columns, x);
-            store_cols<DT>(const_cast<char *>(row_of<DT>(k.y, a.row)), a.c, k.columns, x);
-        } else {
-            const Raw<DT, K_VEC<DT>> w = settled<DT>(load_vector<DT>(row_of<DT>(k.x, a.row), a.c, k.columns), a.c, k.columns);
-            unpack<DT, K_VEC<DT>>(w, x);
-            store_held<DT>(k.hx, a.row, a.c, k.columns, w, x);
-        }
-    }
+    if (!on(k)) return;
+    const At a = place_of<DT>(k);
+    if (k.columns < K_VEC<DT>) pack8<DT, BACK, true>(k, a);
+    else pack8<DT, BACK, false>(k, a);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -192,7 +232,7 @@ void launch_type(RowPass pass, const ActivateK &k, int32_t activation, dim3 grid
 bs_status launch_rows(RowPass pass, const ActivateK &k, int32_t dtype, int32_t activation, void *stream)
 {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((uint32_t)((k.vectors + T * U - 1) / (T * U)));
+    const dim3 grid((uint32_t)((k.vectors + T - 1) / T));
     if (dtype == BS_F32) launch_type<DT_F32>(pass, k, activation, grid, st);
     else if (dtype == BS_BF16) launch_type<DT_BF16>(pass, k, activation, grid, st);
     else launch_type<DT_F16>(pass, k, activation, grid, st);

@@ -83,7 +83,8 @@ BS_DEV void load_grad(const LayerNormK &k, uint64_t row, uint32_t c, float mean,
     if (k.held.codes) {
         HeldVector<DT> h;
         h.load(k.held, row, c, k.C);
-        h.numbers(c, k.C, xh);
+        h.settle(c, k.C);
+        h.numbers(xh);
     } else {
         load_cols<DT>(row_of<DT>(k.x, row), c, k.C, xh);
     }

@@ -32,23 +32,6 @@ BS_DEV void put_params(const LayerNormK &k, uint32_t c, float b, float w)
     put(k.dweight, w);
 }
 
-template <int DT>
-BS_DEV const char *row_of(const RowTensor &t, uint64_t row) { return static_cast<const char *>(t.p) + row * t.stride * K_ES<DT>; }
-
-// Where a lane reads its vector of a row of VEC elements at least, so that every lane reads one of every row and no load stands behind a condition: the
-// compiler counts the loads in flight, and waits for all of them where it cannot.  `moved` puts the columns to their places at the first use.
-template <int DT>
-BS_DEV uint32_t read_column(uint32_t c, uint32_t columns) { return min(c, columns - K_VEC<DT>); }
-template <int DT>
-BS_DEV Raw<DT, K_VEC<DT>> read_vector(const RowTensor &t, uint64_t row, uint32_t at)
-{
-    uint32_t w[4];
-    load_words<4, K_ES<DT>>(row_of<DT>(t, row) + (uint64_t)at * K_ES<DT>, w);
-    Raw<DT, K_VEC<DT>> r;
-    r.q = make_uint4(w[0], w[1], w[2], w[3]);
-    return r;
-}
-
 // Between two uses of words: the numbers are made of them anew, which is cheaper than the registers that would keep them.
 BS_DEV void forget(uint4 &q) { asm("" : "+v"(q.x), "+v"(q.y), "+v"(q.z), "+v"(q.w)); }
 

@@ -21,19 +21,14 @@ struct Kept {
 };
 template <int DT>
 struct Kept<DT, true> {
-    uint32_t codes[K_VEC<DT> / 4], exponent;
-    BS_DEV void read(const LayerNormK &k, uint64_t row, uint32_t c, uint32_t at)
-    {
-        load_words<K_VEC<DT> / 4, 1>(reinterpret_cast<const char *>(k.held.codes) + row * k.C + at, codes);
-        const uint32_t blocks = (k.C + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
-        exponent = k.held.exponents[row * blocks + min(c, k.C - 1) / BS_PACK8_BLOCK];
-    }
-    BS_DEV void move(uint32_t early) { move_codes<DT>(codes, early); }
-    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { from_8_bits<DT>(codes, exponent, v); }
+    HeldVector<DT> h;
+    BS_DEV void read(const LayerNormK &k, uint64_t row, uint32_t c, uint32_t at) { h.read(k.held, row, c, k.C); }
+    BS_DEV void move(uint32_t early) { h.move(early); }
+    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { h.numbers(v); }
     BS_DEV void forget()
     {
 #pragma unroll
-        for (int i = 0; i < K_VEC<DT> / 4; ++i) asm("" : "+v"(codes[i]));
+        for (int i = 0; i < K_VEC<DT> / 4; ++i) asm("" : "+v"(h.codes[i]));
     }
 };
 

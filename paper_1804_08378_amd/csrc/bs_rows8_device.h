@@ -15,6 +15,9 @@ template <int DT>
 constexpr int K_ES = DT == DT_F32 ? 4 : 2;
 
 // ------------------------------------------------------------------------------------------------ access
+template <int DT>
+BS_DEV const char *row_of(const RowTensor &t, uint64_t row) { return static_cast<const char *>(t.p) + row * t.stride * K_ES<DT>; }
+
 // Rows may begin at any element: accesses of up to 128 bits need no more than the element's alignment.
 template <int N, int A>
 BS_DEV void load_words(const char *p, uint32_t (&w)[N])
@@ -158,6 +161,19 @@ BS_DEV Raw<DT, K_VEC<DT>> moved(const Raw<DT, K_VEC<DT>> &r, uint32_t early)
     Raw<DT, K_VEC<DT>> s;
     s.q = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
     return s;
+}
+// The same of rows of a vector at least, where every lane reads one, so that no load stands behind a condition: the compiler counts the loads in flight,
+// and waits for all of them where it cannot.  `moved` by `early_by` puts the columns to their places.
+template <int DT>
+BS_DEV uint32_t read_column(uint32_t c, uint32_t columns) { return min(c, columns - K_VEC<DT>); }
+template <int DT>
+BS_DEV Raw<DT, K_VEC<DT>> read_vector(const RowTensor &t, uint64_t row, uint32_t at)
+{
+    uint32_t w[4];
+    load_words<4, K_ES<DT>>(row_of<DT>(t, row) + (uint64_t)at * K_ES<DT>, w);
+    Raw<DT, K_VEC<DT>> r;
+    r.q = make_uint4(w[0], w[1], w[2], w[3]);
+    return r;
 }
 template <int DT>
 BS_DEV Raw<DT, K_VEC<DT>> settled(const Raw<DT, K_VEC<DT>> &r, uint32_t c, uint32_t columns)
@@ -361,21 +377,27 @@ BS_DEV void settle_codes(uint32_t (&codes)[K_VEC<DT> / 4], uint32_t c, uint32_t 
     if (columns % K_VEC<DT> != 0) move_codes<DT>(codes, early_by<K_VEC<DT>>(c, columns));
 }
 
-// A lane's vector of a row held in 8 bits; `numbers`: 0 behind the last column.
+// A lane's vector of a row held in 8 bits: `load` and `settle` as load_vector and settled, `read` and `move` as read_vector and moved.
 template <int DT>
 struct HeldVector {
     uint32_t codes[K_VEC<DT> / 4], exponent;
+    BS_DEV static uint64_t block_of(uint64_t row, uint32_t c, uint32_t columns)
+    {
+        return row * ((columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK) + min(c, columns - 1) / BS_PACK8_BLOCK;
+    }
     BS_DEV void load(const HeldRows &h, uint64_t row, uint32_t c, uint32_t columns)
     {
         load_codes<DT>(h.codes + row * columns, c, columns, codes);
-        const uint32_t blocks = (columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK;
-        exponent = c < columns ? h.exponents[row * blocks + c / BS_PACK8_BLOCK] : 0u;
+        exponent = h.exponents[block_of(row, c, columns)];
     }
-    BS_DEV void numbers(uint32_t c, uint32_t columns, float (&v)[K_VEC<DT>])
+    BS_DEV void settle(uint32_t c, uint32_t columns) { settle_codes<DT>(codes, c, columns); }
+    BS_DEV void read(const HeldRows &h, uint64_t row, uint32_t c, uint32_t columns)
     {
-        settle_codes<DT>(codes, c, columns);
-        from_8_bits<DT>(codes, exponent, v);
+        load_words<K_VEC<DT> / 4, 1>(reinterpret_cast<const char *>(h.codes) + row * columns + read_column<DT>(c, columns), codes);
+        exponent = h.exponents[block_of(row, c, columns)];
     }
+    BS_DEV void move(uint32_t early) { move_codes<DT>(codes, early); }
+    BS_DEV void numbers(float (&v)[K_VEC<DT>]) const { from_8_bits<DT>(codes, exponent, v); }
 };
 
 // The other way: all lanes of a block call it together.

@@ -26,7 +26,7 @@ inline bs_status check_rows(int64_t rows, int64_t columns, int32_t dtype, std::i
     if (dtype != BS_F32 && dtype != BS_BF16 && dtype != BS_F16) return BS_ERR_UNSUPPORTED;
     if (rows < 0 || columns < 1) return BS_ERR_SHAPE;
     // launches count lanes in 32 bits: four or eight of them a block
-    if (columns > (1ll << 30) || rows > (1ll << 29) || (double)rows * (double)((columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK) > (double)(1ll << 29)) return BS_ERR_UNSUPPORTED;
+    if (columns > (1ll << 30) || rows > (1ll << 28) || (double)rows * (double)((columns + BS_PACK8_BLOCK - 1) / BS_PACK8_BLOCK) > (double)(1ll << 28)) return BS_ERR_UNSUPPORTED;
     for (const int64_t s : strides) {
         if (s != 0 && s < columns) return BS_ERR_SHAPE;
         if (s > (1ll << 40) || (double)rows * (double)s > (double)(1ll << 50)) return BS_ERR_UNSUPPORTED;

@@ -585,7 +585,7 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             while inner and columns * shape[inner - 1] <= 1 << 30:
                 inner -= 1
                 columns *= shape[inner]
-            if t.numel() // columns * -(-columns // bs.BS_PACK8_BLOCK) > 1 << 29:
+            if t.numel() // columns * -(-columns // bs.BS_PACK8_BLOCK) > 1 << 28:
                 return t
             return pack8(t.permute(order).reshape(-1, columns)), t.dtype, order, shape
 

@@ -58,7 +58,7 @@ def test_layer_norm_refusals():
     for call in (forward, backward):
         assert call(norm_desc(rows=-1)) == SHAPE and call(norm_desc(features=0)) == SHAPE
         assert call(norm_desc(dtype=3)) == UNSUPPORTED and call(norm_desc(param_dtype=bs.BS_F16)) == UNSUPPORTED and call(norm_desc(param_dtype=7)) == UNSUPPORTED
-        assert call(norm_desc(features=(1 << 30) + 1)) == UNSUPPORTED and call(norm_desc(rows=(1 << 29) + 1, features=1)) == UNSUPPORTED
+        assert call(norm_desc(features=(1 << 30) + 1)) == UNSUPPORTED and call(norm_desc(rows=(1 << 28) + 1, features=1)) == UNSUPPORTED
         assert call(norm_desc(rows=1 << 28, features=65)) == UNSUPPORTED and call(norm_desc(rows=1 << 62, features=1 << 62)) in (SHAPE, UNSUPPORTED)
         for eps in (-1.0, float("nan"), float("inf")):
             assert call(norm_desc(eps=eps)) == PARAM
@@ -110,7 +110,7 @@ def test_activate_refusals():
     for call in (act, act_backward):
         assert call(act_desc(rows=-1)) == SHAPE and call(act_desc(columns=0)) == SHAPE
         assert call(act_desc(dtype=3)) == UNSUPPORTED and call(act_desc(activation=4)) == UNSUPPORTED and call(act_desc(activation=-1)) == UNSUPPORTED
-        assert call(act_desc(columns=(1 << 30) + 1)) == UNSUPPORTED and call(act_desc(rows=1 << 29, columns=33)) == UNSUPPORTED
+        assert call(act_desc(columns=(1 << 30) + 1)) == UNSUPPORTED and call(act_desc(rows=1 << 28, columns=33)) == UNSUPPORTED
         for name in ("x_stride", "gate_stride", "y_stride", "grad_y_stride", "grad_x_stride", "grad_gate_stride"):
             assert call(act_desc(**{name: 99})) == SHAPE and call(act_desc(**{name: 1 << 50})) == UNSUPPORTED
         assert call(act_desc(), x=0) == NULL and call(act_desc(), x=X + 2) == ALIGN and call(act_desc(), g=A + 1) == ALIGN
@@ -134,7 +134,7 @@ def test_pack8_refusals():
     unpack = lambda d, x=X, q=Q, e=E: status(bs.bs_unpack8, d, q, e, x, 0)
     for call in (pack, unpack):
         assert call(pack_desc(rows=-1)) == SHAPE and call(pack_desc(columns=0)) == SHAPE and call(pack_desc(x_stride=99)) == SHAPE
-        assert call(pack_desc(dtype=3)) == UNSUPPORTED and call(pack_desc(columns=(1 << 30) + 1)) == UNSUPPORTED and call(pack_desc(rows=1 << 29, columns=33)) == UNSUPPORTED
+        assert call(pack_desc(dtype=3)) == UNSUPPORTED and call(pack_desc(columns=(1 << 30) + 1)) == UNSUPPORTED and call(pack_desc(rows=1 << 28, columns=33)) == UNSUPPORTED
         assert call(pack_desc(), x=0) == NULL and call(pack_desc(), q=0) == NULL and call(pack_desc(), e=0) == NULL
         assert call(pack_desc(), x=X + 2) == ALIGN and call(pack_desc(), q=X + 2399) == ALIAS and call(pack_desc(), e=X) == ALIAS
     assert pack(pack_desc(), e=Q + 599) == ALIAS
