@@ -159,6 +159,19 @@ def test_many_rows():
     check(x, w, b, None, dy, None, False)
 
 
+# rows for every number of lanes that one is spread over, several for each work-group, and lengths that leave some of the lanes without columns
+MANY = [(70001, 23), (40001, 64), (33333, 40), (20001, 100), (9001, 200), (9001, 256), (4501, 391), (5001, 1000), (2601, 2048), (1401, 4001), (701, 8200), (601, 16384), (517, 12345),
+        (601, 20000), (301, 32768), (291, 40002)]
+
+
+@pytest.mark.parametrize("checkpoint", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", MANY)
+def test_sums_over_many_rows(shape, dtype, checkpoint):
+    x, w, b, a, dy, dt = operands(shape, dtype, 16)
+    check(x, w, b, a if checkpoint else None, dy, dt if checkpoint else None, checkpoint)
+
+
 def test_large_tensors():
     """Rows behind the first 2^32 bytes and 2^31 elements."""
     n = 8192
