@@ -168,7 +168,7 @@ constexpr int JT = 1024;
 template <int DT, int JC>
 __global__ __launch_bounds__(JT) void layer_norm_grad_join_kernel(LayerNormK k)
 {
-    __shared__ float db[JT], dw[JT];
+    __shared__ float sums[2][JT / 64][JC];
     const uint32_t c = blockIdx.x * JC + threadIdx.x % JC;
     float s0 = 0.0f, s1 = 0.0f;
     if (c < k.C) {
@@ -179,16 +179,21 @@ __global__ __launch_bounds__(JT) void layer_norm_grad_join_kernel(LayerNormK k)
             s1 += in.y;
         }
     }
-    db[threadIdx.x] = s0;
-    dw[threadIdx.x] = s1;
-    for (uint32_t half = JT / 2; half >= JC; half /= 2) {
-        __syncthreads();
-        if (threadIdx.x < half) {
-            db[threadIdx.x] += db[threadIdx.x + half];
-            dw[threadIdx.x] += dw[threadIdx.x + half];
-        }
+    s0 = teams_sum<JC>(s0);
+    s1 = teams_sum<JC>(s1);
+    if (threadIdx.x % 64 < JC) {
+        sums[0][threadIdx.x / 64][threadIdx.x % JC] = s0;
+        sums[1][threadIdx.x / 64][threadIdx.x % JC] = s1;
     }
-    if (threadIdx.x < JC && c < k.C) put_params<DT>(k, c, db[threadIdx.x], dw[threadIdx.x]);
+    __syncthreads();
+    if (threadIdx.x >= JC || c >= k.C) return;
+    float b = 0.0f, w = 0.0f;
+#pragma unroll
+    for (int i = 0; i < JT / 64; ++i) {
+        b += sums[0][i][threadIdx.x];
+        w += sums[1][i][threadIdx.x];
+    }
+    put_params<DT>(k, c, b, w);
 }
 
 // ------------------------------------------------------------------------------------------------ launches

@@ -2,7 +2,8 @@
 //
 // A lane keeps the sums of dy and dy * xh of its columns over all rows of its team, in registers or, of long rows, in LDS (of rows over 16384 columns nowhere: bs_layer_norm.hip sums them); a work-group's teams are
 // added through LDS at the end, and the work-groups' sums are joined by a second launch, in orders that depend on sizes only: equal calls give equal
-// bits.  A work-group is as large as a compute unit takes, and there is one for each: the fewer there are, the fewer sums cross memory.
+// bits.  A work-group is as large as a compute unit takes, and there is one for each: the fewer there are, the fewer sums cross memory (256 parts of 4096
+// columns are 8.4 MB beside the 201 MB of 8192 rows).  The join is a launch of 2.5 to 7 us.
 #include <hip/hip_runtime.h>
 
 #include "bs_layer_norm_team.h"
