@@ -7,8 +7,8 @@ namespace bs {
 
 constexpr uint32_t K_LAYER_NORM_ROW_GROUPS = 512;  // work-groups that walk over long rows, at most: two of each compute unit
 
-constexpr int K_LAYER_NORM_GRAD_THREADS = 1024;           // of a work-group of the backward pass with the rows in registers
-constexpr uint32_t K_LAYER_NORM_GRAD_GROUPS = 256;        // of them at most: one of each compute unit
+constexpr int K_LAYER_NORM_GRAD_THREADS = 1024;  // of a work-group of the backward pass with the rows in registers
+constexpr uint64_t K_LAYER_NORM_GROUPS = 256;     // of work-groups of that size at most: one of each compute unit
 
 struct LayerNormK {
     RowTensor x, addend, y, total;  // backward: x is t; addend, total: p may be nullptr
