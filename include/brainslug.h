@@ -659,8 +659,9 @@ typedef struct bs_activate_desc {
  *   x_codes, x_exponents        device, written: x in 8 bits; both NULL: not wanted
  *   gate_codes, gate_exponents  the same of gate
  * No output shares a byte with an input or another output.
- * Errors: BS_ERR_NULL (x, y; codes without exponents or the other way round; a gate's without a gate), BS_ERR_SHAPE, BS_ERR_UNSUPPORTED (type,
- *         activation; sizes as bs_pack8), BS_ERR_ALIGN, BS_ERR_ALIAS, BS_ERR_HIP.
+ * Errors: BS_ERR_NULL (x, y; codes without exponents or the other way round; a gate's without a gate;
+ *         with a gate, one operand's codes without the other's), BS_ERR_SHAPE, BS_ERR_UNSUPPORTED (type, activation;
+ *         sizes as bs_pack8), BS_ERR_ALIGN, BS_ERR_ALIAS, BS_ERR_HIP.
  */
 BS_API bs_status bs_activate(const bs_activate_desc *desc, const void *x, const void *gate, void *y, int8_t *x_codes, uint8_t *x_exponents,
                              int8_t *gate_codes, uint8_t *gate_exponents, void *stream);

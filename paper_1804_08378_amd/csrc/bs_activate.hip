@@ -4,8 +4,8 @@
 //
 // A lane keeps 128 bits of every tensor; four (float32: eight) neighbouring lanes hold a block and find its largest magnitude by exchanges inside
 // the wave.  A work-group takes neighbouring vectors across row ends, so that short rows leave no lanes without work but those behind a row's end.
-// Memory bounds it: 8192 x 8192 bfloat16 with a gate, both operands to 8 bits, 82 us forward (6.6 TB/s) and 97 backward (5.6); 200704 x 256 to 8 bits 30 us
-// and back 24 (5.2, 6.4).  Both directions of the former, before the loads of a lane stood side by side: two vectors a lane 195 us, four 205, one 184; with
+// Memory bounds it: 8192 x 8192 bfloat16 with a gate, both operands to 8 bits, 82 us forward (6.6 TB/s) and 100 backward (5.4); 200704 x 256 to 8 bits 29 us
+// and back 25 (5.4, 6.3).  Both directions of the former, before the loads of a lane stood side by side: two vectors a lane 195 us, four 205, one 184; with
 // the codes' stores through the caches, where their next reader finds some of them, 182, with the tensors' too 192.
 #include <hip/hip_runtime.h>
 

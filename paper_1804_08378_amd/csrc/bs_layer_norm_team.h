@@ -2,8 +2,8 @@
 //
 // A team of TEAM lanes (a part of a wave, a wave, or several waves) holds a row, a vector of 128 bits a lane up to 1024 lanes, NV of them in longer rows, so
 // that every tensor crosses memory once, and has the next row's vectors under way while it works on this one.  Weight and bias of a lane's columns stay
-// in its registers from row to row.  Memory bounds it: 8192 x 4096 bfloat16 behind an addition 49 us (5.5 TB/s; a copy of that size 5.4), 200704 x 256
-// forward 42 and backward 50 us (4.9, 6.1), 16384 x 2048 through 8 bits 52 and 46 (5.8, 5.1), 8192 x 1024 float32 12 and 17.5 (5.6, 5.7).  What made it so,
+// in its registers from row to row.  Memory bounds it: 8192 x 4096 bfloat16 behind an addition 43 us (6.3 TB/s; a copy 6.6), 200704 x 256
+// forward 37 and backward 52 us (5.5, 6.0), 16384 x 2048 through 8 bits 51 and 48 (5.9, 4.9), 8192 x 1024 float32 12 and 17.4 (5.6, 5.8).  What made it so,
 // same cases: no load behind a condition (backward 57 -> 46, 20 -> 17.5); a row's last vector as one whole load that ends with the row (20000 x 771
 // binary16 forward 50 -> 31); numbers made of their words anew for every use (64 registers forward, 8 waves a SIMD).  More vectors a lane for
 // fewer lanes (64 x 4, 256 x 2) took 160 to 256 registers, and neighbouring rows for a work-group instead of strided ones cost 200704 x 256 forward 7 us.
