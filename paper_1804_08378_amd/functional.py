@@ -557,7 +557,8 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     Held so are tensors on the GPU of `pack8`'s types and sizes with at least `least` elements and two dimensions, more than two of them in the last
     (statistics of rows have no more), dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers of
-    `model` (a module, or an iterable of tensors), which are in use anyway.  A tensor that several nodes keep is held once for each.  Under autocast,
+    `model` (a module, or an iterable of tensors), which are in use anyway; changed in place before the backward pass, they are refused there, as
+    without the block.  A tensor that several nodes keep is held once for each.  Under autocast,
     whose copies of the weights could not be told from activations, and where an autocast begins inside the block, it refuses.
 
     What is exact in 16 bits is not so in 8: an element is off by 0.8 % of the largest of 32 neighbours in memory at most.  A ReLU's gradient then takes
@@ -569,16 +570,15 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         least = _integer(least, "checkpoints_in_8_bits: least", 64)
         memory = {t.untyped_storage().data_ptr() for t in tensors}
 
-        def pack(t):
-            if _autocasts() > self._autocasts:  # (inside an operation autocast itself reads as switched off)
-                raise RuntimeError("checkpoints_in_8_bits: no autocast inside the block")
+        def held(t):
+            """What stands for `t` in 8 bits; None: it stays as it is."""
             # (`tensors` are alive as long as this is: no other memory has their addresses)
             if not t.is_cuda or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or type(t) not in (torch.Tensor, nn.Parameter) or \
                     t.untyped_storage().data_ptr() in memory or torch.jit.is_tracing():
-                return t
+                return None
             order = _dense_order(t)
             if order is None:
-                return t
+                return None
             t = t.detach()
             shape = [t.shape[i] for i in order]
             columns, inner = 1, len(shape)  # rows of as many dimensions as a call takes
@@ -586,12 +586,21 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
                 inner -= 1
                 columns *= shape[inner]
             if t.numel() // columns * -(-columns // bs.BS_PACK8_BLOCK) > 1 << 28:
-                return t
+                return None
             return pack8(t.permute(order).reshape(-1, columns)), t.dtype, order, shape
 
+        def pack(t):
+            if _autocasts() > self._autocasts:  # (inside an operation autocast itself reads as switched off)
+                raise RuntimeError("checkpoints_in_8_bits: no autocast inside the block")
+            return held(t) or (t, t._version)  # (where hooks are set, torch itself compares no versions)
+
         def unpack(kept):
-            if isinstance(kept, torch.Tensor):
-                return kept
+            if len(kept) == 2:
+                t, version = kept
+                if t._version != version:
+                    raise RuntimeError("one of the variables needed for gradient computation has been modified by an inplace operation: a tensor that "
+                                       f"checkpoints_in_8_bits kept as it is, {tuple(t.shape)}, is at version {t._version}; expected version {version} instead")
+                return t
             packed, dtype, order, shape = kept
             back = sorted(range(len(order)), key=order.__getitem__)
             return unpack8(packed, dtype).view(shape).permute(back)

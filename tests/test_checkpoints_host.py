@@ -1,0 +1,53 @@
+"""What `checkpoints_in_8_bits` does with tensors that stay as they are, without a GPU: tensors in host memory all do."""
+import pytest
+import torch
+from torch import nn
+
+from paper_1804_08378_amd import functional as F
+
+
+def parameter_changed(w, x):
+    y = (x * w).exp() * x
+    with torch.no_grad():
+        w.mul_(10.0)  # an optimiser's step
+    return y
+
+
+def result_changed(w, x):
+    y = (x * w).sigmoid()
+    y.mul_(5.0)
+    return y
+
+
+def view_changed(w, x):
+    u = x * 1.0
+    y = u[:, ::2].sin() * w
+    u[:, 1::2].add_(1.0)  # another part of the same memory: autograd counts a tensor's versions together with its views'
+    return y
+
+
+@pytest.mark.parametrize("call", [parameter_changed, result_changed, view_changed])
+def test_in_place_changes_are_seen_in_the_block(call):
+    """With and without the block, a tensor that autograd keeps and that is changed before the backward pass is refused."""
+    for block in (lambda w: torch.enable_grad(), lambda w: F.checkpoints_in_8_bits([w])):
+        w, x = torch.ones((), requires_grad=True), torch.randn(3, 4, requires_grad=True)
+        with block(w):
+            y = call(w, x)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+
+
+def test_changes_before_a_tensor_is_kept_or_of_others_are_allowed():
+    w, x = nn.Parameter(torch.full((4,), 2.0)), torch.randn(3, 4, requires_grad=True)
+    with F.checkpoints_in_8_bits([w]):
+        with torch.no_grad():
+            w.mul_(2.0)
+        u = x * w
+        u.mul_(3.0)            # neither product keeps its result
+        y = u.clone().relu_()  # keeps its result as it is behind the change
+        z = y.sin()
+        other = y.detach().clone().add_(1.0)
+    gx, gw = torch.autograd.grad(z.sum(), [x, w], retain_graph=True)
+    on = (u.detach() > 0).float() * u.detach().clamp(min=0).cos() * 3.0
+    assert torch.equal(other, y.detach() + 1) and torch.allclose(gx, on * 4.0, atol=0, rtol=1e-6) and torch.allclose(gw, (on * x.detach()).sum(0), rtol=1e-5)
+    assert all(torch.equal(a, b) for a, b in zip((gx, gw), torch.autograd.grad(z.sum(), [x, w])))  # (a second pass)
