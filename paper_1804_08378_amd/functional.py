@@ -592,7 +592,9 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         def pack(t):
             if _autocasts() > self._autocasts:  # (inside an operation autocast itself reads as switched off)
                 raise RuntimeError("checkpoints_in_8_bits: no autocast inside the block")
-            return held(t) or (t, t._version)  # (where hooks are set, torch itself compares no versions)
+            # (Another tensor of the same memory and versions: the very result of a node that keeps it would keep that node alive, which no collector sees.
+            # Versions: where hooks are set, torch itself compares none.)
+            return held(t) or (t.detach(), t._version)
 
         def unpack(kept):
             if len(kept) == 2:

@@ -1,4 +1,7 @@
 """What `checkpoints_in_8_bits` does with tensors that stay as they are, without a GPU: tensors in host memory all do."""
+import gc
+import weakref
+
 import pytest
 import torch
 from torch import nn
@@ -51,3 +54,45 @@ def test_changes_before_a_tensor_is_kept_or_of_others_are_allowed():
     on = (u.detach() > 0).float() * u.detach().clamp(min=0).cos() * 3.0
     assert torch.equal(other, y.detach() + 1) and torch.allclose(gx, on * 4.0, atol=0, rtol=1e-6) and torch.allclose(gw, (on * x.detach()).sum(0), rtol=1e-5)
     assert all(torch.equal(a, b) for a, b in zip((gx, gw), torch.autograd.grad(z.sum(), [x, w])))  # (a second pass)
+
+
+class Marked(torch.autograd.Function):
+    """x, by a node that holds an object which can be watched."""
+
+    @staticmethod
+    def forward(ctx, x, mark):
+        ctx.mark = mark
+        return x.view_as(x)
+
+    @staticmethod
+    def backward(ctx, g):
+        return g, None
+
+
+class Mark:
+    pass
+
+
+@pytest.mark.parametrize("keeps_its_result", [torch.exp, torch.sigmoid, torch.relu, torch.tanh, lambda t: t.softmax(-1), lambda t: t.clone().exp_()])
+def test_graphs_without_a_backward_pass_are_freed(keeps_its_result):
+    """An operation that keeps its own result: were that very tensor kept, node and tensor would hold each other."""
+    for block in (torch.enable_grad, lambda: F.checkpoints_in_8_bits([])):
+        x, mark = torch.randn(3, 4, requires_grad=True), Mark()
+        alive = weakref.ref(mark)
+        with block():
+            y = keeps_its_result(Marked.apply(x, mark)) * 2.0
+        del mark
+        assert alive() is not None
+        del y
+        gc.collect()
+        assert alive() is None
+
+
+def test_a_result_that_its_node_keeps_and_that_a_program_holds():
+    """The kept tensor is another one with the same memory: changes are still seen, gradients of gradients go through it."""
+    x = torch.randn(5, dtype=torch.float64, requires_grad=True)
+    with F.checkpoints_in_8_bits([]):
+        y = x.exp()
+        (g,) = torch.autograd.grad(y.sum(), x, create_graph=True)
+        (h,) = torch.autograd.grad(g.sum(), x)
+    assert torch.equal(h, x.detach().exp()) and torch.equal(g, y)
