@@ -10,6 +10,7 @@ torch's functions overrides these too: `torch.fx` records a call of one of them 
 """
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import operator
 from typing import NamedTuple, Optional, Tuple
@@ -550,20 +551,53 @@ def _autocasts() -> int:
     return n
 
 
+class _Statistics:
+    """Which of the tensors that autograd keeps are statistics: factors of a gradient's formula that have to fit its other operands, where a value next to
+    them makes another formula of it.  As far as they can be told:
+    - tensors without a gradient (attention's log sums, layer normalisation's statistics; masks and constants too),
+    - the second, third ... result of one of torch's own operations that is no view of its operand (group normalisation's mean and deviation),
+    - tensors whose sizes are another one's with dimensions taken out, one of the last that were kept (log sums and norms along a dimension).
+    What is taken for one and is none (the second of two stacked operands) only stays as precise as it was."""
+
+    def __init__(self):
+        self._sizes = collections.deque(maxlen=16)  # of the last tensors, without ones
+
+    def found(self, t: torch.Tensor) -> bool:
+        sizes = tuple(n for n in t.shape if n != 1)
+        of_another = any(len(sizes) < len(other) and _left_of(sizes, other) for other in self._sizes)
+        if t.is_floating_point():
+            self._sizes.append(sizes)
+        if not t.requires_grad or of_another:
+            return True
+        return t.output_nr > 0 and not t._is_view() and not isinstance(t.grad_fn, torch.autograd.function.BackwardCFunction)
+
+
+def _left_of(sizes: Tuple[int, ...], other: Tuple[int, ...]) -> bool:
+    """Are `sizes` what is left of `other` when some are taken out?"""
+    rest = iter(other)
+    return all(n in rest for n in sizes)
+
+
 class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """`with checkpoints_in_8_bits(model): y = model(x)`: what autograd keeps for the backward pass in the block -- convolutions' and linear layers'
     inputs, the operands of stacks and of the functions here -- is held by `pack8` and brought back when the backward pass asks for it, so that the
     gradients are those at the values in 8 bits.
 
-    Held so are tensors on the GPU of `pack8`'s types and sizes with at least `least` elements and two dimensions, more than two of them in the last
-    (statistics of rows have no more), dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers of
+    Held so are tensors on the GPU of `pack8`'s types and sizes that have a gradient, with at least `least` elements and two dimensions, more than two
+    of them in the last, dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers of
     `model` (a module, or an iterable of tensors), which are in use anyway; changed in place before the backward pass, they are refused there, as
     without the block.  A tensor that several nodes keep is held once for each.  Under autocast,
     whose copies of the weights could not be told from activations, and where an autocast begins inside the block, it refuses.
 
     What is exact in 16 bits is not so in 8: an element is off by 0.8 % of the largest of 32 neighbours in memory at most.  A ReLU's gradient then takes
     the other side for elements that close to 0, the largest of a pooling window is another one where two are that close; logits lose it from their
-    probabilities (keep the loss outside of the block), and numbers next to masks of the type's lowest value all they are."""
+    probabilities (keep the loss outside of the block), and numbers next to masks of the type's lowest value all they are.
+
+    Statistics stay as they are as far as they can be told: what has no gradient (attention's log sums, constants, masks), the further results of torch's
+    operations (a group normalisation's mean and deviation), and tensors whose sizes are those of one of the last sixteen with dimensions taken out (log
+    sums and norms along a dimension).  A statistic that a program computes by itself, with a gradient and in sizes of its own, is held as any operand, and
+    so are weights computed from parameters (casts, parametrisations).  Attention takes the exponential of its operands' products: the larger the scores, the
+    coarser its gradients at operands in 8 bits."""
 
     def __init__(self, model, least: int = 1 << 14):
         tensors = [*model.parameters(), *model.buffers()] if isinstance(model, nn.Module) else list(model)
@@ -573,8 +607,10 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         def held(t):
             """What stands for `t` in 8 bits; None: it stays as it is."""
             # (`tensors` are alive as long as this is: no other memory has their addresses)
-            if not t.is_cuda or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or type(t) not in (torch.Tensor, nn.Parameter) or \
-                    t.untyped_storage().data_ptr() in memory or torch.jit.is_tracing():
+            if not t.is_cuda or torch.jit.is_tracing() or t.untyped_storage().data_ptr() in memory:
+                return None
+            if self._statistics.found(t) or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or \
+                    type(t) not in (torch.Tensor, nn.Parameter):
                 return None
             order = _dense_order(t)
             if order is None:
@@ -607,13 +643,13 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             back = sorted(range(len(order)), key=order.__getitem__)
             return unpack8(packed, dtype).view(shape).permute(back)
 
-        self._alive, self._autocasts = tensors, 0
+        self._alive, self._autocasts, self._statistics = tensors, 0, _Statistics()
         super().__init__(pack, unpack)
 
     def __enter__(self):
         if torch.is_autocast_enabled("cuda"):
             raise RuntimeError("checkpoints_in_8_bits: not under autocast")
-        self._autocasts = _autocasts()
+        self._autocasts, self._statistics = _autocasts(), _Statistics()
         return super().__enter__()
 
 

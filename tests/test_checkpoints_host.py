@@ -96,3 +96,65 @@ def test_a_result_that_its_node_keeps_and_that_a_program_holds():
         (g,) = torch.autograd.grad(y.sum(), x, create_graph=True)
         (h,) = torch.autograd.grad(g.sum(), x)
     assert torch.equal(h, x.detach().exp()) and torch.equal(g, y)
+
+
+# ------------------------------------------------------------------------------------------------ statistics
+def told(call, *operands):
+    """Sizes of what `call` keeps, and which of them are taken for statistics."""
+    statistics, seen = F._Statistics(), []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: seen.append((tuple(t.shape), statistics.found(t))) or t.detach(), lambda t: t):
+        call(*operands)
+    return [s for s, found in seen if found], [s for s, found in seen if not found]
+
+
+def operand(*sizes):
+    return torch.randn(*sizes, requires_grad=True) * 1.0
+
+
+@pytest.mark.parametrize("call,statistic", [
+    (lambda x: nn.functional.scaled_dot_product_attention(x, x * 2, x * 3), (4, 8, 16)),
+    (lambda x: nn.functional.group_norm(x, 4), (4, 4)),
+    (lambda x: x.logsumexp(-1), (4, 8, 16)),
+    (lambda x: x.logsumexp(1), (4, 16, 32)),
+    (lambda x: x.logsumexp(1, keepdim=True), (4, 1, 16, 32)),
+    (lambda x: x.norm(dim=1), (4, 16, 32)),
+    (lambda x: x.std(dim=2), (4, 8, 32)),
+    (lambda x: nn.functional.layer_norm(x, (32,)), (4, 8, 16, 1)),
+    (lambda x: nn.functional.normalize(x, dim=1), (4, 1, 16, 32)),
+    (lambda x: nn.functional.dropout(x), (4, 8, 16, 32)),  # (a mask)
+])
+def test_statistics_are_told(call, statistic):
+    found, others = told(call, operand(4, 8, 16, 32))
+    assert statistic in found and statistic not in [s for s in others if s != (4, 8, 16, 32)]
+    assert all(s == (4, 8, 16, 32) for s in others)
+
+
+def test_operands_are_no_statistics():
+    x = operand(4, 8, 16, 32)
+    for call in (torch.exp, torch.sin, lambda t: t * t, lambda t: t.relu().view(32, 16, 32).sin().permute(1, 0, 2).exp(), lambda t: [u.sin() for u in t.chunk(2, 1)],
+                 lambda t: [u.sin() for u in t.unbind(0)][:0], lambda t: t.softmax(-1), lambda t: nn.functional.avg_pool2d(t.relu(), 2).exp(),
+                 lambda t: nn.functional.max_pool2d(t, 2)):
+        found, others = told(call, x)
+        assert others and found in ([], [(4, 8, 8, 16)]), (found, others)  # (a maximum's picks are whole numbers without a gradient)
+
+    class Two(torch.autograd.Function):  # as a layer normalisation and its total
+        @staticmethod
+        def forward(ctx, t):
+            a, b = t + 1, t + 2
+            ctx.save_for_backward(t, b)
+            return a, b
+
+    assert told(Two.apply, x) == ([], [(4, 8, 16, 32)] * 2)
+
+
+def test_sizes_are_forgotten():
+    """A tensor of a step's sizes is an operand again once others have been kept: a loop over the steps of a sequence."""
+    x, h = operand(50, 64, 96), operand(64, 96)
+
+    def loop(x, h):
+        x.sin()
+        for _ in range(50):
+            h = h.sin()
+
+    found, others = told(loop, x, h)
+    assert found == [(64, 96)] * 16 and len(others) == 35
