@@ -562,6 +562,9 @@ class _Statistics:
     def __init__(self):
         self._sizes = collections.deque(maxlen=16)  # of the last tensors, without ones
 
+    def begin(self) -> None:
+        self._sizes.clear()
+
     def found(self, t: torch.Tensor) -> bool:
         sizes = tuple(n for n in t.shape if n != 1)
         of_another = any(len(sizes) < len(other) and _left_of(sizes, other) for other in self._sizes)
@@ -584,10 +587,10 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     gradients are those at the values in 8 bits.
 
     Held so are tensors on the GPU of `pack8`'s types and sizes that have a gradient, with at least `least` elements and two dimensions, more than two
-    of them in the last, dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers of
-    `model` (a module, or an iterable of tensors), which are in use anyway; changed in place before the backward pass, they are refused there, as
-    without the block.  A tensor that several nodes keep is held once for each.  Under autocast,
-    whose copies of the weights could not be told from activations, and where an autocast begins inside the block, it refuses.
+    of them in the last, dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers that
+    `model` (a module, or an iterable of tensors) has where the block begins, and any `nn.Parameter`, which are in use anyway; changed in place before the
+    backward pass, they are refused there, as without the block.  A tensor that several nodes keep is held once for each.  Under autocast, whose copies of the
+    weights could not be told from activations, and where an autocast begins inside the block, it refuses.
 
     What is exact in 16 bits is not so in 8: an element is off by 0.8 % of the largest of 32 neighbours in memory at most.  A ReLU's gradient then takes
     the other side for elements that close to 0, the largest of a pooling window is another one where two are that close; logits lose it from their
@@ -600,16 +603,19 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     coarser its gradients at operands in 8 bits."""
 
     def __init__(self, model, least: int = 1 << 14):
-        tensors = [*model.parameters(), *model.buffers()] if isinstance(model, nn.Module) else list(model)
+        self._model = model if isinstance(model, nn.Module) else list(model)
+        # what the hooks read: not self, as graphs hold the hooks and a model may hold its graph
+        self._autocasts, self._memory, self._statistics = [0], set(), _Statistics()  # _memory: where the model's tensors are
+        autocasts, memory, statistics = self._autocasts, self._memory, self._statistics
         least = _integer(least, "checkpoints_in_8_bits: least", 64)
-        memory = {t.untyped_storage().data_ptr() for t in tensors}
 
         def held(t):
             """What stands for `t` in 8 bits; None: it stays as it is."""
-            # (`tensors` are alive as long as this is: no other memory has their addresses)
             if not t.is_cuda or torch.jit.is_tracing() or t.untyped_storage().data_ptr() in memory:
                 return None
-            if self._statistics.found(t) or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or \
+            if isinstance(t, nn.Parameter) or isinstance(t._base, nn.Parameter):  # (made or moved inside the block)
+                return None
+            if statistics.found(t) or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or \
                     type(t) not in (torch.Tensor, nn.Parameter):
                 return None
             order = _dense_order(t)
@@ -626,7 +632,7 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             return pack8(t.permute(order).reshape(-1, columns)), t.dtype, order, shape
 
         def pack(t):
-            if _autocasts() > self._autocasts:  # (inside an operation autocast itself reads as switched off)
+            if _autocasts() > autocasts[0]:  # (inside an operation autocast itself reads as switched off)
                 raise RuntimeError("checkpoints_in_8_bits: no autocast inside the block")
             # (Another tensor of the same memory and versions: the very result of a node that keeps it would keep that node alive, which no collector sees.
             # Versions: where hooks are set, torch itself compares none.)
@@ -643,13 +649,16 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             back = sorted(range(len(order)), key=order.__getitem__)
             return unpack8(packed, dtype).view(shape).permute(back)
 
-        self._alive, self._autocasts, self._statistics = tensors, 0, _Statistics()
         super().__init__(pack, unpack)
 
     def __enter__(self):
         if torch.is_autocast_enabled("cuda"):
             raise RuntimeError("checkpoints_in_8_bits: not under autocast")
-        self._autocasts, self._statistics = _autocasts(), _Statistics()
+        self._autocasts[0] = _autocasts()
+        self._statistics.begin()
+        tensors = (*self._model.parameters(), *self._model.buffers()) if isinstance(self._model, nn.Module) else self._model
+        self._memory.clear()  # (a model that was moved or cast since has other memory)
+        self._memory.update(t.untyped_storage().data_ptr() for t in tensors if not nn.parameter.is_lazy(t))
         return super().__enter__()
 
 

@@ -88,6 +88,17 @@ def test_graphs_without_a_backward_pass_are_freed(keeps_its_result):
         assert alive() is None
 
 
+def test_a_model_that_holds_its_result_is_freed():
+    """Graphs hold the block's hooks: these hold no model."""
+    model, mark = nn.Linear(4, 4), Mark()
+    model.mark, alive = mark, weakref.ref(mark)
+    with F.checkpoints_in_8_bits(model):
+        model.last = model(torch.randn(3, 4, requires_grad=True)).exp()
+    del model, mark
+    gc.collect()
+    assert alive() is None
+
+
 def test_a_result_that_its_node_keeps_and_that_a_program_holds():
     """The kept tensor is another one with the same memory: changes are still seen, gradients of gradients go through it."""
     x = torch.randn(5, dtype=torch.float64, requires_grad=True)

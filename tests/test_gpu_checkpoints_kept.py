@@ -88,3 +88,32 @@ def test_the_operators_here_keep_their_operands_so(held):
         v = n(m)
     assert held == [x.numel()] * 3 + [m.numel()]
     assert all(g.isfinite().all() for g in torch.autograd.grad(z.sum() + v.sum(), (x, a, m)))
+
+
+# ------------------------------------------------------------------------------------------------ parameters
+def test_a_model_that_moves_behind_the_blocks_making(held):
+    """Its parameters and buffers are those that it has where the block begins."""
+    m = nn.Linear(128, 96)
+    m.register_buffer("table", torch.randn(128, 128, requires_grad=True))
+    block = F.checkpoints_in_8_bits(m, least=64)
+    m.cuda()
+    x = torch.randn(64, 128, device="cuda", requires_grad=True)
+    for _ in range(2):
+        with block:
+            y = m(x @ m.table)
+        (gx,) = torch.autograd.grad(y.sum(), x)
+        want = (m.weight.sum(0) @ m.table.t()).detach().expand_as(gx)
+        assert float((gx - want).norm()) <= 1e-5 * float(want.norm())  # (sums of 224 terms; weights in 8 bits miss it by some 0.3 %)
+        assert sorted(held) == [x.numel()] * 2  # the operands of both products
+        held.clear()
+        m.double().float()  # (a round trip: new memory)
+
+
+def test_parameters_made_inside_the_block(held):
+    m = nn.Sequential(nn.LazyLinear(96), nn.ReLU(), nn.Linear(96, 64)).cuda()
+    x = torch.randn(64, 128, device="cuda", requires_grad=True)
+    with F.checkpoints_in_8_bits(m, least=64):
+        y = m(x)
+    assert sorted(held) == [64 * 96, 64 * 96, 64 * 128]  # operands of the products and the ReLU's result
+    (gx,) = torch.autograd.grad(y.sum(), x)
+    assert gx.isfinite().all()
