@@ -611,7 +611,7 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
         def held(t):
             """What stands for `t` in 8 bits; None: it stays as it is."""
-            if not t.is_cuda or torch.jit.is_tracing() or t.untyped_storage().data_ptr() in memory:
+            if not t.is_cuda or t.layout != torch.strided or torch.jit.is_tracing() or t.untyped_storage().data_ptr() in memory:
                 return None
             if isinstance(t, nn.Parameter) or isinstance(t._base, nn.Parameter):  # (made or moved inside the block)
                 return None
@@ -658,7 +658,7 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         self._statistics.begin()
         tensors = (*self._model.parameters(), *self._model.buffers()) if isinstance(self._model, nn.Module) else self._model
         self._memory.clear()  # (a model that was moved or cast since has other memory)
-        self._memory.update(t.untyped_storage().data_ptr() for t in tensors if not nn.parameter.is_lazy(t))
+        self._memory.update(t.untyped_storage().data_ptr() for t in tensors if not nn.parameter.is_lazy(t) and t.layout == torch.strided)
         return super().__enter__()
 
 

@@ -169,3 +169,12 @@ def test_sizes_are_forgotten():
 
     found, others = told(loop, x, h)
     assert found == [(64, 96)] * 16 and len(others) == 35
+
+
+def test_a_model_with_sparse_buffers():
+    m = nn.Linear(4, 4)
+    m.register_buffer("graph", torch.eye(4).to_sparse())
+    x = torch.randn(4, 4, requires_grad=True)
+    with F.checkpoints_in_8_bits(m):
+        y = torch.sparse.mm(m.graph, m(x))
+    assert torch.allclose(torch.autograd.grad(y.sum(), x)[0], m.weight.detach().sum(0).expand(4, 4), atol=1e-6)

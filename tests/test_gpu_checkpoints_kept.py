@@ -117,3 +117,10 @@ def test_parameters_made_inside_the_block(held):
     assert sorted(held) == [64 * 96, 64 * 96, 64 * 128]  # operands of the products and the ReLU's result
     (gx,) = torch.autograd.grad(y.sum(), x)
     assert gx.isfinite().all()
+
+
+def test_sparse_tensors_stay_as_they_are(held):
+    t = torch.sparse_coo_tensor(torch.arange(64, device="cuda").repeat(2, 1), torch.randn(64, device="cuda"), (4096, 4096)).requires_grad_(True)
+    block = F.checkpoints_in_8_bits([], least=64)
+    kept = block.pack_hook(t)
+    assert not held and torch.equal(block.unpack_hook(kept)._values(), t.detach()._values())
