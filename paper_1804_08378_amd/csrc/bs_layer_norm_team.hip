@@ -115,7 +115,7 @@ __global__ __launch_bounds__(K_THREADS<TEAM>) void layer_norm_team_kernel(LayerN
         for (int j = 0; j < NV; ++j) {
             const uint32_t c = (j * TEAM + lane) * VEC;
             forget(t[j].q);
-            if (ADD && k.total.p) store_vector<DT>(const_cast<char *>(row_of<DT>(k.total, row)), c, k.C, t[j]);
+            if (k.total.p) store_vector<DT>(const_cast<char *>(row_of<DT>(k.total, row)), c, k.C, t[j]);
             float v[VEC], wj[VEC], bj[VEC];
             unpack<DT, VEC>(t[j], v);
             if (k.held.codes) store_held<DT>(k.held, row, c, k.C, t[j], v);

@@ -264,3 +264,19 @@ def test_module():
         m(x[..., :99].cuda())
     assert F.LayerNorm(8, elementwise_affine=False).cuda()(x[..., :8].cuda()).shape == (3, 4, 8) and F.LayerNorm(8, bias=False).bias is None
     assert "checkpoint=True" in repr(m)
+
+
+@pytest.mark.parametrize("dtype", list(ref.DTYPES))
+@pytest.mark.parametrize("n", [5, 8, 100, 515, 4096, 16389, 40001])
+def test_the_total_of_no_addend(n, dtype):
+    """The C entry writes t where it is wanted, with an addend or without: then it is x.  Rows shorter than a vector, in registers, over memory."""
+    x = torch.randn(3, n, dtype=ref.DTYPES[dtype], device="cuda")
+    buffers = torch.full((2, 3, n + 16), 7.0, dtype=x.dtype, device="cuda")
+    y, total = buffers[0, :, 8:8 + n], buffers[1, :, 8:8 + n]
+    d = bs.bs_layer_norm_desc()
+    d.rows, d.features, d.eps, d.dtype, d.param_dtype = 3, n, 1e-5, {"f32": bs.BS_F32, "bf16": bs.BS_BF16, "f16": bs.BS_F16}[dtype], bs.BS_F32
+    d.y_stride = d.total_stride = n + 16
+    bs.bs_layer_norm(d, x.data_ptr(), 0, 0, 0, y.data_ptr(), total.data_ptr(), 0, 0, 0, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(total, x) and torch.equal(y, F.layer_norm(x))
+    assert (buffers[:, :, :8] == 7).all() and (buffers[:, :, 8 + n:] == 7).all()
