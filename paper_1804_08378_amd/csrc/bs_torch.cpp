@@ -549,7 +549,8 @@ bool optional_tensor(PyObject *o, at::Tensor &t)
     t = *p;
     return t.defined() && !dual(t);
 }
-bool on_gpu(const at::Tensor &t, const at::Device &dev) { return t.is_cuda() && t.has_storage() && t.device() == dev; }
+// (Not a view whose sign is turned when it is read, as the imaginary part of a conjugate is: its memory holds other numbers.)
+bool on_gpu(const at::Tensor &t, const at::Device &dev) { return t.is_cuda() && t.has_storage() && t.device() == dev && !t.is_neg(); }
 
 // Elements from a pixel to the next of a channels-last tensor or a channel slice of one; 0: it is neither.
 int64_t pixel_stride(const at::Tensor &t)
@@ -607,7 +608,7 @@ struct NormCall {
     bool read(PyObject *xo, PyObject *groups, PyObject *wo, PyObject *bo, PyObject *ro, PyObject *act, PyObject *eps)
     {
         const at::Tensor *xp = tensor_of(xo);
-        if (!g_operators.norm || !xp || recorders_active() || !xp->defined() || dual(*xp) || !xp->is_cuda() || !xp->has_storage() || xp->dim() != 4) return false;
+        if (!g_operators.norm || !xp || recorders_active() || !xp->defined() || dual(*xp) || !xp->is_cuda() || !xp->has_storage() || xp->is_neg() || xp->dim() != 4) return false;
         x = *xp;
         int64_t g, a;
         if (!read_int(groups, g) || !read_int(act, a) || !read_float(eps, d.eps) || g < 1 || g > x.size(1)) return false;
@@ -744,7 +745,7 @@ struct HeadCall {
     bool read(PyObject *lo, PyObject *to, PyObject *top, PyObject *ignore)
     {
         const at::Tensor *lp = tensor_of(lo);
-        if (!g_operators.head || !lp || recorders_active() || !lp->defined() || dual(*lp) || !lp->is_cuda() || !lp->has_storage() || lp->dim() != 2) return false;
+        if (!g_operators.head || !lp || recorders_active() || !lp->defined() || dual(*lp) || !lp->is_cuda() || !lp->has_storage() || lp->is_neg() || lp->dim() != 2) return false;
         logits = *lp;
         int64_t k;
         if (!optional_tensor(to, targets) || !read_int(top, k) || k < 0 || k > BS_MAX_TOP || !read_int(ignore, d.ignore_index)) return false;
@@ -864,7 +865,7 @@ struct RowsCall {
     // An operand of like's shape, type and device that is read in place (or none).
     bool beside(const at::Tensor &t, int64_t &stride) const
     {
-        return !t.defined() || (on_gpu(t, like.device()) && t.sizes() == like.sizes() && t.scalar_type() == like.scalar_type() && !t.is_neg() && (stride = rows_step(t)) != 0);
+        return !t.defined() || (on_gpu(t, like.device()) && t.sizes() == like.sizes() && t.scalar_type() == like.scalar_type() && (stride = rows_step(t)) != 0);
     }
     bool parameter(const at::Tensor &t, int32_t &type, bool first) const
     {

@@ -101,6 +101,7 @@ def _pixel_stride(t: torch.Tensor) -> Optional[int]:
 
 def _readable(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """`t` and its pixel stride; a copy in channels-last order where it cannot be read in place."""
+    t = t.resolve_neg()
     step = _pixel_stride(t)
     if step is None:
         t = t.contiguous(memory_format=torch.channels_last)
@@ -124,8 +125,8 @@ def _norm_operands(x, groups, weight, bias, residual, activation, eps, grad=None
     if params:
         d.param_dtype = _dtype(params[0], "group_norm")
     for p in params:
-        if tuple(p.shape) != (x.shape[1],) or not p.is_contiguous() or p.device != x.device:
-            raise ValueError("group_norm: weight and bias hold one element a channel, contiguous, on x's device")
+        if tuple(p.shape) != (x.shape[1],) or not p.is_contiguous() or p.is_neg() or p.device != x.device:
+            raise ValueError("group_norm: weight and bias hold one element a channel, contiguous (no negated view), on x's device")
         if p.dtype not in (torch.float32, x.dtype) or p.dtype != params[0].dtype:
             raise TypeError("group_norm: weight and bias are both float32 or both of x's type")
     for t, name in ((residual, "residual"), (grad, "grad")):
@@ -157,7 +158,7 @@ def _run_norm(x, groups, weight, bias, residual, activation, eps, out, keep_stat
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device, memory_format=torch.channels_last)
     else:
         step = _pixel_stride(out)
-        if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or step is None:
+        if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device or step is None or out.is_neg():
             raise ValueError("group_norm: out must have x's shape, type and device, channels last or a channel slice of such a tensor")
         d.y_stride = step
         torch.autograd.graph.increment_version(out)  # (written through its pointer, which autograd does not see)
@@ -301,6 +302,7 @@ def _row_stride(t: torch.Tensor) -> Optional[int]:
 
 
 def _readable_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    t = t.resolve_neg()
     step = _row_stride(t)
     return (t, step) if step is not None else (t.contiguous(), t.shape[1])
 
@@ -362,12 +364,12 @@ def log_probs_backward(logits, targets, lse, entropy, grad_logp=None, grad_entro
             if t is not None and (tuple(t.shape) != (rows,) or t.device != logits.device or
                                   not (t.dtype == torch.float32 or (t is lse and t.dtype == torch.float64))):
                 raise ValueError("log_probs_backward: lse, entropy and their gradients hold one float32 (lse: or float64) a row, on the logits' device")
-            given.append(t.contiguous() if t is not None else None)
+            given.append(t.resolve_neg().contiguous() if t is not None else None)
         lse, entropy, grad_logp, grad_entropy = given
         d.lse_bytes = lse.element_size()
         if out is None:
             out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or _row_stride(out) is None:
+        elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or _row_stride(out) is None or out.is_neg():
             raise ValueError("log_probs_backward: out must have the logits' shape, type and device, its classes contiguous")
         else:
             torch.autograd.graph.increment_version(out)  # (written through its pointer, which autograd does not see)
@@ -676,8 +678,8 @@ def _row_params(params, like: torch.Tensor, dtype: int) -> int:
     code = bs.BS_F32
     given = [p for p in params if p is not None]
     for p in given:
-        if tuple(p.shape) != (like.shape[-1],) or not p.is_contiguous() or p.device != like.device:
-            raise ValueError("layer_norm: weight and bias hold one element a feature, contiguous, on the rows' device")
+        if tuple(p.shape) != (like.shape[-1],) or not p.is_contiguous() or p.is_neg() or p.device != like.device:
+            raise ValueError("layer_norm: weight and bias hold one element a feature, contiguous (no negated view), on the rows' device")
         code = _dtype(p, "layer_norm")
         if code not in (bs.BS_F32, dtype) or p.dtype != given[0].dtype:
             raise TypeError("layer_norm: weight and bias are both float32 or both of the rows' type")
