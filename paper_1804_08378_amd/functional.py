@@ -554,8 +554,8 @@ def _autocasts() -> int:
 
 
 class _Statistics:
-    """Which of the tensors that autograd keeps are statistics: factors of a gradient's formula that have to fit its other operands, where a value next to
-    them makes another formula of it.  As far as they can be told:
+    """Which of the tensors that autograd keeps, one after another, are statistics: factors of a gradient's formula that have to fit its other operands,
+    where a value next to them makes another formula of it.  As far as they can be told:
     - tensors without a gradient (attention's log sums, layer normalisation's statistics; masks and constants too),
     - the second, third ... result of one of torch's own operations that is no view of its operand (group normalisation's mean and deviation),
     - tensors whose sizes are another one's with dimensions taken out, one of the last that were kept (log sums and norms along a dimension).
@@ -568,13 +568,18 @@ class _Statistics:
         self._sizes.clear()
 
     def found(self, t: torch.Tensor) -> bool:
-        sizes = tuple(n for n in t.shape if n != 1)
-        of_another = any(len(sizes) < len(other) and _left_of(sizes, other) for other in self._sizes)
-        if t.is_floating_point():
-            self._sizes.append(sizes)
-        if not t.requires_grad or of_another:
+        if not t.requires_grad:
             return True
-        return t.output_nr > 0 and not t._is_view() and not isinstance(t.grad_fn, torch.autograd.function.BackwardCFunction)
+        sizes = tuple(t.shape)
+        if 1 in sizes:
+            sizes = tuple(n for n in sizes if n != 1)
+        of_another, dims = False, len(sizes)
+        for other in self._sizes:
+            if len(other) > dims and _left_of(sizes, other):
+                of_another = True
+                break
+        self._sizes.append(sizes)
+        return of_another or (t.output_nr > 0 and not t._is_view() and not isinstance(t.grad_fn, torch.autograd.function.BackwardCFunction))
 
 
 def _left_of(sizes: Tuple[int, ...], other: Tuple[int, ...]) -> bool:
@@ -591,8 +596,10 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     Held so are tensors on the GPU of `pack8`'s types and sizes that have a gradient, with at least `least` elements and two dimensions, more than two
     of them in the last, dense in memory (any order of dimensions).  The others stay as they are, and so do the parameters and buffers that
     `model` (a module, or an iterable of tensors) has where the block begins, and any `nn.Parameter`, which are in use anyway; changed in place before the
-    backward pass, they are refused there, as without the block.  A tensor that several nodes keep is held once for each.  Under autocast, whose copies of the
-    weights could not be told from activations, and where an autocast begins inside the block, it refuses.
+    backward pass, they are refused there, as without the block.  A tensor that several nodes keep is held once for each, 1.03 bytes
+    an element and node against the 2 or 4 that it takes as it is, so that the input of three projections in 16 bits takes more than without the block (nothing
+    is looked up by the tensor that it was made of, whose numbers may change without a trace, by a graph's replay for one).  Under autocast, whose copies
+    of the weights could not be told from activations, and where an autocast begins inside the block, it refuses.
 
     What is exact in 16 bits is not so in 8: an element is off by 0.8 % of the largest of 32 neighbours in memory at most.  A ReLU's gradient then takes
     the other side for elements that close to 0, the largest of a pooling window is another one where two are that close; logits lose it from their
@@ -613,12 +620,14 @@ class checkpoints_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
         def held(t):
             """What stands for `t` in 8 bits; None: it stays as it is."""
-            if not t.is_cuda or t.layout != torch.strided or torch.jit.is_tracing() or t.untyped_storage().data_ptr() in memory:
+            kind = type(t)
+            if torch.jit.is_tracing() or not t.is_cuda or not (kind is torch.Tensor or kind is nn.Parameter) or t.dtype not in _DTYPES or \
+                    t.layout != torch.strided or t.dim() < 2 or t.numel() < max(1, least):  # (what is that small is no statistic's operand either)
                 return None
-            if isinstance(t, nn.Parameter) or isinstance(t._base, nn.Parameter):  # (made or moved inside the block)
+            if statistics.found(t) or t.shape[-1] <= 2 or kind is nn.Parameter or t.untyped_storage().data_ptr() in memory:
                 return None
-            if statistics.found(t) or t.dtype not in _DTYPES or t.numel() < max(1, least) or t.dim() < 2 or t.shape[-1] <= 2 or \
-                    type(t) not in (torch.Tensor, nn.Parameter):
+            base = t._base
+            if base is not None and isinstance(base, nn.Parameter):  # (made or moved inside the block)
                 return None
             order = _dense_order(t)
             if order is None:
@@ -866,8 +875,8 @@ def _run_activate(x, activation, gate, checkpoint, recorded=False, traced=False)
 
 
 def activate_forward(x, activation: str = "silu", gate=None, checkpoint: bool = False) -> Activated:
-    """act(x) * gate, or act(x); `checkpoint`: x and gate too in 8 bits.  Rows (the last dimension) of either operand may lie further apart than they
-    are long, as in the halves of one product's result (other memory orders are copied first)."""
+    """act(x) * gate, or act(x); `checkpoint`: x and gate too in 8 bits.  A ReLU of NaN is 0, where torch's is NaN.  Rows (the last dimension) of either
+    operand may lie further apart than they are long, as in the halves of one product's result (other memory orders are copied first)."""
     return _run_activate(x, activation, gate, checkpoint)
 
 

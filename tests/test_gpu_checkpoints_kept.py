@@ -5,6 +5,7 @@ from torch import nn
 
 import rows_reference as ref
 from paper_1804_08378_amd import functional as F
+from paper_1804_08378_amd.frontend import optimize
 
 pytestmark = pytest.mark.gpu
 
@@ -65,6 +66,14 @@ def test_a_log_sum_stays_as_it_is(held):
     assert float((g.cpu().double() - want).abs().max()) <= 2e-5 * float(want.max())  # (arguments of up to 55 and results: roundings of 2^-24 of 55, 8e-6 in all)
 
 
+def test_norms_of_parameters_stay_as_they_are(held):
+    w = nn.Parameter(torch.randn(64, 512, 8, device="cuda"))
+    with F.checkpoints_in_8_bits([w]):
+        y = w.norm(dim=-1)
+    assert not held
+    torch.testing.assert_close(torch.autograd.grad(y.sum(), w)[0], w.detach() / y.detach()[..., None])
+
+
 def test_what_has_no_gradient_stays_as_it_is(held):
     x, constant = torch.randn(256, 256, device="cuda", requires_grad=True), torch.randn(256, 256, device="cuda")
     with F.checkpoints_in_8_bits([]):
@@ -88,6 +97,25 @@ def test_the_operators_here_keep_their_operands_so(held):
         v = n(m)
     assert held == [x.numel()] * 3 + [m.numel()]
     assert all(g.isfinite().all() for g in torch.autograd.grad(z.sum() + v.sum(), (x, a, m)))
+
+
+def test_stacks_and_batch_normalisations(held):
+    """A stack's operand, the result of a convolution, is held; a batch normalisation in training mode too keeps its operand so, and may run twice."""
+    model = nn.Sequential(nn.Conv2d(8, 32, 3, padding=1), nn.BatchNorm2d(32), nn.ReLU(), nn.AvgPool2d(2)).cuda().eval()
+    for p in model[1].parameters():
+        p.requires_grad_(False)
+    fast = optimize(model)
+    x = torch.randn(8, 8, 32, 32, device="cuda")
+    with F.checkpoints_in_8_bits(fast, least=64):
+        y = fast(x)
+    assert held == [8 * 32 * 32 * 32]
+    assert all(g.isfinite().all() for g in torch.autograd.grad(y.sum(), [*model[0].parameters()]))
+    held.clear()
+    m = nn.Sequential(nn.Conv2d(8, 32, 1), nn.BatchNorm2d(32)).cuda()
+    with F.checkpoints_in_8_bits(m, least=64):
+        y = m(x) + m(x * 2.0)
+    assert held == [8 * 32 * 32 * 32] * 2
+    assert all(g.isfinite().all() for g in torch.autograd.grad(y.sum(), [*m.parameters()]))
 
 
 # ------------------------------------------------------------------------------------------------ parameters
