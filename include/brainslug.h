@@ -643,7 +643,8 @@ BS_API bs_status bs_unpack8(const bs_pack8_desc *desc, const int8_t *codes, cons
  * Activation with an optional gate: y = act(x) * gate, or act(x), over rows of `columns` elements, and the gradients
  *   grad_x = grad_y * gate * act'(x),  grad_gate = grad_y * act(x).
  * The forward pass can leave x and gate in 8 bits (above) for the backward pass, which then computes at the values they stand for.
- * Arithmetic is float32, results are rounded once to the storage type.
+ * Arithmetic is float32, results are rounded once to the storage type.  relu(NaN) is 0 and so is its gradient (z > 0 is false), as in stacks and
+ * bs_group_norm; the other activations pass NaN on.
  */
 typedef struct bs_activate_desc {
     int64_t rows, columns; /* rows may be 0: nothing is enqueued                      */
@@ -697,7 +698,7 @@ typedef struct bs_layer_norm_desc {
  *   x, addend         device (addend NULL: none), aligned to their element size, as are all tensors here
  *   weight, bias      device, `features` elements each; NULL: ones, zeros
  *   y                 device, written
- *   total             device, written: t.  NULL: not wanted
+ *   total             device, written: t (without an addend: x).  NULL: not wanted
  *   stats             device, 8-byte aligned, written: mean and 1 / sqrt(var + eps) of every row, floats; NULL: not wanted
  *   codes, exponents  device, written: t in 8 bits; both NULL: not wanted
  * No output shares a byte with an input or another output.
